@@ -487,6 +487,231 @@ typedef struct wfst_debug_opts {
 
 int wfst_set_debug_opts(const wfst_debug_opts *opts);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Acoustic-model operators: what makes the log-likelihood rows that the
+ * search reads.  The layers of a feed-forward acoustic model (matrix product
+ * with bias, activation and residual; root-mean-square norm with the
+ * residual's addition and an output in 8 bits), its training from a teacher's
+ * top logits, and the conversion of its logits to rows for wfst_decode.
+ *
+ * Unlike the decode calls these only enqueue: a call checks its arguments,
+ * launches its kernels on hip_stream (of the current HIP device) and returns.
+ * It allocates nothing, copies nothing to or from the host and may be
+ * captured into a HIP graph.  All matrices, vectors and workspaces are device
+ * memory of the current device and must stay valid until the stream has
+ * passed the call.  Outputs must not overlap inputs or one another, except
+ * where a call says so.  Results do not depend on timing: no sum is taken in
+ * an order that can change from run to run.
+ *
+ * Sums, statistics and everything between the inputs and an output are held
+ * in float32; an output in fewer bits is rounded once, to nearest, ties to
+ * even, on its way out (wfst_am_linear_backward states the one exception).
+ * An infinity or NaN reaches the outputs that depend on it by the formula.
+ */
+#define WFST_F32 0
+#define WFST_F16 1
+#define WFST_BF16 2
+#define WFST_F8E4M3 3   /* OCP e4m3: 448 is the largest value, no infinities */
+
+/* A row-major matrix: element (r, c) is data[r * row_stride + c].  data is
+   aligned to its element type; larger alignment of data and row_stride (16
+   bytes) is faster.  Where a matrix is optional, data == NULL leaves it out
+   (its other fields are then not read). */
+typedef struct wfst_matrix {
+    void *data;
+    int64_t rows, cols;   /* each < 2^31 */
+    int64_t row_stride;   /* elements, >= cols */
+    int32_t type;         /* WFST_F32, ... */
+    int32_t reserved;     /* 0 */
+} wfst_matrix;
+
+/* activations */
+#define WFST_ACT_NONE 0
+#define WFST_ACT_RELU 1   /* max(z, 0); slope 0 at 0 */
+#define WFST_ACT_SILU 2   /* z / (1 + exp(-z)) */
+#define WFST_ACT_GELU 3   /* z / 2 (1 + erf(z / sqrt 2)) */
+
+/*
+ * wfst_am_linear -- one layer over M rows:
+ *   z[m][n] = sum_k x[m][k] w[n][k]  (* x_scale[m] * w_scale[n])  + bias[n]
+ *   y[m][n] = act(z[m][n]) + residual[m][n]
+ *
+ *   x        [M x K], w [N x K], of one type: WFST_F16, WFST_BF16 or
+ *            WFST_F8E4M3; M >= 0, K >= 1, N >= 1
+ *   residual [M x N] optional, of y's type; may be y itself (same data,
+ *            stride and type)
+ *   pre      [M x N] optional output: z, of y's type (for the gradient)
+ *   y        [M x N] output, WFST_F32, WFST_F16 or WFST_BF16
+ *   x_scale  [M], w_scale [N] float32: what an 8-bit row stands for, times
+ *            its elements; both needed with WFST_F8E4M3, both NULL otherwise
+ *   bias     [N] float32 or NULL
+ *
+ * Errors: WFST_EINVAL, WFST_EDEVICE.
+ */
+typedef struct wfst_am_linear_args {
+    wfst_matrix x, w, residual, pre, y;
+    const float *x_scale, *w_scale, *bias;
+    int32_t activation;
+    int32_t reserved;
+} wfst_am_linear_args;
+
+int wfst_am_linear(const wfst_am_linear_args *args, void *hip_stream);
+
+/*
+ * wfst_am_linear_backward -- gradients of wfst_am_linear (16-bit types; the
+ * residual's gradient is dy itself):
+ *   dz = dy * act'(pre);  dx = dz w;  dw = dz^T x;  dbias[n] = sum_m dz[m][n]
+ *
+ *   dy, pre  [M x N], x [M x K], w [N x K], all of one type, WFST_F16 or
+ *            WFST_BF16; pre is not read with WFST_ACT_NONE
+ *   dx [M x K], dw [N x K], dbias [N] float32: outputs, each optional; dx and
+ *            dw WFST_F32, WFST_F16 or WFST_BF16.  x is read for dw only and w
+ *            for dx only (data may be NULL otherwise)
+ *   workspace  at least wfst_am_linear_backward_workspace bytes, 256-byte
+ *            aligned
+ *
+ * The matrix products read dz in the 16-bit type (the matrix cores multiply
+ * 16-bit operands); dbias sums the unrounded dz.  M = 0 gives zero dw, dbias.
+ * Errors: WFST_EINVAL (also a workspace that is too small), WFST_EDEVICE.
+ */
+typedef struct wfst_am_linear_backward_args {
+    wfst_matrix dy, pre, x, w, dx, dw;
+    float *dbias;
+    void *workspace;
+    int64_t workspace_bytes;
+    int32_t activation;
+    int32_t reserved;
+} wfst_am_linear_backward_args;
+
+/* The workspace that args needs (its workspace fields and data pointers are
+   only tested for NULL); it depends on sizes, types and which outputs are
+   asked for. */
+int wfst_am_linear_backward_workspace(const wfst_am_linear_backward_args *args, int64_t *bytes);
+int wfst_am_linear_backward(const wfst_am_linear_backward_args *args, void *hip_stream);
+
+/*
+ * wfst_am_norm -- root-mean-square norm of each row, with the residual's
+ * addition before it and an output in 8 bits after it:
+ *   s = x + residual;  v = s / sqrt(mean(s^2) + eps) * gain
+ *   y = v, or with y of type WFST_F8E4M3:
+ *   y_scale = max|v| / 448 (at least the smallest normal float32; a row of
+ *   zeros gives zeros),  y = v / y_scale
+ *
+ *   x        [M x D], WFST_F32, WFST_F16 or WFST_BF16; M >= 0, D >= 1
+ *   residual [M x D] optional, of x's type
+ *   sum      [M x D] optional output: s, of x's type; may be x or residual
+ *            itself (same data and stride).  The norm is taken of the
+ *            unrounded s
+ *   y        [M x D] output, any type
+ *   y_scale  [M] float32, needed with WFST_F8E4M3, NULL otherwise
+ *   gain     [D] float32 or NULL (ones);  eps > 0, finite
+ *
+ * Errors: WFST_EINVAL, WFST_EDEVICE.
+ */
+typedef struct wfst_am_norm_args {
+    wfst_matrix x, residual, sum, y;
+    const float *gain;
+    float *y_scale;
+    float eps;
+    int32_t reserved;
+} wfst_am_norm_args;
+
+int wfst_am_norm(const wfst_am_norm_args *args, void *hip_stream);
+
+/*
+ * wfst_am_norm_backward -- gradients of v (wfst_am_norm) with respect to s
+ * and gain; with u = dy * gain and r = 1 / sqrt(mean(s^2) + eps):
+ *   dx = r (u - s r^2 mean(u s)) + dsum;  dgain[d] = sum_m dy[m][d] s[m][d] r[m]
+ *
+ *   dy, s    [M x D] of one type, WFST_F32, WFST_F16 or WFST_BF16
+ *   dsum     [M x D] optional, of that type: the gradient that reaches s past
+ *            the norm (the residual stream's)
+ *   dx       [M x D] optional output of that type: the gradient of x and of
+ *            residual; may be dy or dsum itself (same data and stride)
+ *   dgain    [D] float32, optional output (zeros for M = 0)
+ *   workspace  at least wfst_am_norm_backward_workspace bytes, 256-byte aligned
+ *
+ * Errors: WFST_EINVAL, WFST_EDEVICE.
+ */
+typedef struct wfst_am_norm_backward_args {
+    wfst_matrix dy, s, dsum, dx;
+    const float *gain;
+    float *dgain;
+    void *workspace;
+    int64_t workspace_bytes;
+    float eps;
+    int32_t reserved;
+} wfst_am_norm_backward_args;
+
+int wfst_am_norm_backward_workspace(const wfst_am_norm_backward_args *args, int64_t *bytes);
+int wfst_am_norm_backward(const wfst_am_norm_backward_args *args, void *hip_stream);
+
+/*
+ * wfst_am_distill -- loss of a student's logits against a teacher's top
+ * logits, and its gradient.  Per row m, over the used entries j of the
+ * teacher's k (an index inside [0, L) and a logit above -inf; a unit that
+ * occurs twice counts twice):
+ *   p = softmax(top_logit / temperature),  q = softmax(logits / temperature)
+ *   loss[m]       = weight[m] temperature^2 sum_j p_j (log p_j - log q[top_index_j])
+ *   dlogits[m][l] = weight[m] temperature (q[l] - sum of p_j with top_index_j = l)
+ * A row without a used entry, or with weight 0 (a padded frame), has loss 0
+ * and gradient 0 whatever its logits hold.  A term with p_j = 0 is 0.
+ *
+ *   logits    [M x L] WFST_F32, WFST_F16 or WFST_BF16; M >= 0, L >= 1
+ *   top_logit [M x k] of any of these types, 1 <= k <= 256
+ *   top_index [M x k] int32, dense
+ *   weight    [M] float32 or NULL (ones); temperature > 0, finite
+ *   loss      [M] float32 output, optional
+ *   lse       [M] float32 output, optional: log sum exp(logits / temperature),
+ *             which wfst_am_distill_backward reads
+ *   dlogits   [M x L] output, optional, of the logits' type; may be logits
+ *             itself (same data and stride)
+ *
+ * Errors: WFST_EINVAL, WFST_EDEVICE.
+ */
+#define WFST_AM_MAX_TOP 256
+
+typedef struct wfst_am_distill_args {
+    wfst_matrix logits, top_logit, dlogits;
+    const int32_t *top_index;
+    const float *weight;
+    float *loss;
+    float *lse;
+    float temperature;
+    int32_t reserved;
+} wfst_am_distill_args;
+
+int wfst_am_distill(const wfst_am_distill_args *args, void *hip_stream);
+
+/* The gradient alone, for a loss whose weights are known only after it
+   (weight[m] = the gradient that reaches loss[m], times the forward call's
+   weight): reads lse, writes dlogits; loss is not touched. */
+int wfst_am_distill_backward(const wfst_am_distill_args *args, void *hip_stream);
+
+/*
+ * wfst_am_loglikes -- logits to the rows that wfst_decode reads:
+ *   ll[m][l] = scale (logits[m][l] - log sum_l' exp(logits[m][l']) - log_prior[l])
+ * A unit whose logit or log prior is -inf (never seen in training) has ll
+ * -inf, and so has a row whose logits are all -inf.  Logits without NaN or
+ * +inf give rows that the decode calls accept.
+ *
+ *   logits    [M x L] WFST_F32, WFST_F16 or WFST_BF16; M >= 0, L >= 1
+ *   ll        [M x L] float32 output
+ *   log_prior [L] float32 or NULL (zeros): the log probability of each unit;
+ *             scale > 0, finite: the acoustic scale
+ *
+ * Errors: WFST_EINVAL, WFST_EDEVICE.
+ */
+typedef struct wfst_am_loglikes_args {
+    wfst_matrix logits, ll;
+    const float *log_prior;
+    float scale;
+    int32_t reserved;
+} wfst_am_loglikes_args;
+
+int wfst_am_loglikes(const wfst_am_loglikes_args *args, void *hip_stream);
+
 /* One environment switch, read once per process: WFSTDEC_DEBUG_TIMING (any
  * value) prints a wall-clock breakdown of each decode call on stderr (setup,
  * search, results; the workspace split and the frames redone on the
