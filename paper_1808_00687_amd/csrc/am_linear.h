@@ -1,0 +1,48 @@
+// What the files of the acoustic model's matrix products share.
+#pragma once
+
+#include "am_tile.h"
+
+namespace wfd {
+
+// out = a b^T, both k-contiguous (am_linear_f16.hip, am_linear_bf16.hip, am_linear_f8.hip)
+template <typename E>
+void am_product_forward(const AmProduct &p, hipStream_t st);
+// dx[m][k] = sum_n dz[m][n] w[n][k]: w is k-major
+template <typename E>
+void am_product_dx(const AmProduct &p, hipStream_t st);
+// dw[n][k] = sum_m dz[m][n] x[m][k]: both are k-major
+template <typename E>
+void am_product_dw(const AmProduct &p, hipStream_t st);
+
+inline bool am_rows_aligned(const wfst_matrix &m)
+{
+    return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && m.row_stride * am_type_bytes(m.type) % 16 == 0;
+}
+
+// row stride of dz in the workspace: rows on 16 bytes
+constexpr int64_t am_dz_stride(int64_t n) { return (n + 7) & ~int64_t{7}; }
+
+struct BackwardPlan {
+    int64_t dz_bytes, partial_bytes;
+    int32_t dx_splits, dw_splits;
+};
+
+inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a)
+{
+    const int64_t M = a.dy.rows, N = a.dy.cols;
+    BackwardPlan p{0, 0, 1, 1};
+    if (a.activation != WFST_ACT_NONE && (a.dx.data || a.dw.data)) p.dz_bytes = (M * am_dz_stride(N) * 2 + 255) & ~int64_t{255};
+    if (a.dx.data) {
+        p.dx_splits = am_splits(M, a.dx.cols, N);
+        p.partial_bytes = am_partial_bytes(M, a.dx.cols, p.dx_splits);
+    }
+    if (a.dw.data) {
+        p.dw_splits = am_splits(N, a.dw.cols, M);
+        const int64_t b = am_partial_bytes(N, a.dw.cols, p.dw_splits);
+        p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
+    }
+    return p;
+}
+
+}  // namespace wfd

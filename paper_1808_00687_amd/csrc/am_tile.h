@@ -1,0 +1,543 @@
+// Tiled matrix products on the matrix cores:
+//   out[i][j] = epilogue(sum_k a[i][k] b[j][k])
+// with each operand stored k-contiguous (rows of k) or k-major (rows of i or
+// j, one row a k).
+//
+// A workgroup computes a BM x BN tile, stage by stage: a stage holds 128 bytes
+// of k for every row of the tile (64 values of 16 bits, 128 of 8).  Two stages
+// lie in LDS; the next one is fetched while the matrix cores work on the
+// present one.  The fetch goes straight from memory to LDS (16 bytes a lane, no
+// registers); operands that are not aligned to 16 bytes go through registers.
+//
+// LDS layout.  A stage is a row of 16-byte chunks for each row of the operand
+// as stored; a chunk sits at its index XOR a function of the row, so that the
+// lanes of one read meet all banks.  The memory-to-LDS fetch writes lane after
+// lane, so the permutation is applied to the address that a lane reads.
+//   k-contiguous: a lane's fragment is one chunk (8 values of 16 bits) of its row
+//   k-major: a fragment is gathered by two transposing LDS reads; each takes 4
+//   rows (k) by 16 columns from a group of 16 lanes and hands every lane its
+//   column's 4 values
+// The order of k inside a fragment does not matter as long as both operands
+// have the same.
+//
+// The product is issued with b as the first matrix-core operand, so a lane's
+// results are 4 consecutive j of one i.  Where b is k-contiguous the rows of b
+// are dealt to the fragments so that a lane holds 4 * TJ consecutive j.
+#pragma once
+
+#include "am_device.h"
+
+namespace wfd {
+
+using i16x4 = short __attribute__((ext_vector_type(4)));
+using i32x4 = int __attribute__((ext_vector_type(4)));
+using i32x4_any = int __attribute__((ext_vector_type(4), aligned(1)));   // at any address
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using f16x8 = f16 __attribute__((ext_vector_type(8)));
+using bf16x8 = bf16 __attribute__((ext_vector_type(8)));
+
+#define AM_LDS __attribute__((address_space(3)))
+#define AM_GLOBAL __attribute__((address_space(1)))
+
+constexpr int kStageBytes = 128;   // of k, a row
+
+struct AmOperand {
+    const char *data;
+    int64_t ld;        // bytes between rows as stored
+    int32_t extent;    // i or j
+};
+
+struct AmProduct {
+    AmOperand a, b;
+    int32_t inner;             // k
+    int32_t splits;            // parts of k, one workgroup each per tile; > 1: sums go to `partial`
+    float *partial;            // [splits][a.extent][b.extent]
+    const float *a_scale, *b_scale, *bias;
+    wfst_matrix residual, pre, out;
+    int32_t activation;
+    int32_t vec;               // out, residual and pre have 16-byte aligned rows
+};
+
+__device__ __forceinline__ float am_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+__device__ __forceinline__ float am_silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + am_exp(-z)); }
+
+__device__ __forceinline__ float am_gelu(float z) { return 0.5f * z * (1.0f + erff(z * 0.70710678f)); }
+
+template <int N>
+__device__ __forceinline__ void am_activate(float (&v)[N], int32_t kind)
+{
+    if (kind == WFST_ACT_RELU)
+        #pragma unroll
+        for (int i = 0; i < N; i++) v[i] = v[i] < 0.0f ? 0.0f : v[i];   // a NaN stays one
+    else if (kind == WFST_ACT_SILU)
+        #pragma unroll
+        for (int i = 0; i < N; i++) v[i] = am_silu(v[i]);
+    else if (kind == WFST_ACT_GELU)
+        #pragma unroll
+        for (int i = 0; i < N; i++) v[i] = am_gelu(v[i]);
+}
+
+// N consecutive values of row i from column j on; `full`: all inside, rows 16-byte aligned
+template <typename T, int N>
+__device__ __forceinline__ void am_store_row(const wfst_matrix &m, int64_t i, int64_t j, const float (&v)[N], bool full)
+{
+    T *p = static_cast<T *>(m.data) + i * m.row_stride + j;
+    constexpr int kStep = N * sizeof(T) >= 16 ? 16 / sizeof(T) : N;
+    using V = T __attribute__((ext_vector_type(kStep)));
+    if (full) {
+        #pragma unroll
+        for (int s = 0; s < N; s += kStep) {
+            V t;
+            #pragma unroll
+            for (int e = 0; e < kStep; e++) t[e] = static_cast<T>(v[s + e]);
+            *(AM_GLOBAL V *)(p + s) = t;
+        }
+        return;
+    }
+    #pragma unroll
+    for (int e = 0; e < N; e++)
+        if (j + e < m.cols) ((AM_GLOBAL T *)p)[e] = static_cast<T>(v[e]);
+}
+
+template <int N>
+__device__ __forceinline__ void am_store(const wfst_matrix &m, int64_t i, int64_t j, const float (&v)[N], bool full)
+{
+    if (m.type == WFST_BF16) am_store_row<bf16>(m, i, j, v, full);
+    else if (m.type == WFST_F16) am_store_row<f16>(m, i, j, v, full);
+    else am_store_row<float>(m, i, j, v, full);
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void am_add_row(const wfst_matrix &m, int64_t i, int64_t j, float (&v)[N], bool full)
+{
+    const T *p = static_cast<const T *>(m.data) + i * m.row_stride + j;
+    constexpr int kStep = N * sizeof(T) >= 16 ? 16 / sizeof(T) : N;
+    using V = T __attribute__((ext_vector_type(kStep)));
+    if (full) {
+        #pragma unroll
+        for (int s = 0; s < N; s += kStep) {
+            const V t = *(const AM_GLOBAL V *)(p + s);
+            #pragma unroll
+            for (int e = 0; e < kStep; e++) v[s + e] += static_cast<float>(t[e]);
+        }
+        return;
+    }
+    #pragma unroll
+    for (int e = 0; e < N; e++)
+        if (j + e < m.cols) v[e] += static_cast<float>(((const AM_GLOBAL T *)p)[e]);
+}
+
+template <int N>
+__device__ __forceinline__ void am_add(const wfst_matrix &m, int64_t i, int64_t j, float (&v)[N], bool full)
+{
+    if (m.type == WFST_BF16) am_add_row<bf16>(m, i, j, v, full);
+    else if (m.type == WFST_F16) am_add_row<f16>(m, i, j, v, full);
+    else am_add_row<float>(m, i, j, v, full);
+}
+
+// The epilogue of N consecutive j of row i (j < cols), their scales and biases at hand.
+template <int N>
+__device__ __forceinline__ void am_finish(const AmProduct &p, int64_t i, int64_t j, float (&v)[N],
+                                          const float (&b_scale)[N], const float (&bias)[N])
+{
+    const bool full = p.vec && j + N <= p.b.extent;
+    if (p.a_scale) {
+        const float s = p.a_scale[i];
+        #pragma unroll
+        for (int e = 0; e < N; e++) v[e] *= s * b_scale[e];
+    }
+    if (p.bias)
+        #pragma unroll
+        for (int e = 0; e < N; e++) v[e] += bias[e];
+    if (p.pre.data) am_store(p.pre, i, j, v, full);
+    am_activate(v, p.activation);
+    if (p.residual.data) am_add(p.residual, i, j, v, full);
+    am_store(p.out, i, j, v, full);
+}
+
+template <int N>
+__device__ __forceinline__ void am_columns(const AmProduct &p, int64_t j, float (&b_scale)[N], float (&bias)[N])
+{
+    #pragma unroll
+    for (int e = 0; e < N; e++) {
+        const int64_t c = j + e < p.b.extent ? j + e : p.b.extent - 1;
+        b_scale[e] = p.b_scale ? p.b_scale[c] : 1.0f;
+        bias[e] = p.bias ? p.bias[c] : 0.0f;
+    }
+}
+
+template <typename E>
+__device__ __forceinline__ f32x4 am_mfma(i32x4 x, i32x4 y, f32x4 c)
+{
+    if constexpr (__is_same(E, f16))
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+}
+
+// 16 e4m3 values as bf16, which holds each exactly
+__device__ __forceinline__ void am_widen(i32x4 v, i32x4 &lo, i32x4 &hi)
+{
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+        lo[2 * e] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e], 1.0f, false));
+        lo[2 * e + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e], 1.0f, true));
+        hi[2 * e] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e + 2], 1.0f, false));
+        hi[2 * e + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e + 2], 1.0f, true));
+    }
+}
+
+// Tile (ti, tj) of workgroup `block` of `count`.  Workgroups go to the 8
+// chiplets in turn; each chiplet gets a run of consecutive tiles, and runs go
+// through blocks of 8 rows of tiles, so a chiplet's L2 sees few rows and columns.
+__device__ __forceinline__ void am_tile_of(uint32_t block, uint32_t rows, uint32_t cols, uint32_t &ti, uint32_t &tj)
+{
+    const uint32_t count = rows * cols, each = count / 8, more = count % 8, xcd = block % 8;
+    const uint32_t t = xcd * each + (xcd < more ? xcd : more) + block / 8;
+    const uint32_t group = t / (8 * cols), at = t % (8 * cols);
+    const uint32_t height = rows - group * 8 < 8 ? rows - group * 8 : 8;
+    ti = group * 8 + at % height;
+    tj = at / height;
+}
+
+constexpr int am_log2(int x) { return x <= 1 ? 0 : 1 + am_log2(x / 2); }
+
+// One operand's part of the tile kernel: R rows (i or j), kMajor its storage,
+// kDeal > 1: rows dealt to fragments so that a lane gets kDeal runs of 4 rows.
+template <typename E, int R, int kWaves, bool kMajor, int kDeal>
+struct AmSide {
+    static constexpr int kEl = sizeof(E);
+    static constexpr int kPerWave = R / 8 / kWaves;      // fetches of 1 KiB a wave
+    static constexpr int kRowChunks = kMajor ? R * kEl / 16 : 8;
+    static constexpr int kBytes = R * kStageBytes;
+    static_assert(R % (8 * kWaves) == 0, "a stage is whole fetches");
+
+    // chunk permutation of a stored row
+    __device__ static __forceinline__ int permute(int row)
+    {
+        if constexpr (kMajor) {
+            // 16 lanes read 4 rows, 32 lanes 8: rows 0-3 and 8-11 (or 4 more), 32 bytes each
+            if constexpr (kRowChunks >= 16) return ((row & 3) | ((row >> 3) & 1) << 2) << 1;
+            else return (((row >> 1) & 1) | ((row >> 3) & 1) << 1) << 1;
+        } else if constexpr (kDeal > 1) {
+            return ((row >> 1) & 1) | ((row >> (2 + am_log2(kDeal))) & 3) << 1;
+        } else {
+            return (row >> 1) & 7;
+        }
+    }
+
+    int32_t voff[kPerWave];      // direct: byte offset of each fetch from the stage's base
+
+    // the row as stored, and the chunk in it, that a lane fetches
+    __device__ static __forceinline__ int row_of(int q, int wave, int lane) { return ((wave * kPerWave + q) * 64 + lane) / kRowChunks; }
+    __device__ static __forceinline__ int chunk_of(int q, int wave, int lane)
+    {
+        return (lane % kRowChunks) ^ permute(row_of(q, wave, lane));
+    }
+    static_assert(64 % kRowChunks == 0 || kRowChunks % 64 == 0, "");
+
+    __device__ __forceinline__ void init(const AmOperand &o, int wave, int lane)
+    {
+#pragma unroll
+        for (int q = 0; q < kPerWave; q++)
+            voff[q] = row_of(q, wave, lane) * static_cast<int32_t>(o.ld) + chunk_of(q, wave, lane) * 16;
+    }
+
+    // Before the fetch of a last, partial stage with `tail` bytes of k: chunks
+    // from k's end on get an offset past any range.  k-major rows past the end
+    // are past the range already.
+    __device__ __forceinline__ void cut(int32_t tail, int wave, int lane)
+    {
+        if constexpr (!kMajor)
+#pragma unroll
+            for (int q = 0; q < kPerWave; q++)
+                voff[q] = chunk_of(q, wave, lane) * 16 < tail ? voff[q] : static_cast<int32_t>(0x80000000u);
+    }
+
+    // Straight to LDS.  Rows past the operand's end are past the range of the
+    // buffer descriptor and read as zeros.
+    __device__ __forceinline__ void fetch(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, char *stage, int wave)
+    {
+        int64_t skip, size;
+        if constexpr (kMajor) {
+            skip = k0 * o.ld + first * kEl;
+            size = (static_cast<int64_t>(inner) - 1) * o.ld + static_cast<int64_t>(o.extent) * kEl;
+        } else {
+            skip = first * o.ld + static_cast<int64_t>(k0) * kEl;
+            size = (static_cast<int64_t>(o.extent) - 1) * o.ld + static_cast<int64_t>(inner) * kEl;
+        }
+        const int64_t left = size - skip;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(o.data) + skip, 0,
+                                                            static_cast<int>(left < 0x7FFFFFFF ? left : 0x7FFFFFFF), 0x00027000);
+#pragma unroll
+        for (int q = 0; q < kPerWave; q++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (AM_LDS void *)((AM_LDS char *)stage + (wave * kPerWave + q) * 1024),
+                                                     16, voff[q], 0, 0, 0);
+    }
+
+    // Through registers, any alignment: what is outside reads as zeros.
+    __device__ __forceinline__ void load(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, i32x4 (&r)[kPerWave], int wave, int lane)
+    {
+        #pragma unroll
+        for (int q = 0; q < kPerWave; q++) {
+            const int row = row_of(q, wave, lane), chunk = chunk_of(q, wave, lane);
+            const int64_t k = kMajor ? k0 + row : k0 + chunk * (16 / kEl);
+            const int64_t x = kMajor ? first + chunk * (16 / kEl) : first + row;
+            const int64_t along = kMajor ? o.extent - x : inner - k;      // values left in the stored row
+            const bool inside = kMajor ? k < inner : x < o.extent;
+            const AM_GLOBAL char *p = (const AM_GLOBAL char *)o.data + (kMajor ? k * o.ld + x * kEl : x * o.ld + k * kEl);
+            i32x4 v = {0, 0, 0, 0};
+            if (inside && along >= 16 / kEl) {
+                v = *(const AM_GLOBAL i32x4_any *)p;
+            } else if (inside && along > 0) {
+                uint32_t w[4] = {0, 0, 0, 0};
+                #pragma unroll
+                for (int e = 0; e < 16 / kEl; e++)
+                    if (e < along) {
+                        uint32_t t;
+                        if constexpr (kEl == 2) t = ((const AM_GLOBAL uint16_t *)p)[e];
+                        else t = ((const AM_GLOBAL uint8_t *)p)[e];
+                        w[e * kEl / 4] |= t << (e * kEl % 4 * 8);
+                    }
+                v = i32x4{static_cast<int>(w[0]), static_cast<int>(w[1]), static_cast<int>(w[2]), static_cast<int>(w[3])};
+            }
+            r[q] = v;
+        }
+    }
+    __device__ __forceinline__ void put(const i32x4 (&r)[kPerWave], char *stage, int wave, int lane)
+    {
+        #pragma unroll
+        for (int q = 0; q < kPerWave; q++)
+            *reinterpret_cast<i32x4 *>(stage + ((wave * kPerWave + q) * 64 + lane) * 16) = r[q];
+    }
+
+    // Fragment f (of the wave's rows from `base` on), half kk of a stage's k (32 values of 16 bits, 64 of 8)
+    __device__ __forceinline__ i32x4 fragment(const char *stage, int base, int f, int kk, int lane) const
+    {
+        const int g = lane >> 4, s = lane & 15;
+        if constexpr (kMajor) {
+            i16x4 h[2];
+            #pragma unroll
+            for (int t = 0; t < 2; t++) {
+                const int row = kk * 32 + g * 8 + t * 4 + (s >> 2), col = base + f * 16 + (s & 3) * 4;
+                const int at = row * (R * kEl) + (((col >> 3) ^ permute(row)) << 4) + (col & 7) * 2;
+                h[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AM_LDS i16x4 *)((AM_LDS char *)stage + at));
+            }
+            return __builtin_bit_cast(i32x4, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int row = kDeal > 1 ? base + (s >> 2) * (4 * kDeal) + f * 4 + (s & 3) : base + f * 16 + s;
+            return *reinterpret_cast<const i32x4 *>(stage + row * kStageBytes + (((kk * 4 + g) ^ permute(row)) << 4));
+        }
+    }
+};
+
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64, 2) void am_tile_kernel(AmProduct p)
+{
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub alone
+    constexpr int kWaves = WM * WN, TI = BM / WM / 16, TJ = BN / WN / 16;
+    constexpr int kDeal = kMajorB ? 1 : TJ;
+    using SideA = AmSide<E, BM, kWaves, kMajorA, 1>;
+    using SideB = AmSide<E, BN, kWaves, kMajorB, kDeal>;
+    // one object a stage, so the compiler knows that a fetch into one does not touch the other
+    __shared__ __attribute__((aligned(1024))) char a0[SideA::kBytes], b0[SideB::kBytes], a1[SideA::kBytes], b1[SideB::kBytes];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t ti, tj;
+    am_tile_of(blockIdx.x, (p.a.extent + BM - 1) / BM, (p.b.extent + BN - 1) / BN, ti, tj);
+    const int64_t i0 = static_cast<int64_t>(ti) * BM, j0 = static_cast<int64_t>(tj) * BN;
+    const int wi = wave / WN * (BM / WM), wj = wave % WN * (BN / WN);
+
+    constexpr int kStageK = kStageBytes / sizeof(E);
+    const int32_t stages = (p.inner + kStageK - 1) / kStageK;
+    const int32_t s_first = static_cast<int32_t>(static_cast<int64_t>(stages) * blockIdx.y / p.splits);
+    const int32_t s_last = static_cast<int32_t>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / p.splits);
+
+    SideA sa;
+    SideB sb;
+    f32x4 acc[TI][TJ];
+    #pragma unroll
+    for (int f = 0; f < TI; f++)
+        #pragma unroll
+        for (int g = 0; g < TJ; g++) acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const auto multiply = [&](const char *as, const char *bs) {
+#pragma unroll
+        for (int kk = 0; kk < 2; kk++) {
+            if constexpr (sizeof(E) == 1) {
+                // The 8-bit matrix instructions drop the low bits of products far below the largest one of
+                // their 128 (errors up to 2^-12 of it); as bf16 the products and their sums are kept in 32 bits
+                i32x4 y0[TJ], y1[TJ], x0, x1;
+#pragma unroll
+                for (int g = 0; g < TJ; g++) am_widen(sb.fragment(bs, wj, g, kk, lane), y0[g], y1[g]);
+#pragma unroll
+                for (int f = 0; f < TI; f++) {
+                    am_widen(sa.fragment(as, wi, f, kk, lane), x0, x1);
+#pragma unroll
+                    for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<bf16>(y0[g], x0, acc[f][g]);
+#pragma unroll
+                    for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<bf16>(y1[g], x1, acc[f][g]);
+                }
+            } else {
+                i32x4 y[TJ];
+#pragma unroll
+                for (int g = 0; g < TJ; g++) y[g] = sb.fragment(bs, wj, g, kk, lane);
+#pragma unroll
+                for (int f = 0; f < TI; f++) {
+                    const i32x4 x = sa.fragment(as, wi, f, kk, lane);
+#pragma unroll
+                    for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<E>(y[g], x, acc[f][g]);
+                }
+            }
+        }
+    };
+
+    if constexpr (kDirect) {
+        const int32_t tail = (p.inner % kStageK) * static_cast<int32_t>(sizeof(E));
+        sa.init(p.a, wave, lane);
+        sb.init(p.b, wave, lane);
+        const auto fetch = [&](char *as, char *bs, int32_t s) {
+            if (s >= s_last) return;
+            if (s + 1 == stages && tail) {
+                sa.cut(tail, wave, lane);
+                sb.cut(tail, wave, lane);
+            }
+            sa.fetch(p.a, i0, p.inner, s * kStageK, as, wave);
+            sb.fetch(p.b, j0, p.inner, s * kStageK, bs, wave);
+        };
+        fetch(a0, b0, s_first);
+        int32_t s = s_first;
+        for (; s + 2 <= s_last; s += 2) {
+            __syncthreads();   // this stage has landed, the other one is read
+            fetch(a1, b1, s + 1);
+            multiply(a0, b0);
+            __syncthreads();
+            fetch(a0, b0, s + 2);
+            multiply(a1, b1);
+        }
+        if (s < s_last) {
+            __syncthreads();
+            multiply(a0, b0);
+        }
+    } else {
+        i32x4 ra[SideA::kPerWave], rb[SideB::kPerWave];
+        const auto load = [&](int32_t s) {
+            if (s >= s_last) return;
+            sa.load(p.a, i0, p.inner, s * kStageK, ra, wave, lane);
+            sb.load(p.b, j0, p.inner, s * kStageK, rb, wave, lane);
+        };
+        const auto put = [&](char *as, char *bs) {
+            sa.put(ra, as, wave, lane);
+            sb.put(rb, bs, wave, lane);
+        };
+        if (s_first < s_last) {
+            load(s_first);
+            put(a0, b0);
+        }
+        int32_t s = s_first;
+        for (; s + 2 <= s_last; s += 2) {
+            __syncthreads();
+            load(s + 1);
+            multiply(a0, b0);
+            put(a1, b1);
+            __syncthreads();
+            load(s + 2);
+            multiply(a1, b1);
+            if (s + 2 < s_last) put(a0, b0);
+        }
+        if (s < s_last) {
+            __syncthreads();
+            multiply(a0, b0);
+        }
+    }
+
+    // a lane's runs of consecutive j: one of 4 * TJ, or TJ of 4
+    constexpr int kRun = 4 * kDeal, kRuns = TJ / kDeal;
+    #pragma unroll
+    for (int t = 0; t < kRuns; t++) {
+        const int64_t j = j0 + wj + (lane >> 4) * kRun + t * 16;
+        if (j >= p.b.extent) continue;
+        float b_scale[kRun], bias[kRun];
+        if (p.splits == 1) am_columns(p, j, b_scale, bias);
+        #pragma unroll
+        for (int f = 0; f < TI; f++) {
+            const int64_t i = i0 + wi + f * 16 + (lane & 15);
+            if (i >= p.a.extent) continue;
+            float v[kRun];
+            #pragma unroll
+            for (int d = 0; d < kDeal; d++)
+                #pragma unroll
+                for (int e = 0; e < 4; e++) v[d * 4 + e] = acc[f][t * kDeal + d][e];
+            if (p.splits == 1) {
+                am_finish(p, i, j, v, b_scale, bias);
+            } else {
+                float *o = p.partial + (static_cast<int64_t>(blockIdx.y) * p.a.extent + i) * p.b.extent + j;
+                #pragma unroll
+                for (int e = 0; e < kRun; e++)
+                    if (j + e < p.b.extent) o[e] = v[e];
+            }
+        }
+    }
+#endif
+}
+
+// --------------------------------------------------------------------------
+// host side
+// --------------------------------------------------------------------------
+
+// 16-byte fetches: rows aligned, ending on 16 bytes, offsets inside a tile in 31 bits
+inline bool am_direct(const AmOperand &o, bool major, int32_t inner, int el)
+{
+    const int64_t row = static_cast<int64_t>(major ? o.extent : inner) * el;
+    return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && row % 16 == 0 && o.ld < (int64_t{1} << 22);
+}
+
+// sums the parts of a split product and finishes them (am_linear.hip)
+void am_launch_join(const AmProduct &p, hipStream_t st);
+
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, int BM, int BN, int WM, int WN>
+void am_launch_tiles(const AmProduct &p, hipStream_t st)
+{
+    const int64_t tiles = ((static_cast<int64_t>(p.a.extent) + BM - 1) / BM) * ((static_cast<int64_t>(p.b.extent) + BN - 1) / BN);
+    am_tile_kernel<E, kMajorA, kMajorB, kDirect, BM, BN, WM, WN>
+        <<<dim3(static_cast<unsigned>(tiles), p.splits), WM * WN * 64, 0, st>>>(p);
+    if (p.splits > 1) am_launch_join(p, st);
+}
+
+constexpr int64_t kComputeUnits = 256;
+
+// Parts of k for a product without an epilogue: as many as fill the chip with
+// 64 x 64 tiles, of 4 stages at least.
+inline int32_t am_splits(int64_t rows, int64_t cols, int64_t inner)
+{
+    const int64_t tiles = ((rows + 63) / 64) * ((cols + 63) / 64), stages = (inner + 63) / 64;
+    int64_t s = 2 * kComputeUnits / tiles;
+    s = s < stages / 4 ? s : stages / 4;
+    return static_cast<int32_t>(s < 1 ? 1 : s > 64 ? 64 : s);
+}
+
+inline int64_t am_partial_bytes(int64_t rows, int64_t cols, int32_t splits)
+{
+    return splits > 1 ? (rows * cols * splits * 4 + 255) & ~int64_t{255} : 0;
+}
+
+template <typename E, bool kMajorA, bool kMajorB>
+void am_product(const AmProduct &p, hipStream_t st)
+{
+    const auto tiles = [&](int64_t t) { return ((p.a.extent + t - 1) / t) * ((p.b.extent + t - 1) / t); };
+    if (am_direct(p.a, kMajorA, p.inner, sizeof(E)) && am_direct(p.b, kMajorB, p.inner, sizeof(E))) {
+        if (p.splits == 1 && tiles(256) >= kComputeUnits / 2)
+            am_launch_tiles<E, kMajorA, kMajorB, true, 256, 256, 2, 4>(p, st);
+        else if (p.splits == 1 && tiles(128) >= kComputeUnits / 2)
+            am_launch_tiles<E, kMajorA, kMajorB, true, 128, 128, 2, 2>(p, st);
+        else
+            am_launch_tiles<E, kMajorA, kMajorB, true, 64, 64, 2, 2>(p, st);
+    } else if (p.splits == 1 && tiles(128) >= kComputeUnits / 2) {
+        am_launch_tiles<E, kMajorA, kMajorB, false, 128, 128, 2, 2>(p, st);
+    } else {
+        am_launch_tiles<E, kMajorA, kMajorB, false, 64, 64, 2, 2>(p, st);
+    }
+}
+
+}  // namespace wfd

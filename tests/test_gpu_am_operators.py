@@ -136,6 +136,24 @@ def test_linear_long_inner(am, dt):
     linear_case(am, 140, 8200, 150, dt, "none", F32, 2)
 
 
+# enough tiles for the larger tile sizes, with ragged edges and a last stage of k that is not full
+LARGE = [(1500, 200, 1400), (2900, 144, 3016), (2000, 1040, 2100), (1501, 203, 1403)]
+
+
+@pytest.mark.parametrize("dt", [BF16, F16, F8])
+@pytest.mark.parametrize("m,k,n", LARGE)
+def test_linear_large_tiles(am, m, k, n, dt):
+    linear_case(am, m, k, n, dt, "silu", BF16, 3, residual=True, pre=True)
+    linear_case(am, m, k, n, dt, "gelu", F32, 4, bias=False, out_pad=3)
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("m,k,n", [(1500, 1400, 200), (2904, 3016, 136), (136, 2904, 3016), (1501, 1403, 70)])
+def test_linear_backward_large_tiles(am, m, k, n, dt):
+    backward_case(am, m, k, n, dt, "relu", 3)
+    backward_case(am, m, k, n, dt, "none", 4, pad=8, weight_dtype=F32)
+
+
 @pytest.mark.parametrize("m", [4, 300])
 @pytest.mark.parametrize("dt", [BF16, F16, F8])
 def test_linear_infinity_and_nan_stay_in_their_rows(am, m, dt):
