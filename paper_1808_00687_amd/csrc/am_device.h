@@ -18,39 +18,104 @@ struct f8 {          // OCP e4m3
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(f16 x) { return static_cast<float>(x); }
 __device__ __forceinline__ float to_f32(bf16 x) { return static_cast<float>(x); }
-__device__ __forceinline__ float to_f32(f8 x) { return __builtin_amdgcn_cvt_f32_fp8(x.bits, 0); }
-
-// float32 to T, to nearest, ties to even
-template <typename T>
-__device__ __forceinline__ T from_f32(float x)
+// Reductions over a wave without LDS: lanes meet by quad and row permutations,
+// then rows of 16 and halves are swapped.  Every lane gets the result, always in
+// the same order.
+template <int kPattern>
+__device__ __forceinline__ int dpp(int v)
 {
-    return static_cast<T>(x);
+    return __builtin_amdgcn_update_dpp(v, v, kPattern, 0xF, 0xF, true);
 }
 
-// the conversion does not saturate: a finite value past the range would be NaN
-template <>
-__device__ __forceinline__ f8 from_f32<f8>(float x)
+template <typename Op>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t v, Op op)
 {
-    x = x > kE4m3Max ? kE4m3Max : x < -kE4m3Max ? -kE4m3Max : x;   // a NaN stays one
-    return f8{static_cast<uint8_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xFF)};
+    v = op(v, static_cast<uint32_t>(dpp<0xB1>(static_cast<int>(v))));    // lane ^ 1
+    v = op(v, static_cast<uint32_t>(dpp<0x4E>(static_cast<int>(v))));    // lane ^ 2
+    v = op(v, static_cast<uint32_t>(dpp<0x141>(static_cast<int>(v))));   // mirrored in 8
+    v = op(v, static_cast<uint32_t>(dpp<0x140>(static_cast<int>(v))));   // mirrored in 16
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = op(r[0], r[1]);
+    const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return op(h[0], h[1]);
 }
 
 __device__ __forceinline__ float wave_sum(float v)
 {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    return __uint_as_float(wave_reduce(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
 }
 
 __device__ __forceinline__ float wave_max(float v)
 {
-    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
+    return __uint_as_float(wave_reduce(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }));
 }
 
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
 {
-    for (int o = 32; o; o >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), o)));
-    return v;
+    return wave_reduce(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
+
+#define AM_LDS __attribute__((address_space(3)))
+#define AM_GLOBAL __attribute__((address_space(1)))
+
+// 8 consecutive elements of a row, at any address (16-byte accesses need no
+// alignment on this hardware); n of them exist, the others read as `fill`.
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int64_t n, float (&x)[8], float fill = 0.0f)
+{
+    using V = T __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    if (n >= 8) {
+        const V v = *(const AM_GLOBAL V *)p;
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = static_cast<float>(v[e]);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = e < n ? static_cast<float>(((const AM_GLOBAL T *)p)[e]) : fill;
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int64_t n, const float (&x)[8])
+{
+    using V = T __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    V v;
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = static_cast<T>(x[e]);
+    if (n >= 8) {
+        *(AM_GLOBAL V *)p = v;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        if (e < n) ((AM_GLOBAL T *)p)[e] = v[e];
+}
+
+// To e4m3, to nearest, ties to even.  The conversion does not saturate: the
+// values are at most 448 but for roundings (and 464 is the first that overflows).
+template <>
+__device__ __forceinline__ void store8<f8>(f8 *p, int64_t n, const float (&x)[8])
+{
+    using V = uint32_t __attribute__((ext_vector_type(2), aligned(1)));
+    V v;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        int t = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h], x[4 * h + 1], 0, false);
+        v[h] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h + 2], x[4 * h + 3], t, true));
+    }
+    if (n >= 8) {
+        *(AM_GLOBAL V *)p = v;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        if (e < n) ((AM_GLOBAL uint8_t *)p)[e] = static_cast<uint8_t>(v[e >> 2] >> (e & 3) * 8);
+}
+
+// exp for softmax and activations: good to about |x| 2^-24 relative
+__device__ __forceinline__ float am_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 }  // namespace wfd

@@ -23,19 +23,30 @@ inline bool am_rows_aligned(const wfst_matrix &m)
 // row stride of dz in the workspace: rows on 16 bytes
 constexpr int64_t am_dz_stride(int64_t n) { return (n + 7) & ~int64_t{7}; }
 
+// The workspace: dz (where the activation has a slope), then room that the
+// column sums and each product's parts use one after the other.
 struct BackwardPlan {
     int64_t dz_bytes, partial_bytes;
     int32_t dx_splits, dw_splits;
+    int32_t across;   // threads side by side in the pass over dy
+    int64_t strips;   // of rows, in that pass
 };
 
 inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a)
 {
     const int64_t M = a.dy.rows, N = a.dy.cols;
-    BackwardPlan p{0, 0, 1, 1};
+    BackwardPlan p{0, 0, 1, 1, 1, 1};
+    while (p.across < 64 && p.across * 8 < N) p.across *= 2;
+    // 4 rows a thread at least, about 1,024 workgroups at most
+    const int64_t wide = (N + p.across * 8 - 1) / (p.across * 8), tall = M * p.across / 1024, most = 1024 / wide;
+    p.strips = tall < most ? tall : most;
+    if (p.strips < 1) p.strips = 1;
+    if (a.dbias && p.strips > 1) p.partial_bytes = (p.strips * N * 4 + 255) & ~int64_t{255};
     if (a.activation != WFST_ACT_NONE && (a.dx.data || a.dw.data)) p.dz_bytes = (M * am_dz_stride(N) * 2 + 255) & ~int64_t{255};
     if (a.dx.data) {
         p.dx_splits = am_splits(M, a.dx.cols, N);
-        p.partial_bytes = am_partial_bytes(M, a.dx.cols, p.dx_splits);
+        const int64_t b = am_partial_bytes(M, a.dx.cols, p.dx_splits);
+        p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
     }
     if (a.dw.data) {
         p.dw_splits = am_splits(N, a.dw.cols, M);

@@ -1,5 +1,6 @@
 // The acoustic model's layers: wfst_am_linear and its gradients.
 #include "am_linear.h"
+#include "am_rows.h"
 
 namespace wfd {
 namespace {
@@ -28,25 +29,43 @@ __global__ __launch_bounds__(256) void join_kernel(AmProduct p)
     }
 }
 
-constexpr int kColumns = 256;
-
-// dz = dy * act'(pre) in the operands' type, and the column sums of the unrounded dz
+// dz = dy * act'(pre) in the operands' type, and sums of the unrounded dz over
+// a strip of rows.  8 columns a thread; `across` threads (a power of two) side
+// by side, 256 / across rows at a time.  sums: [strips][N].
 template <typename T>
-__global__ __launch_bounds__(kColumns) void slope_kernel(wfst_am_linear_backward_args a, T *dz)
+__global__ __launch_bounds__(256) void slope_kernel(wfst_am_linear_backward_args a, T *dz, float *sums, int across)
 {
+    __shared__ float part[256][9];
     const int64_t M = a.dy.rows, N = a.dy.cols, ld = am_dz_stride(N);
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * kColumns + threadIdx.x;
-    if (n >= N) return;
-    float sum = 0.0f;
-    for (int64_t m = 0; m < M; m++) {
-        float g = to_f32(static_cast<const T *>(a.dy.data)[m * a.dy.row_stride + n]);
-        if (a.activation != WFST_ACT_NONE) {
-            g *= slope(to_f32(static_cast<const T *>(a.pre.data)[m * a.pre.row_stride + n]), a.activation);
-            if (dz) dz[m * ld + n] = from_f32<T>(g);
+    const int down = 256 / across, x = threadIdx.x % across, y = threadIdx.x / across;
+    const int64_t n = (static_cast<int64_t>(blockIdx.x) * across + x) * 8;
+    const int64_t first = M * blockIdx.y / gridDim.y, last = M * (blockIdx.y + 1) / gridDim.y;
+    float sum[8] = {};
+    if (n < N)
+        for (int64_t m = first + y; m < last; m += down) {
+            float g[8];
+            load8(static_cast<const T *>(a.dy.data) + m * a.dy.row_stride + n, N - n, g);
+            if (a.activation != WFST_ACT_NONE) {
+                float z[8];
+                load8(static_cast<const T *>(a.pre.data) + m * a.pre.row_stride + n, N - n, z);
+#pragma unroll
+                for (int e = 0; e < 8; e++) g[e] *= slope(z[e], a.activation);
+                if (dz) store8(dz + m * ld + n, N - n, g);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e++) sum[e] += g[e];
         }
-        sum += g;
+    if (!sums) return;
+#pragma unroll
+    for (int e = 0; e < 8; e++) part[threadIdx.x][e] = sum[e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < across * 8; c += 256) {
+        const int64_t col = static_cast<int64_t>(blockIdx.x) * across * 8 + c;
+        if (col >= N) break;
+        float t = 0.0f;
+        for (int r = 0; r < down; r++) t += part[r * across + c / 8][c % 8];
+        sums[blockIdx.y * N + col] = t;
     }
-    if (a.dbias) a.dbias[n] = sum;
 }
 
 template <typename T>
@@ -56,11 +75,15 @@ void launch_backward(const wfst_am_linear_backward_args &a, hipStream_t st)
     const BackwardPlan plan = am_backward_plan(a);
     char *work = static_cast<char *>(a.workspace);
     T *dz = plan.dz_bytes ? reinterpret_cast<T *>(work) : nullptr;
-    if (a.dbias || dz)
-        slope_kernel<T><<<static_cast<unsigned>((N + kColumns - 1) / kColumns), kColumns, 0, st>>>(a, dz);
+    float *sums = a.dbias ? plan.strips > 1 ? reinterpret_cast<float *>(work + plan.dz_bytes) : a.dbias : nullptr;
+    if (a.dbias || dz) {
+        const dim3 grid(static_cast<unsigned>((N + plan.across * 8 - 1) / (plan.across * 8)), static_cast<unsigned>(plan.strips));
+        slope_kernel<T><<<grid, 256, 0, st>>>(a, dz, sums, plan.across);
+        if (sums && plan.strips > 1) am_launch_column_join(sums, plan.strips, N, a.dbias, st);
+    }
     const char *g = dz ? reinterpret_cast<const char *>(dz) : static_cast<const char *>(a.dy.data);
     const int64_t ld = (dz ? am_dz_stride(N) : a.dy.row_stride) * static_cast<int64_t>(sizeof(T));
-    float *partial = reinterpret_cast<float *>(work + plan.dz_bytes);
+    float *partial = reinterpret_cast<float *>(work + plan.dz_bytes);   // the column sums are joined by then
     if (a.dx.data && M > 0) {
         AmProduct p{};
         p.a = {g, ld, static_cast<int32_t>(M)};

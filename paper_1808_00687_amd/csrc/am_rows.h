@@ -1,0 +1,143 @@
+// Rows of the acoustic model's row operators: who reads which part, and the
+// reductions over a row.
+//
+// A row belongs to TPR threads (a wave, 256 or 1024), 8 consecutive columns at
+// a time: chunk c is thread c % TPR's.  With NV > 0 a thread holds its NV chunks
+// in registers, so a row is read once; with NV = 0 the row is too long for that
+// and every pass reads it again.
+#pragma once
+
+#include "am_device.h"
+
+namespace wfd {
+
+constexpr int64_t kRowHeld = 32768;   // longest row held in registers
+
+template <int TPR, int NV>
+struct RowShape {
+    static constexpr int kThreads = TPR < 256 ? 256 : TPR;
+    static constexpr int kRows = kThreads / TPR;           // rows a workgroup works on
+    static constexpr int kWaves = TPR / 64;                // waves a row
+    static constexpr int kTpr = TPR, kNv = NV;
+};
+
+// Calls go(shape) with the shape for rows of D columns.
+template <typename F>
+void am_row_shape(int64_t D, F go)
+{
+    if (D <= 512) go(RowShape<64, 1>{});
+    else if (D <= 1024) go(RowShape<64, 2>{});
+    else if (D <= 2048) go(RowShape<64, 4>{});
+    else if (D <= 4096) go(RowShape<256, 2>{});
+    else if (D <= 6144) go(RowShape<256, 3>{});
+    else if (D <= 8192) go(RowShape<256, 4>{});
+    else if (D <= 16384) go(RowShape<1024, 2>{});
+    else if (D <= kRowHeld) go(RowShape<1024, 4>{});
+    else go(RowShape<1024, 0>{});
+}
+
+// Workgroups for M rows: all of them up to `most`, which then take several.
+template <typename S>
+unsigned am_row_blocks(int64_t M, int64_t most)
+{
+    const int64_t n = (M + S::kRows - 1) / S::kRows;
+    return static_cast<unsigned>(n < most ? n : most);
+}
+
+template <typename S>
+struct RowPart {
+    static constexpr int kHeld = S::kNv > 0 ? S::kNv : 1;
+    int64_t cols;
+    int t;
+    float x[kHeld][8];
+
+    // fetch(column, left, x): 8 values from a column on, `left` of which exist (may be negative)
+    template <typename L>
+    __device__ __forceinline__ void hold(int64_t cols_, int t_, L fetch)
+    {
+        cols = cols_, t = t_;
+        if constexpr (S::kNv > 0)
+#pragma unroll
+            for (int v = 0; v < S::kNv; v++) {
+                const int64_t c = (static_cast<int64_t>(v) * S::kTpr + t) * 8;
+                fetch(c, cols - c, x[v]);
+            }
+    }
+    // use(column, left, x) for each chunk that holds a column of the row
+    template <typename L, typename F>
+    __device__ __forceinline__ void each(L fetch, F use)
+    {
+        if constexpr (S::kNv > 0) {
+#pragma unroll
+            for (int v = 0; v < S::kNv; v++) {
+                const int64_t c = (static_cast<int64_t>(v) * S::kTpr + t) * 8;
+                if (c < cols) use(c, cols - c, x[v]);
+            }
+        } else {
+            for (int64_t c = static_cast<int64_t>(t) * 8; c < cols; c += S::kTpr * 8) {
+                fetch(c, cols - c, x[0]);
+                use(c, cols - c, x[0]);
+            }
+        }
+    }
+};
+
+// LDS of the reductions.  Two sets, used in turn, so that one barrier a
+// reduction is enough: a set is written again only after the other one's barrier.
+struct RowScratch {
+    float a[2][16], b[2][16];
+};
+
+template <typename S>
+__device__ __forceinline__ float row_sum(float v, RowScratch &r, int &turn)
+{
+    v = wave_sum(v);
+    if constexpr (S::kWaves == 1) return v;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) r.a[turn][wave] = v;
+    __syncthreads();
+    float s = r.a[turn][0];
+#pragma unroll
+    for (int i = 1; i < S::kWaves; i++) s += r.a[turn][i];
+    turn ^= 1;
+    return s;
+}
+
+// two sums at once
+template <typename S>
+__device__ __forceinline__ void row_sums(float &u, float &v, RowScratch &r, int &turn)
+{
+    u = wave_sum(u), v = wave_sum(v);
+    if constexpr (S::kWaves == 1) return;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) r.a[turn][wave] = u, r.b[turn][wave] = v;
+    __syncthreads();
+    u = r.a[turn][0], v = r.b[turn][0];
+#pragma unroll
+    for (int i = 1; i < S::kWaves; i++) u += r.a[turn][i], v += r.b[turn][i];
+    turn ^= 1;
+}
+
+// largest magnitude by its bits: a NaN counts as larger than an infinity
+template <typename S>
+__device__ __forceinline__ uint32_t row_max_u32(uint32_t v, RowScratch &r, int &turn)
+{
+    v = wave_max_u32(v);
+    if constexpr (S::kWaves == 1) return v;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) r.a[turn][wave] = __uint_as_float(v);
+    __syncthreads();
+    uint32_t m = __float_as_uint(r.a[turn][0]);
+#pragma unroll
+    for (int i = 1; i < S::kWaves; i++) {
+        const uint32_t o = __float_as_uint(r.a[turn][i]);
+        m = m > o ? m : o;
+    }
+    turn ^= 1;
+    return m;
+}
+
+// Column sums over strips of rows: partial[strips][n] -> out[n], in order of the strips (am_norm.hip)
+void am_launch_column_join(const float *partial, int64_t strips, int64_t n, float *out, hipStream_t st);
+
+}  // namespace wfd

@@ -36,9 +36,6 @@ using f32x4 = float __attribute__((ext_vector_type(4)));
 using f16x8 = f16 __attribute__((ext_vector_type(8)));
 using bf16x8 = bf16 __attribute__((ext_vector_type(8)));
 
-#define AM_LDS __attribute__((address_space(3)))
-#define AM_GLOBAL __attribute__((address_space(1)))
-
 constexpr int kStageBytes = 128;   // of k, a row
 
 struct AmOperand {
@@ -57,8 +54,6 @@ struct AmProduct {
     int32_t activation;
     int32_t vec;               // out, residual and pre have 16-byte aligned rows
 };
-
-__device__ __forceinline__ float am_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 __device__ __forceinline__ float am_silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + am_exp(-z)); }
 
