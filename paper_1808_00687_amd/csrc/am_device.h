@@ -62,56 +62,62 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
 #define AM_LDS __attribute__((address_space(3)))
 #define AM_GLOBAL __attribute__((address_space(1)))
 
-// 8 consecutive elements of a row, at any address (16-byte accesses need no
+// C consecutive elements of a row, at any address (wide accesses need no
 // alignment on this hardware); n of them exist, the others read as `fill`.
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, int64_t n, float (&x)[8], float fill = 0.0f)
+template <typename T, int C>
+using Chunk = T __attribute__((ext_vector_type(C), aligned(sizeof(T))));
+
+template <typename T, int C>
+__device__ __forceinline__ Chunk<T, C> load_chunk(const T *p, int64_t n, T fill)
 {
-    using V = T __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-    if (n >= 8) {
-        const V v = *(const AM_GLOBAL V *)p;
+    if (n >= C) return *(const AM_GLOBAL Chunk<T, C> *)p;
+    Chunk<T, C> v;
 #pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = static_cast<float>(v[e]);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; e++) x[e] = e < n ? static_cast<float>(((const AM_GLOBAL T *)p)[e]) : fill;
+    for (int e = 0; e < C; e++) v[e] = e < n ? ((const AM_GLOBAL T *)p)[e] : fill;
+    return v;
 }
 
-template <typename T>
-__device__ __forceinline__ void store8(T *p, int64_t n, const float (&x)[8])
+template <typename T, int C>
+__device__ __forceinline__ void load_floats(const T *p, int64_t n, float (&x)[C], float fill = 0.0f)
 {
-    using V = T __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-    V v;
+    const Chunk<T, C> v = load_chunk<T, C>(p, n, static_cast<T>(fill));
 #pragma unroll
-    for (int e = 0; e < 8; e++) v[e] = static_cast<T>(x[e]);
-    if (n >= 8) {
-        *(AM_GLOBAL V *)p = v;
+    for (int e = 0; e < C; e++) x[e] = static_cast<float>(v[e]);
+}
+
+template <typename T, int C>
+__device__ __forceinline__ void store_floats(T *p, int64_t n, const float (&x)[C])
+{
+    Chunk<T, C> v;
+#pragma unroll
+    for (int e = 0; e < C; e++) v[e] = static_cast<T>(x[e]);
+    if (n >= C) {
+        *(AM_GLOBAL Chunk<T, C> *)p = v;
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 8; e++)
+    for (int e = 0; e < C; e++)
         if (e < n) ((AM_GLOBAL T *)p)[e] = v[e];
 }
 
 // To e4m3, to nearest, ties to even.  The conversion does not saturate: the
 // values are at most 448 but for roundings (and 464 is the first that overflows).
-template <>
-__device__ __forceinline__ void store8<f8>(f8 *p, int64_t n, const float (&x)[8])
+template <int C>
+__device__ __forceinline__ void store_floats(f8 *p, int64_t n, const float (&x)[C])
 {
-    using V = uint32_t __attribute__((ext_vector_type(2), aligned(1)));
+    using V = uint32_t __attribute__((ext_vector_type(C / 4), aligned(1)));
     V v;
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
-        int t = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h], x[4 * h + 1], 0, false);
+    for (int h = 0; h < C / 4; h++) {
+        const int t = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h], x[4 * h + 1], 0, false);
         v[h] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h + 2], x[4 * h + 3], t, true));
     }
-    if (n >= 8) {
+    if (n >= C) {
         *(AM_GLOBAL V *)p = v;
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 8; e++)
+    for (int e = 0; e < C; e++)
         if (e < n) ((AM_GLOBAL uint8_t *)p)[e] = static_cast<uint8_t>(v[e >> 2] >> (e & 3) * 8);
 }
 

@@ -44,13 +44,13 @@ __global__ __launch_bounds__(256) void slope_kernel(wfst_am_linear_backward_args
     if (n < N)
         for (int64_t m = first + y; m < last; m += down) {
             float g[8];
-            load8(static_cast<const T *>(a.dy.data) + m * a.dy.row_stride + n, N - n, g);
+            load_floats(static_cast<const T *>(a.dy.data) + m * a.dy.row_stride + n, N - n, g);
             if (a.activation != WFST_ACT_NONE) {
                 float z[8];
-                load8(static_cast<const T *>(a.pre.data) + m * a.pre.row_stride + n, N - n, z);
+                load_floats(static_cast<const T *>(a.pre.data) + m * a.pre.row_stride + n, N - n, z);
 #pragma unroll
                 for (int e = 0; e < 8; e++) g[e] *= slope(z[e], a.activation);
-                if (dz) store8(dz + m * ld + n, N - n, g);
+                if (dz) store_floats(dz + m * ld + n, N - n, g);
             }
 #pragma unroll
             for (int e = 0; e < 8; e++) sum[e] += g[e];

@@ -23,66 +23,66 @@ __device__ __forceinline__ T *row_out(const wfst_matrix &m, int64_t r)
     return static_cast<T *>(m.data) + r * m.row_stride;
 }
 
-__device__ __forceinline__ void load_gain(const float *gain, int64_t c, int64_t left, float (&g)[8])
-{
-    if (gain) {
-        load8(gain + c, left, g);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; e++) g[e] = 1.0f;
-}
+// chunks where a matrix has 32-bit elements are half as long
+template <typename T>
+constexpr int kChunk = sizeof(T) == 4 ? 4 : 8;
 
 template <typename T, typename S, bool k8Bits>
 __global__ __launch_bounds__(S::kThreads) void norm_kernel(wfst_am_norm_args a)
 {
     __shared__ RowScratch scratch;
     int turn = 0;
-    const int64_t M = a.x.rows, D = a.x.cols;
+    const int64_t M = a.x.rows, D = a.x.cols, step = static_cast<int64_t>(gridDim.x) * S::kRows;
     const int t = threadIdx.x % S::kTpr;
-    RowPart<S> gain;
-    const auto load_g = [&](int64_t c, int64_t left, float (&g)[8]) { load_gain(a.gain, c, left, g); };
-    gain.hold(D, t, load_g);
-    for (int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kTpr; m < M;
-         m += static_cast<int64_t>(gridDim.x) * S::kRows) {
-        const T *x = row<T>(a.x, m), *r = a.residual.data ? row<T>(a.residual, m) : nullptr;
-        const auto load_s = [&](int64_t c, int64_t left, float (&v)[8]) {
-            load8(x + c, left, v);
-            if (!r) return;
-            float w[8];
-            load8(r + c, left, w);
+    RowPart<S, float> gain;
+    if (a.gain) gain.hold(a.gain, D, t);
+    RowPart<S, T> x, r, x_next, r_next;
+    const auto hold = [&](int64_t m) {
+        if (m >= M) return;
+        x_next.hold(row<T>(a.x, m), D, t);
+        if (a.residual.data) r_next.hold(row<T>(a.residual, m), D, t);
+    };
+    int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kTpr;
+    hold(m);
+    for (; m < M; m += step) {
+        x = x_next, r = r_next;
+        hold(m + step);   // the next row is on its way while this one is worked on
+        const auto sum_of = [&](int v, int64_t c, int64_t left, float (&s)[S::kC]) {
+            x.get(v, c, left, s);
+            if (!a.residual.data) return;
+            float w[S::kC];
+            r.get(v, c, left, w);
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[e] += w[e];
+            for (int e = 0; e < S::kC; e++) s[e] += w[e];
         };
-        RowPart<S> s;
-        s.hold(D, t, load_s);
-        float ss = 0.0f;
-        s.each(load_s, [&](int64_t, int64_t, float (&v)[8]) {
+        const auto times_gain = [&](int v, int64_t c, int64_t left, float (&s)[S::kC]) {
+            if (!a.gain) return;
+            float g[S::kC];
+            gain.get(v, c, left, g);
 #pragma unroll
-            for (int e = 0; e < 8; e++) ss = fmaf(v[e], v[e], ss);
+            for (int e = 0; e < S::kC; e++) s[e] *= g[e];
+        };
+        float ss = 0.0f;
+        S::each(D, t, [&](int v, int64_t c, int64_t left) {
+            float s[S::kC];
+            sum_of(v, c, left, s);
+#pragma unroll
+            for (int e = 0; e < S::kC; e++) ss = fmaf(s[e], s[e], ss);
         });
         const float rho = 1.0f / sqrtf(row_sum<S>(ss, scratch, turn) / static_cast<float>(D) + a.eps);
-        int v_at = 0;   // the chunk's place among the held ones
-        const auto gain_of = [&](int64_t c, int64_t left, float (&g)[8]) {
-            if constexpr (S::kNv > 0) {
-#pragma unroll
-                for (int e = 0; e < 8; e++) g[e] = gain.x[v_at][e];
-                v_at++;
-            } else {
-                load_gain(a.gain, c, left, g);
-            }
-        };
         float inv = 1.0f;
         if constexpr (k8Bits) {
             uint32_t top = 0;
-            v_at = 0;
-            s.each(load_s, [&](int64_t c, int64_t left, float (&v)[8]) {
-                float g[8];
-                gain_of(c, left, g);
+            S::each(D, t, [&](int v, int64_t c, int64_t left) {
+                float s[S::kC];
+                sum_of(v, c, left, s);
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const uint32_t b = e < left ? __float_as_uint(v[e] * rho * g[e]) & 0x7FFFFFFFu : 0;
-                    top = top > b ? top : b;
+                for (int e = 0; e < S::kC; e++) s[e] *= rho;
+                times_gain(v, c, left, s);
+#pragma unroll
+                for (int e = 0; e < S::kC; e++) {
+                    const uint32_t b = __float_as_uint(s[e]) & 0x7FFFFFFFu;
+                    top = e < left && b > top ? b : top;
                 }
             });
             float scale = __uint_as_float(row_max_u32<S>(top, scratch, turn)) / kE4m3Max;
@@ -90,19 +90,24 @@ __global__ __launch_bounds__(S::kThreads) void norm_kernel(wfst_am_norm_args a)
             inv = 1.0f / scale;
             if (t == 0) a.y_scale[m] = scale;
         }
-        T *sum = a.sum.data ? row_out<T>(a.sum, m) : nullptr;
-        v_at = 0;
-        s.each(load_s, [&](int64_t c, int64_t left, float (&v)[8]) {
-            float g[8];
-            gain_of(c, left, g);
-            if (sum) store8(sum + c, left, v);
-            float y[8];
+        S::each(D, t, [&](int v, int64_t c, int64_t left) {
+            float s[S::kC];
+            sum_of(v, c, left, s);
+            if (a.sum.data) store_floats(row_out<T>(a.sum, m) + c, left, s);
 #pragma unroll
-            for (int e = 0; e < 8; e++) y[e] = v[e] * rho * g[e] * inv;
-            if constexpr (k8Bits) store8(row_out<f8>(a.y, m) + c, left, y);
-            else if (a.y.type == WFST_BF16) store8(row_out<bf16>(a.y, m) + c, left, y);
-            else if (a.y.type == WFST_F16) store8(row_out<f16>(a.y, m) + c, left, y);
-            else store8(row_out<float>(a.y, m) + c, left, y);
+            for (int e = 0; e < S::kC; e++) s[e] *= rho;
+            times_gain(v, c, left, s);
+            if constexpr (k8Bits) {
+#pragma unroll
+                for (int e = 0; e < S::kC; e++) s[e] *= inv;
+                store_floats(row_out<f8>(a.y, m) + c, left, s);
+            } else if (a.y.type == WFST_BF16) {
+                store_floats(row_out<bf16>(a.y, m) + c, left, s);
+            } else if (a.y.type == WFST_F16) {
+                store_floats(row_out<f16>(a.y, m) + c, left, s);
+            } else {
+                store_floats(row_out<float>(a.y, m) + c, left, s);
+            }
         });
     }
 }
@@ -114,63 +119,89 @@ __global__ __launch_bounds__(S::kThreads) void norm_backward_kernel(wfst_am_norm
 {
     __shared__ RowScratch scratch;
     int turn = 0;
-    const int64_t M = a.s.rows, D = a.s.cols;
+    const int64_t M = a.s.rows, D = a.s.cols, step = static_cast<int64_t>(gridDim.x) * S::kRows;
     const int t = threadIdx.x % S::kTpr;
-    constexpr int kHeld = RowPart<S>::kHeld;
-    float dg[kHeld][8] = {};
-    for (int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kTpr; m < M;
-         m += static_cast<int64_t>(gridDim.x) * S::kRows) {
-        const T *s_row = row<T>(a.s, m), *dy_row = row<T>(a.dy, m);
-        const T *ds_row = a.dsum.data ? row<T>(a.dsum, m) : nullptr;
-        T *dx = a.dx.data ? row_out<T>(a.dx, m) : nullptr;
-        const auto load_s = [&](int64_t c, int64_t left, float (&v)[8]) { load8(s_row + c, left, v); };
-        const auto load_dy = [&](int64_t c, int64_t left, float (&v)[8]) { load8(dy_row + c, left, v); };
-        RowPart<S> s, dy;
-        s.hold(D, t, load_s);
-        dy.hold(D, t, load_dy);
-        float ss = 0.0f, us = 0.0f;
-        int v_at = 0;
-        s.each(load_s, [&](int64_t c, int64_t left, float (&v)[8]) {
-            float g[8];
-            load_gain(a.gain, c, left, g);
-            if constexpr (S::kNv == 0) load_dy(c, left, dy.x[0]);
-            const float(&w)[8] = dy.x[S::kNv > 0 ? v_at : 0];
+    RowPart<S, float> gain;
+    if (a.gain) gain.hold(a.gain, D, t);
+    float dg[S::kHeld][S::kC] = {};
+    RowPart<S, T> s, dy, ds, s_next, dy_next;
+    const auto hold = [&](int64_t m) {
+        if (m >= M) return;
+        s_next.hold(row<T>(a.s, m), D, t);
+        dy_next.hold(row<T>(a.dy, m), D, t);
+    };
+    int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kTpr;
+    hold(m);
+    for (; m < M; m += step) {
+        s = s_next, dy = dy_next;
+        if (a.dsum.data) ds.hold(row<T>(a.dsum, m), D, t);
+        hold(m + step);
+        const auto u_of = [&](int v, int64_t c, int64_t left, const float (&w)[S::kC], float (&u)[S::kC]) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                ss = fmaf(v[e], v[e], ss);
-                us = fmaf(w[e] * g[e], v[e], us);
+            for (int e = 0; e < S::kC; e++) u[e] = w[e];
+            if (!a.gain) return;
+            float g[S::kC];
+            gain.get(v, c, left, g);
+#pragma unroll
+            for (int e = 0; e < S::kC; e++) u[e] *= g[e];
+        };
+        float ss = 0.0f, us = 0.0f;
+        S::each(D, t, [&](int v, int64_t c, int64_t left) {
+            float x[S::kC], w[S::kC], u[S::kC];
+            s.get(v, c, left, x);
+            dy.get(v, c, left, w);
+            u_of(v, c, left, w, u);
+#pragma unroll
+            for (int e = 0; e < S::kC; e++) {
+                ss = fmaf(x[e], x[e], ss);
+                us = fmaf(u[e], x[e], us);
             }
-            v_at++;
         });
         row_sums<S>(ss, us, scratch, turn);
         const float rho = 1.0f / sqrtf(ss / static_cast<float>(D) + a.eps);
         const float c0 = rho * rho * (us / static_cast<float>(D));
         if (S::kNv == 0 && rhos && t == 0) rhos[m] = rho;
-        if (S::kNv == 0 && !dx) continue;
-        v_at = 0;
-        s.each(load_s, [&](int64_t c, int64_t left, float (&v)[8]) {
-            if constexpr (S::kNv == 0) load_dy(c, left, dy.x[0]);
-            const float(&w)[8] = dy.x[S::kNv > 0 ? v_at : 0];
+        if (S::kNv == 0 && !a.dx.data) continue;
+        S::each(D, t, [&](int v, int64_t c, int64_t left) {
+            float x[S::kC], w[S::kC], u[S::kC];
+            s.get(v, c, left, x);
+            dy.get(v, c, left, w);
+            u_of(v, c, left, w, u);
             if constexpr (S::kNv > 0)
 #pragma unroll
-                for (int e = 0; e < 8; e++) dg[v_at][e] = fmaf(w[e] * rho, v[e], dg[v_at][e]);
-            v_at++;
-            if (!dx) return;
-            float g[8], d[8] = {};
-            load_gain(a.gain, c, left, g);
-            if (ds_row) load8(ds_row + c, left, d);
+                for (int e = 0; e < S::kC; e++) dg[v][e] = fmaf(w[e] * rho, x[e], dg[v][e]);
+            if (!a.dx.data) return;
+            float d[S::kC];
 #pragma unroll
-            for (int e = 0; e < 8; e++) d[e] += rho * (w[e] * g[e] - v[e] * c0);
-            store8(dx + c, left, d);
+            for (int e = 0; e < S::kC; e++) d[e] = rho * (u[e] - x[e] * c0);
+            if (a.dsum.data) {
+                ds.get(v, c, left, u);
+#pragma unroll
+                for (int e = 0; e < S::kC; e++) d[e] += u[e];
+            }
+            store_floats(row_out<T>(a.dx, m) + c, left, d);
         });
     }
     if (S::kNv == 0 || !partial) return;
-    // the rows' sums of a workgroup side by side in `partial`
-    float *o = partial + (static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kTpr) * D;
+    if constexpr (S::kRows == 1) {
+        S::each(D, t, [&](int v, int64_t c, int64_t left) { store_floats(partial + blockIdx.x * D + c, left, dg[v]); });
+    } else {
+        // the workgroup's rows' sums, one after the other
+        __shared__ float total[S::kHeld * S::kTpr * S::kC];
+        for (int w = 0; w < S::kRows; w++) {
+            __syncthreads();
+            if (static_cast<int>(threadIdx.x) / S::kTpr != w) continue;
 #pragma unroll
-    for (int v = 0; v < kHeld; v++) {
-        const int64_t c = (static_cast<int64_t>(v) * S::kTpr + t) * 8;
-        if (c < D) store8(o + c, D - c, dg[v]);
+            for (int v = 0; v < S::kHeld; v++)
+#pragma unroll
+                for (int e = 0; e < S::kC; e++) {
+                    float &o = total[(v * S::kC + e) * S::kTpr + t];
+                    o = w ? o + dg[v][e] : dg[v][e];
+                    dg[v][e] = o;
+                }
+        }
+        if (threadIdx.x / S::kTpr == S::kRows - 1)
+            S::each(D, t, [&](int v, int64_t c, int64_t left) { store_floats(partial + blockIdx.x * D + c, left, dg[v]); });
     }
 }
 
@@ -203,15 +234,15 @@ __global__ __launch_bounds__(256) void column_join_kernel(const float *partial, 
 }
 
 constexpr int64_t kForwardBlocks = 256 * 16;
-constexpr int64_t kBackwardBlocks = 256 * 2;
+constexpr int64_t kBackwardBlocks = 256 * 4;
 
 // strips of rows whose sums of the gain's gradient are joined
 int64_t dgain_strips(int64_t M, int64_t D)
 {
     int64_t n = 0;
-    am_row_shape(D, [&](auto shape) {
+    am_row_shape<8>(D, [&](auto shape) {   // the same for shorter chunks
         using S = decltype(shape);
-        n = S::kNv > 0 ? static_cast<int64_t>(am_row_blocks<S>(M, kBackwardBlocks)) * S::kRows : 0;
+        n = S::kNv > 0 ? static_cast<int64_t>(am_row_blocks<S>(M, kBackwardBlocks)) : 0;
     });
     return n;
 }
@@ -219,7 +250,7 @@ int64_t dgain_strips(int64_t M, int64_t D)
 template <typename T>
 void launch_norm(const wfst_am_norm_args &a, hipStream_t st)
 {
-    am_row_shape(a.x.cols, [&](auto shape) {
+    am_row_shape<kChunk<T>>(a.x.cols, [&](auto shape) {
         using S = decltype(shape);
         const unsigned g = am_row_blocks<S>(a.x.rows, kForwardBlocks);
         if (a.y.type == WFST_F8E4M3) norm_kernel<T, S, true><<<g, S::kThreads, 0, st>>>(a);
@@ -232,12 +263,12 @@ void launch_norm_backward(const wfst_am_norm_backward_args &a, hipStream_t st)
 {
     const int64_t M = a.s.rows, D = a.s.cols;
     float *work = static_cast<float *>(a.workspace);
-    am_row_shape(D, [&](auto shape) {
+    am_row_shape<kChunk<T>>(D, [&](auto shape) {
         using S = decltype(shape);
         const unsigned g = M ? am_row_blocks<S>(M, kBackwardBlocks) : 0;
         if constexpr (S::kNv > 0) {
             if (M) norm_backward_kernel<T, S><<<g, S::kThreads, 0, st>>>(a, a.dgain ? work : nullptr, nullptr);
-            if (a.dgain) am_launch_column_join(work, static_cast<int64_t>(g) * S::kRows, D, a.dgain, st);
+            if (a.dgain) am_launch_column_join(work, g, D, a.dgain, st);
         } else {
             // the gain's gradient before dx may overwrite dy
             wfst_am_norm_backward_args b = a;

@@ -1,10 +1,12 @@
 // Rows of the acoustic model's row operators: who reads which part, and the
 // reductions over a row.
 //
-// A row belongs to TPR threads (a wave, 256 or 1024), 8 consecutive columns at
-// a time: chunk c is thread c % TPR's.  With NV > 0 a thread holds its NV chunks
-// in registers, so a row is read once; with NV = 0 the row is too long for that
-// and every pass reads it again.
+// A row belongs to TPR threads (a wave, 256 or 1024), C consecutive columns at
+// a time: chunk c is thread c % TPR's.  C is 8 where every matrix has 16-bit
+// elements and 4 where one has 32-bit ones, so that no access is wider than 16
+// bytes and neighbouring lanes' accesses touch.  With NV > 0 a thread holds its
+// NV chunks in registers, as they are in memory, so a row is read once; with
+// NV = 0 the row is too long for that and every pass reads it again.
 #pragma once
 
 #include "am_device.h"
@@ -13,27 +15,44 @@ namespace wfd {
 
 constexpr int64_t kRowHeld = 32768;   // longest row held in registers
 
-template <int TPR, int NV>
+template <int TPR, int NV, int C>
 struct RowShape {
     static constexpr int kThreads = TPR < 256 ? 256 : TPR;
     static constexpr int kRows = kThreads / TPR;           // rows a workgroup works on
     static constexpr int kWaves = TPR / 64;                // waves a row
-    static constexpr int kTpr = TPR, kNv = NV;
+    static constexpr int kTpr = TPR, kNv = NV, kC = C;
+    static constexpr int kHeld = NV > 0 ? NV : 1;
+
+    // use(v, column, left) for each of thread t's chunks with a column below cols: `left` columns are left there
+    template <typename F>
+    __device__ __forceinline__ static void each(int64_t cols, int t, F use)
+    {
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int v = 0; v < NV; v++) {
+                const int64_t c = (static_cast<int64_t>(v) * TPR + t) * C;
+                if (c < cols) use(v, c, cols - c);
+            }
+        } else {
+            for (int64_t c = static_cast<int64_t>(t) * C; c < cols; c += TPR * C) use(0, c, cols - c);
+        }
+    }
 };
 
 // Calls go(shape) with the shape for rows of D columns.
-template <typename F>
+template <int C, typename F>
 void am_row_shape(int64_t D, F go)
 {
-    if (D <= 512) go(RowShape<64, 1>{});
-    else if (D <= 1024) go(RowShape<64, 2>{});
-    else if (D <= 2048) go(RowShape<64, 4>{});
-    else if (D <= 4096) go(RowShape<256, 2>{});
-    else if (D <= 6144) go(RowShape<256, 3>{});
-    else if (D <= 8192) go(RowShape<256, 4>{});
-    else if (D <= 16384) go(RowShape<1024, 2>{});
-    else if (D <= kRowHeld) go(RowShape<1024, 4>{});
-    else go(RowShape<1024, 0>{});
+    constexpr int k = 8 / C;
+    if (D <= 512) go(RowShape<64, 1 * k, C>{});
+    else if (D <= 1024) go(RowShape<64, 2 * k, C>{});
+    else if (D <= 2048) go(RowShape<64, 4 * k, C>{});
+    else if (D <= 4096) go(RowShape<256, 2 * k, C>{});
+    else if (D <= 6144) go(RowShape<256, 3 * k, C>{});
+    else if (D <= 8192) go(RowShape<256, 4 * k, C>{});
+    else if (D <= 16384) go(RowShape<1024, 2 * k, C>{});
+    else if (D <= kRowHeld) go(RowShape<1024, 4 * k, C>{});
+    else go(RowShape<1024, 0, C>{});
 }
 
 // Workgroups for M rows: all of them up to `most`, which then take several.
@@ -44,40 +63,29 @@ unsigned am_row_blocks(int64_t M, int64_t most)
     return static_cast<unsigned>(n < most ? n : most);
 }
 
-template <typename S>
+// A thread's chunks of one row, held or read when asked for.
+template <typename S, typename T>
 struct RowPart {
-    static constexpr int kHeld = S::kNv > 0 ? S::kNv : 1;
-    int64_t cols;
-    int t;
-    float x[kHeld][8];
+    const T *p;
+    Chunk<T, S::kC> held[S::kHeld];
 
-    // fetch(column, left, x): 8 values from a column on, `left` of which exist (may be negative)
-    template <typename L>
-    __device__ __forceinline__ void hold(int64_t cols_, int t_, L fetch)
+    __device__ __forceinline__ void hold(const T *row, int64_t cols, int t, T fill = static_cast<T>(0.0f))
     {
-        cols = cols_, t = t_;
+        p = row;
         if constexpr (S::kNv > 0)
 #pragma unroll
             for (int v = 0; v < S::kNv; v++) {
-                const int64_t c = (static_cast<int64_t>(v) * S::kTpr + t) * 8;
-                fetch(c, cols - c, x[v]);
+                const int64_t c = (static_cast<int64_t>(v) * S::kTpr + t) * S::kC;
+                held[v] = load_chunk<T, S::kC>(row + c, cols - c, fill);
             }
     }
-    // use(column, left, x) for each chunk that holds a column of the row
-    template <typename L, typename F>
-    __device__ __forceinline__ void each(L fetch, F use)
+    __device__ __forceinline__ void get(int v, int64_t c, int64_t left, float (&x)[S::kC], float fill = 0.0f) const
     {
         if constexpr (S::kNv > 0) {
 #pragma unroll
-            for (int v = 0; v < S::kNv; v++) {
-                const int64_t c = (static_cast<int64_t>(v) * S::kTpr + t) * 8;
-                if (c < cols) use(c, cols - c, x[v]);
-            }
+            for (int e = 0; e < S::kC; e++) x[e] = static_cast<float>(held[v][e]);
         } else {
-            for (int64_t c = static_cast<int64_t>(t) * 8; c < cols; c += S::kTpr * 8) {
-                fetch(c, cols - c, x[0]);
-                use(c, cols - c, x[0]);
-            }
+            load_floats<T, S::kC>(p + c, left, x, fill);
         }
     }
 };

@@ -17,22 +17,26 @@ __device__ __forceinline__ const T *row(const wfst_matrix &m, int64_t r)
     return static_cast<const T *>(m.data) + r * m.row_stride;
 }
 
-// log sum exp over the row of each thread's part; fetch gives x already divided
-// by the temperature, -inf beyond the row.  -inf for a row of -inf.
-template <typename S, typename L>
-__device__ __forceinline__ float row_lse(RowPart<S> &x, L fetch, RowScratch &r, int &turn)
+// log sum exp over a row; get(v, c, left, x) gives a chunk, already divided by
+// the temperature, -inf beyond the row.  -inf for a row of -inf.
+template <typename S, typename G>
+__device__ __forceinline__ float row_lse(int64_t cols, int t, G get, RowScratch &r, int &turn)
 {
     float top = -INFINITY;
-    x.each(fetch, [&](int64_t, int64_t, float (&v)[8]) {
+    S::each(cols, t, [&](int v, int64_t c, int64_t left) {
+        float x[S::kC];
+        get(v, c, left, x);
 #pragma unroll
-        for (int e = 0; e < 8; e++) top = fmaxf(top, v[e]);
+        for (int e = 0; e < S::kC; e++) top = fmaxf(top, x[e]);
     });
     top = wave_max(top);
     float shift = top == -INFINITY ? 0.0f : top;
     float s = 0.0f;
-    x.each(fetch, [&](int64_t, int64_t, float (&v)[8]) {
+    S::each(cols, t, [&](int v, int64_t c, int64_t left) {
+        float x[S::kC];
+        get(v, c, left, x);
 #pragma unroll
-        for (int e = 0; e < 8; e++) s += am_exp(v[e] - shift);
+        for (int e = 0; e < S::kC; e++) s += am_exp(x[e] - shift);
     });
     s = wave_sum(s);
     if constexpr (S::kWaves > 1) {
@@ -56,36 +60,29 @@ __global__ __launch_bounds__(S::kThreads) void loglikes_kernel(wfst_am_loglikes_
 {
     __shared__ RowScratch scratch;
     int turn = 0;
-    const int64_t M = a.logits.rows, L = a.logits.cols;
+    const int64_t M = a.logits.rows, L = a.logits.cols, step = static_cast<int64_t>(gridDim.x) * S::kRows;
     const int t = threadIdx.x % S::kTpr;
-    RowPart<S> prior;
-    const auto load_p = [&](int64_t c, int64_t left, float (&p)[8]) {
-        if (a.log_prior) {
-            load8(a.log_prior + c, left, p);
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; e++) p[e] = 0.0f;
-    };
-    prior.hold(L, t, load_p);
-    for (int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kTpr; m < M;
-         m += static_cast<int64_t>(gridDim.x) * S::kRows) {
-        const T *x_row = row<T>(a.logits, m);
+    RowPart<S, float> prior;
+    if (a.log_prior) prior.hold(a.log_prior, L, t);
+    RowPart<S, T> x, next;
+    const T low = static_cast<T>(-INFINITY);
+    int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kTpr;
+    if (m < M) next.hold(row<T>(a.logits, m), L, t, low);
+    for (; m < M; m += step) {
+        x = next;
+        if (m + step < M) next.hold(row<T>(a.logits, m + step), L, t, low);   // on its way while this row is worked on
         float *ll = static_cast<float *>(a.ll.data) + m * a.ll.row_stride;
-        const auto load_x = [&](int64_t c, int64_t left, float (&v)[8]) { load8(x_row + c, left, v, -INFINITY); };
-        RowPart<S> x;
-        x.hold(L, t, load_x);
-        const float lse = row_lse<S>(x, load_x, scratch, turn);
-        int v_at = 0;
-        x.each(load_x, [&](int64_t c, int64_t left, float (&v)[8]) {
-            if constexpr (S::kNv == 0) load_p(c, left, prior.x[0]);
-            const float(&p)[8] = prior.x[S::kNv > 0 ? v_at : 0];
-            v_at++;
-            float o[8];
+        const float lse = row_lse<S>(L, t, [&](int v, int64_t c, int64_t left, float (&o)[S::kC]) {
+            x.get(v, c, left, o, -INFINITY);
+        }, scratch, turn);
+        S::each(L, t, [&](int v, int64_t c, int64_t left) {
+            float o[S::kC], p[S::kC] = {};
+            x.get(v, c, left, o);
+            if (a.log_prior) prior.get(v, c, left, p);
 #pragma unroll
-            for (int e = 0; e < 8; e++)
-                o[e] = v[e] == -INFINITY || p[e] == -INFINITY ? -INFINITY : a.scale * ((v[e] - lse) - p[e]);
-            store8(ll + c, left, o);
+            for (int e = 0; e < S::kC; e++)
+                o[e] = o[e] == -INFINITY || p[e] == -INFINITY ? -INFINITY : a.scale * ((o[e] - lse) - p[e]);
+            store_floats(ll + c, left, o);
         });
     }
 }
@@ -126,19 +123,23 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
     const int64_t M = a.logits.rows, L = a.logits.cols;
     const int k = static_cast<int>(a.top_logit.cols), t = threadIdx.x % S::kTpr, sub = threadIdx.x / S::kTpr;
     const float temp = a.temperature, inv_t = 1.0f / temp;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
+    const T low = static_cast<T>(-INFINITY);
     Entries &tab = tables[sub];
-    for (int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + sub; m < M; m += static_cast<int64_t>(gridDim.x) * S::kRows) {
+    RowPart<S, T> x, next;
+    int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + sub;
+    if (m < M) next.hold(row<T>(a.logits, m), L, t, low);
+    for (; m < M; m += step) {
         const T *x_row = row<T>(a.logits, m);
         T *d = a.dlogits.data ? static_cast<T *>(a.dlogits.data) + m * a.dlogits.row_stride : nullptr;
-        const auto load_x = [&](int64_t c, int64_t left, float (&v)[8]) {
-            load8(x_row + c, left, v, -INFINITY);
+        x = next;
+        if (m + step < M) next.hold(row<T>(a.logits, m + step), L, t, low);   // on its way while this row is worked on
+        const auto get_x = [&](int v, int64_t c, int64_t left, float (&o)[S::kC]) {
+            x.get(v, c, left, o, -INFINITY);
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[e] *= inv_t;
+            for (int e = 0; e < S::kC; e++) o[e] *= inv_t;
         };
         const float w = a.weight ? a.weight[m] : 1.0f;
-        RowPart<S> x;
-        if (w != 0.0f || !kBackward) x.hold(L, t, load_x);
-        else x.cols = L, x.t = t;
 
         // the entries: shares, and for each unit one list entry with its whole mass
         int32_t unit[kEntries];
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
                     }
                 if (!first) continue;
                 tab.mass[j] = mass;
-                tab.next[j] = atomicExch(&heads[sub][(unit[i] >> 3) % S::kTpr], j);
+                tab.next[j] = atomicExch(&heads[sub][unit[i] / S::kC % S::kTpr], j);
             }
         }
         // every x of a unit is in registers, and the entries are in place, before dlogits may overwrite a row
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
 
         float lse = 0.0f;
         if constexpr (kBackward) lse = a.lse[m];
-        else if (live || a.lse) lse = row_lse<S>(x, load_x, scratch, turn);
+        else if (live || a.lse) lse = row_lse<S>(L, t, get_x, scratch, turn);
         if constexpr (!kBackward) {
             if (a.lse && t == 0) a.lse[m] = lse;
             if (a.loss && t < 64) {
@@ -227,21 +228,23 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
         if (d) {
             const float scale = w * temp;
             if (live) {
-                x.each(load_x, [&](int64_t c, int64_t left, float (&v)[8]) {
-                    float g[8];
+                S::each(L, t, [&](int v, int64_t c, int64_t left) {
+                    float g[S::kC];
+                    get_x(v, c, left, g);
 #pragma unroll
-                    for (int e = 0; e < 8; e++) g[e] = am_exp(v[e] - lse);
-                    for (int j = heads[sub][t]; j >= 0; j = tab.next[j])
-                        if (tab.unit[j] >> 3 == c >> 3)
+                    for (int e = 0; e < S::kC; e++) g[e] = am_exp(g[e] - lse);
+                    for (int j = heads[sub][t]; j >= 0; j = tab.next[j]) {
+                        const int64_t at = tab.unit[j] - c;
 #pragma unroll
-                            for (int e = 0; e < 8; e++) g[e] -= (tab.unit[j] & 7) == e ? tab.mass[j] : 0.0f;
+                        for (int e = 0; e < S::kC; e++) g[e] -= at == e ? tab.mass[j] : 0.0f;
+                    }
 #pragma unroll
-                    for (int e = 0; e < 8; e++) g[e] *= scale;
-                    store8(d + c, left, g);
+                    for (int e = 0; e < S::kC; e++) g[e] *= scale;
+                    store_floats(d + c, left, g);
                 });
             } else {
-                const float zero[8] = {};
-                for (int64_t c = static_cast<int64_t>(t) * 8; c < L; c += S::kTpr * 8) store8(d + c, L - c, zero);
+                const float zero[S::kC] = {};
+                for (int64_t c = static_cast<int64_t>(t) * S::kC; c < L; c += S::kTpr * S::kC) store_floats(d + c, L - c, zero);
             }
         }
         // the tables are written again for the next row
@@ -250,12 +253,12 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
     }
 }
 
-constexpr int64_t kBlocks = 256 * 16;
+constexpr int64_t kBlocks = 256 * 8;
 
 template <typename T>
 void launch_loglikes(const wfst_am_loglikes_args &a, hipStream_t st)
 {
-    am_row_shape(a.logits.cols, [&](auto shape) {
+    am_row_shape<4>(a.logits.cols, [&](auto shape) {
         using S = decltype(shape);
         loglikes_kernel<T, S><<<am_row_blocks<S>(a.logits.rows, kBlocks), S::kThreads, 0, st>>>(a);
     });
@@ -264,7 +267,7 @@ void launch_loglikes(const wfst_am_loglikes_args &a, hipStream_t st)
 template <typename T>
 void launch_distill(const wfst_am_distill_args &a, bool backward, hipStream_t st)
 {
-    am_row_shape(a.logits.cols, [&](auto shape) {
+    am_row_shape<sizeof(T) == 4 ? 4 : 8>(a.logits.cols, [&](auto shape) {
         using S = decltype(shape);
         const unsigned g = am_row_blocks<S>(a.logits.rows, kBlocks);
         if (backward) distill_kernel<T, S, true><<<g, S::kThreads, 0, st>>>(a);
