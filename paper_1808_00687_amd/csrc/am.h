@@ -1,5 +1,5 @@
 // Acoustic-model operators: what the checks (am.cpp) and the kernels
-// (am_norm.hip, am_softmax.hip, am_linear*.hip) share.
+// (am_norm.hip, am_distill.hip, am_loglikes.hip, am_linear*.hip) share.
 #pragma once
 
 #include <hip/hip_runtime.h>

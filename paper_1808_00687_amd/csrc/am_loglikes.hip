@@ -1,0 +1,62 @@
+// Log-likelihood rows from logits.
+//
+// Bound by memory: a row is read once into registers; each wave takes its
+// maximum and the sum of exponentials relative to it, the waves' pairs are joined
+// (a row's log sum exp in one barrier), and the row is written from registers.
+#include "am_softmax.h"
+
+namespace wfd {
+namespace {
+
+template <typename T, typename S>
+__global__ __launch_bounds__(S::kThreads) void loglikes_kernel(wfst_am_loglikes_args a)
+{
+    __shared__ RowScratch scratch;
+    int turn = 0;
+    const int64_t M = a.logits.rows, L = a.logits.cols, step = static_cast<int64_t>(gridDim.x) * S::kRows;
+    const int t = threadIdx.x % S::kTpr;
+    RowPart<S, float> prior;
+    if (a.log_prior) prior.hold(a.log_prior, L, t);
+    RowPart<S, T> x, next;
+    const T low = static_cast<T>(-INFINITY);
+    int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kTpr;
+    if (m < M) next.hold(row<T>(a.logits, m), L, t, low);
+    for (; m < M; m += step) {
+        x = next;
+        if (m + step < M) next.hold(row<T>(a.logits, m + step), L, t, low);   // on its way while this row is worked on
+        float *ll = static_cast<float *>(a.ll.data) + m * a.ll.row_stride;
+        const float lse = lse_of(row_stat<S>(L, t, kLog2e, [&](int v, int64_t c, int64_t left, float (&o)[S::kC]) {
+            x.get(v, c, left, o, -INFINITY);
+        }, [](int, const float (&)[S::kC]) {}, scratch, turn));
+        S::each(L, t, [&](int v, int64_t c, int64_t left) {
+            float o[S::kC], p[S::kC] = {};
+            x.get(v, c, left, o);
+            if (a.log_prior) prior.get(v, c, left, p);
+#pragma unroll
+            for (int e = 0; e < S::kC; e++)
+                o[e] = o[e] == -INFINITY || p[e] == -INFINITY ? -INFINITY : a.scale * ((o[e] - lse) - p[e]);
+            store_floats(ll + c, left, o);
+        });
+    }
+}
+
+template <typename T>
+void launch(const wfst_am_loglikes_args &a, hipStream_t st)
+{
+    am_row_shape<4>(a.logits.cols, [&](auto shape) {
+        using S = decltype(shape);
+        loglikes_kernel<T, S><<<am_row_blocks<S>(a.logits.rows, kSoftmaxBlocks), S::kThreads, 0, st>>>(a);
+    });
+}
+
+}  // namespace
+
+hipError_t am_launch_loglikes(const wfst_am_loglikes_args &a, hipStream_t st)
+{
+    if (a.logits.type == WFST_F32) launch<float>(a, st);
+    else if (a.logits.type == WFST_F16) launch<f16>(a, st);
+    else launch<bf16>(a, st);
+    return hipGetLastError();
+}
+
+}  // namespace wfd

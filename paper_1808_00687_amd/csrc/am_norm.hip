@@ -217,30 +217,38 @@ __global__ __launch_bounds__(256) void norm_dgain_kernel(wfst_am_norm_backward_a
     a.dgain[d] = t;
 }
 
-// 32 columns a workgroup, 8 threads a column
-__global__ __launch_bounds__(256) void column_join_kernel(const float *partial, int64_t strips, int64_t n, float *out)
+// 32 columns a workgroup, 32 threads a column, 4 strips of a thread on their way at a time
+__global__ __launch_bounds__(1024) void column_join_kernel(const float *partial, int64_t strips, int64_t n, float *out)
 {
-    __shared__ float part[8][32];
+    __shared__ float part[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + x;
     float t = 0.0f;
-    if (c < n)
-        for (int64_t s = y; s < strips; s += 8) t += partial[s * n + c];
+    if (c < n) {
+        int64_t s = y;
+        for (; s + 96 < strips; s += 128) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[i] = partial[(s + i * 32) * n + c];
+            t += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+        for (; s < strips; s += 32) t += partial[s * n + c];
+    }
     part[y][x] = t;
     __syncthreads();
     if (y != 0 || c >= n) return;
-    for (int i = 1; i < 8; i++) t += part[i][x];
+    for (int i = 1; i < 32; i++) t += part[i][x];
     out[c] = t;
 }
 
 constexpr int64_t kForwardBlocks = 256 * 16;
-constexpr int64_t kBackwardBlocks = 256 * 4;
+constexpr int64_t kBackwardBlocks = 256 * 3;
 
 // strips of rows whose sums of the gain's gradient are joined
 int64_t dgain_strips(int64_t M, int64_t D)
 {
     int64_t n = 0;
-    am_row_shape<8>(D, [&](auto shape) {   // the same for shorter chunks
+    am_row_shape_lean<8>(D, [&](auto shape) {   // the same for shorter chunks
         using S = decltype(shape);
         n = S::kNv > 0 ? static_cast<int64_t>(am_row_blocks<S>(M, kBackwardBlocks)) : 0;
     });
@@ -263,7 +271,7 @@ void launch_norm_backward(const wfst_am_norm_backward_args &a, hipStream_t st)
 {
     const int64_t M = a.s.rows, D = a.s.cols;
     float *work = static_cast<float *>(a.workspace);
-    am_row_shape<kChunk<T>>(D, [&](auto shape) {
+    am_row_shape_lean<kChunk<T>>(D, [&](auto shape) {
         using S = decltype(shape);
         const unsigned g = M ? am_row_blocks<S>(M, kBackwardBlocks) : 0;
         if constexpr (S::kNv > 0) {
@@ -286,7 +294,7 @@ void launch_norm_backward(const wfst_am_norm_backward_args &a, hipStream_t st)
 
 void am_launch_column_join(const float *partial, int64_t strips, int64_t n, float *out, hipStream_t st)
 {
-    column_join_kernel<<<static_cast<unsigned>((n + 31) / 32), 256, 0, st>>>(partial, strips, n, out);
+    column_join_kernel<<<static_cast<unsigned>((n + 31) / 32), 1024, 0, st>>>(partial, strips, n, out);
 }
 
 hipError_t am_launch_norm(const wfst_am_norm_args &a, hipStream_t st)

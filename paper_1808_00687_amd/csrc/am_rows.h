@@ -55,6 +55,17 @@ void am_row_shape(int64_t D, F go)
     else go(RowShape<1024, 0, C>{});
 }
 
+// The same for an operator that holds several matrices and sums besides:
+// rows of 1,024 to 2,048 go to 256 threads, a chunk each.
+template <int C, typename F>
+void am_row_shape_lean(int64_t D, F go)
+{
+    constexpr int k = 8 / C;
+    if (D > 1024 && D <= 2048) go(RowShape<256, 1 * k, C>{});
+    else if (D > 4096 && D <= 8192) go(RowShape<1024, 1 * k, C>{});
+    else am_row_shape<C>(D, go);
+}
+
 // Workgroups for M rows: all of them up to `most`, which then take several.
 template <typename S>
 unsigned am_row_blocks(int64_t M, int64_t most)

@@ -1,0 +1,74 @@
+// Softmax statistics of a row, for the operators over units.
+#pragma once
+
+#include "am_rows.h"
+
+namespace wfd {
+
+template <typename T>
+__device__ __forceinline__ const T *row(const wfst_matrix &m, int64_t r)
+{
+    return static_cast<const T *>(m.data) + r * m.row_stride;
+}
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+// A row's softmax statistics in base 2, with y = x * c and c = log2(e) / temperature:
+struct RowStat {
+    float top;    // largest y; 0 for a row of -inf
+    float own;    // largest y of the thread's wave, likewise: what `keep` got is relative to it
+    float sum;    // of 2^(y - top)
+};
+
+// get(v, column, left, x): a chunk, -inf beyond the row.  keep(v, e): 2^(y - own) of the chunk.
+template <typename S, typename G, typename K>
+__device__ __forceinline__ RowStat row_stat(int64_t cols, int t, float c, G get, K keep, RowScratch &r, int &turn)
+{
+    float top = -INFINITY;
+    S::each(cols, t, [&](int v, int64_t at, int64_t left) {
+        float x[S::kC];
+        get(v, at, left, x);
+#pragma unroll
+        for (int e = 0; e < S::kC; e++) top = fmaxf(top, x[e]);
+    });
+    top = wave_max(top) * c;
+    RowStat o;
+    o.own = top == -INFINITY ? 0.0f : top;
+    float s = 0.0f;
+    S::each(cols, t, [&](int v, int64_t at, int64_t left) {
+        float x[S::kC];
+        get(v, at, left, x);
+#pragma unroll
+        for (int e = 0; e < S::kC; e++) {
+            x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], c, -o.own));
+            s += x[e];
+        }
+        keep(v, x);
+    });
+    s = wave_sum(s);
+    if constexpr (S::kWaves > 1) {
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) r.a[turn][wave] = top, r.b[turn][wave] = s;
+        __syncthreads();
+        top = r.a[turn][0];
+#pragma unroll
+        for (int i = 1; i < S::kWaves; i++) top = fmaxf(top, r.a[turn][i]);
+        o.top = top == -INFINITY ? 0.0f : top;
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::kWaves; i++)   // a wave of -inf has sum 0
+            s += r.a[turn][i] == -INFINITY ? r.b[turn][i] : r.b[turn][i] * __builtin_amdgcn_exp2f(r.a[turn][i] - o.top);
+        turn ^= 1;
+    } else {
+        o.top = o.own;
+    }
+    o.sum = s;
+    return o;
+}
+
+// log sum exp of x / temperature; -inf for a row of -inf
+__device__ __forceinline__ float lse_of(const RowStat &s) { return s.top * kLn2 + logf(s.sum); }
+
+constexpr int64_t kSoftmaxBlocks = 256 * 8;
+
+}  // namespace wfd
