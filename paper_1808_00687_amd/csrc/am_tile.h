@@ -357,34 +357,55 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void am_tile_kernel(AmProduct p)
         #pragma unroll
         for (int g = 0; g < TJ; g++) acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const auto multiply = [&](const char *as, const char *bs) {
+    // A stage is 2 TI steps of TJ products; step t has half t / TI of the
+    // stage's k and rows t % TI.  Fragments are read two steps ahead, also over
+    // the end of a stage: its last reads are done two steps before its last
+    // products, and there the waves meet, the stage after next is fetched into
+    // this one's place and the next one's first fragments are read.  The
+    // scheduling fences keep that order.
+    constexpr int kSteps = 2 * TI, kAhead = 2, kX = 4;   // kX divides kSteps: the next stage's first x are none of the last two
+    static_assert(TI >= 2 && kSteps % kX == 0, "");
+    i32x4 x[kX], y[2][TJ];
+    const auto read_y = [&](const char *bs, int kk) {
 #pragma unroll
-        for (int kk = 0; kk < 2; kk++) {
-            if constexpr (sizeof(E) == 1) {
-                // The 8-bit matrix instructions drop the low bits of products far below the largest one of
-                // their 128 (errors up to 2^-12 of it); as bf16 the products and their sums are kept in 32 bits
-                i32x4 y0[TJ], y1[TJ], x0, x1;
+        for (int g = 0; g < TJ; g++) y[kk][g] = sb.fragment(bs, wj, g, kk, lane);
+    };
+    const auto read_x = [&](const char *as, int t) { x[t % kX] = sa.fragment(as, wi, t % TI, t / TI, lane); };
+    i32x4 y0[TJ], y1[TJ];   // 8 bits: y widened
+    const auto products = [&](int t) {
+        const int f = t % TI, kk = t / TI;
+        if constexpr (sizeof(E) == 1) {
+            // The 8-bit matrix instructions drop the low bits of products far below the largest one of
+            // their 128 (errors up to 2^-12 of it); as bf16 the products and their sums are kept in 32 bits
+            if (f == 0)
 #pragma unroll
-                for (int g = 0; g < TJ; g++) am_widen(sb.fragment(bs, wj, g, kk, lane), y0[g], y1[g]);
+                for (int g = 0; g < TJ; g++) am_widen(y[kk][g], y0[g], y1[g]);
+            i32x4 x0, x1;
+            am_widen(x[t % kX], x0, x1);
 #pragma unroll
-                for (int f = 0; f < TI; f++) {
-                    am_widen(sa.fragment(as, wi, f, kk, lane), x0, x1);
+            for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<bf16>(y0[g], x0, acc[f][g]);
 #pragma unroll
-                    for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<bf16>(y0[g], x0, acc[f][g]);
+            for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<bf16>(y1[g], x1, acc[f][g]);
+        } else {
 #pragma unroll
-                    for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<bf16>(y1[g], x1, acc[f][g]);
-                }
-            } else {
-                i32x4 y[TJ];
+            for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<E>(y[kk][g], x[t % kX], acc[f][g]);
+        }
+    };
+    const auto first_reads = [&](const char *as, const char *bs) {
+        read_y(bs, 0);
 #pragma unroll
-                for (int g = 0; g < TJ; g++) y[g] = sb.fragment(bs, wj, g, kk, lane);
+        for (int t = 0; t < kAhead; t++) read_x(as, t);
+    };
+    // one stage; next(): what to do where the waves meet
+    const auto stage = [&](const char *as, const char *bs, auto next) {
 #pragma unroll
-                for (int f = 0; f < TI; f++) {
-                    const i32x4 x = sa.fragment(as, wi, f, kk, lane);
-#pragma unroll
-                    for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<E>(y[g], x, acc[f][g]);
-                }
-            }
+        for (int t = 0; t < kSteps; t++) {
+            if (t == TI - kAhead) read_y(bs, 1);
+            if (t + kAhead < kSteps) read_x(as, t + kAhead);
+            if (t + kAhead == kSteps) next();
+            __builtin_amdgcn_sched_barrier(0);
+            products(t);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
@@ -401,22 +422,39 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void am_tile_kernel(AmProduct p)
             sa.fetch(p.a, i0, p.inner, s * kStageK, as, wave);
             sb.fetch(p.b, j0, p.inner, s * kStageK, bs, wave);
         };
-        fetch(a0, b0, s_first);
+        // stages in pairs; of an odd number the first goes alone, through the second place
         int32_t s = s_first;
-        for (; s + 2 <= s_last; s += 2) {
-            __syncthreads();   // this stage has landed, the other one is read
+        if ((s_last - s_first) % 2) {
+            fetch(a1, b1, s);
+            fetch(a0, b0, s + 1);
+            __syncthreads();
+            first_reads(a1, b1);
+            stage(a1, b1, [&] {
+                __syncthreads();
+                first_reads(a0, b0);
+                fetch(a1, b1, s + 2);
+            });
+            s++;
+        } else {
+            fetch(a0, b0, s);
             fetch(a1, b1, s + 1);
-            multiply(a0, b0);
             __syncthreads();
-            fetch(a0, b0, s + 2);
-            multiply(a1, b1);
+            first_reads(a0, b0);
         }
-        if (s < s_last) {
-            __syncthreads();
-            multiply(a0, b0);
+        for (; s < s_last; s += 2) {
+            stage(a0, b0, [&] {
+                __syncthreads();   // the next stage has landed, this one is read
+                first_reads(a1, b1);
+                fetch(a0, b0, s + 2);
+            });
+            stage(a1, b1, [&] {
+                __syncthreads();
+                first_reads(a0, b0);
+                fetch(a1, b1, s + 3);
+            });
         }
     } else {
-        i32x4 ra[SideA::kPerWave], rb[SideB::kPerWave];
+        i32x4 ra[SideA::kPerWave] = {}, rb[SideB::kPerWave] = {};
         const auto load = [&](int32_t s) {
             if (s >= s_last) return;
             sa.load(p.a, i0, p.inner, s * kStageK, ra, wave, lane);
@@ -426,24 +464,31 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void am_tile_kernel(AmProduct p)
             sa.put(ra, as, wave, lane);
             sb.put(rb, bs, wave, lane);
         };
-        if (s_first < s_last) {
-            load(s_first);
-            put(a0, b0);
-        }
         int32_t s = s_first;
-        for (; s + 2 <= s_last; s += 2) {
+        if ((s_last - s_first) % 2) {
+            load(s);
+            put(a1, b1);
             __syncthreads();
             load(s + 1);
-            multiply(a0, b0);
+            first_reads(a1, b1);
+            stage(a1, b1, [] {});
+            put(a0, b0);
+            s++;
+        } else {
+            load(s);
+            put(a0, b0);
+        }
+        for (; s < s_last; s += 2) {
+            __syncthreads();
+            load(s + 1);
+            first_reads(a0, b0);
+            stage(a0, b0, [] {});
             put(a1, b1);
             __syncthreads();
             load(s + 2);
-            multiply(a1, b1);
-            if (s + 2 < s_last) put(a0, b0);
-        }
-        if (s < s_last) {
-            __syncthreads();
-            multiply(a0, b0);
+            first_reads(a1, b1);
+            stage(a1, b1, [] {});
+            put(a0, b0);
         }
     }
 
