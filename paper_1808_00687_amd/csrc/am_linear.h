@@ -7,13 +7,13 @@ namespace wfd {
 
 // out = a b^T, both k-contiguous (am_linear_f16.hip, am_linear_bf16.hip, am_linear_f8.hip)
 template <typename E>
-void am_product_forward(const AmProduct &p, hipStream_t st);
+void am_product_forward(const AmProduct &p, int32_t tile, hipStream_t st);
 // dx[m][k] = sum_n dz[m][n] w[n][k]: w is k-major
 template <typename E>
-void am_product_dx(const AmProduct &p, hipStream_t st);
+void am_product_dx(const AmProduct &p, int32_t tile, hipStream_t st);
 // dw[n][k] = sum_m dz[m][n] x[m][k]: both are k-major
 template <typename E>
-void am_product_dw(const AmProduct &p, hipStream_t st);
+void am_product_dw(const AmProduct &p, int32_t tile, hipStream_t st);
 
 inline bool am_rows_aligned(const wfst_matrix &m)
 {
@@ -27,7 +27,7 @@ constexpr int64_t am_dz_stride(int64_t n) { return (n + 7) & ~int64_t{7}; }
 // column sums and each product's parts use one after the other.
 struct BackwardPlan {
     int64_t dz_bytes, partial_bytes;
-    int32_t dx_splits, dw_splits;
+    AmPlan dx, dw;
     int32_t across;   // threads side by side in the pass over dy
     int64_t strips;   // of rows, in that pass
 };
@@ -35,7 +35,7 @@ struct BackwardPlan {
 inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a)
 {
     const int64_t M = a.dy.rows, N = a.dy.cols;
-    BackwardPlan p{0, 0, 1, 1, 1, 1};
+    BackwardPlan p{0, 0, {64, 1}, {64, 1}, 1, 1};
     while (p.across < 64 && p.across * 8 < N) p.across *= 2;
     // 4 rows a thread at least, about 1,024 workgroups at most
     const int64_t wide = (N + p.across * 8 - 1) / (p.across * 8), tall = M * p.across / 1024, most = 1024 / wide;
@@ -44,13 +44,13 @@ inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a)
     if (a.dbias && p.strips > 1) p.partial_bytes = (p.strips * N * 4 + 255) & ~int64_t{255};
     if (a.activation != WFST_ACT_NONE && (a.dx.data || a.dw.data)) p.dz_bytes = (M * am_dz_stride(N) * 2 + 255) & ~int64_t{255};
     if (a.dx.data) {
-        p.dx_splits = am_splits(M, a.dx.cols, N);
-        const int64_t b = am_partial_bytes(M, a.dx.cols, p.dx_splits);
+        p.dx = am_plan(M, a.dx.cols, N, true);
+        const int64_t b = am_partial_bytes(M, a.dx.cols, p.dx.splits);
         p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
     }
     if (a.dw.data) {
-        p.dw_splits = am_splits(N, a.dw.cols, M);
-        const int64_t b = am_partial_bytes(N, a.dw.cols, p.dw_splits);
+        p.dw = am_plan(N, a.dw.cols, M, true);
+        const int64_t b = am_partial_bytes(N, a.dw.cols, p.dw.splits);
         p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
     }
     return p;

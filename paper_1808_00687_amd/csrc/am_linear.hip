@@ -89,22 +89,22 @@ void launch_backward(const wfst_am_linear_backward_args &a, hipStream_t st)
         p.a = {g, ld, static_cast<int32_t>(M)};
         p.b = {static_cast<const char *>(a.w.data), a.w.row_stride * 2, static_cast<int32_t>(a.dx.cols)};
         p.inner = static_cast<int32_t>(N);
-        p.splits = plan.dx_splits;
+        p.splits = plan.dx.splits;
         p.partial = partial;
         p.out = a.dx;
         p.vec = am_rows_aligned(p.out);
-        am_product_dx<T>(p, st);
+        am_product_dx<T>(p, plan.dx.tile, st);
     }
     if (a.dw.data) {
         AmProduct p{};
         p.a = {g, ld, static_cast<int32_t>(N)};
         p.b = {static_cast<const char *>(a.x.data), a.x.row_stride * 2, static_cast<int32_t>(a.dw.cols)};
         p.inner = static_cast<int32_t>(M);
-        p.splits = plan.dw_splits;
+        p.splits = plan.dw.splits;
         p.partial = partial;   // the other product's parts are joined by now
         p.out = a.dw;
         p.vec = am_rows_aligned(p.out);
-        am_product_dw<T>(p, st);
+        am_product_dw<T>(p, plan.dw.tile, st);
     }
 }
 
@@ -128,9 +128,10 @@ hipError_t am_launch_linear(const wfst_am_linear_args &a, hipStream_t st)
     p.residual = a.residual, p.pre = a.pre, p.out = a.y;
     p.activation = a.activation;
     p.vec = am_rows_aligned(a.y) && (!a.residual.data || am_rows_aligned(a.residual)) && (!a.pre.data || am_rows_aligned(a.pre));
-    if (a.x.type == WFST_F16) am_product_forward<f16>(p, st);
-    else if (a.x.type == WFST_BF16) am_product_forward<bf16>(p, st);
-    else am_product_forward<f8>(p, st);
+    const int32_t tile = am_plan(a.x.rows, a.w.rows, a.x.cols, false).tile;
+    if (a.x.type == WFST_F16) am_product_forward<f16>(p, tile, st);
+    else if (a.x.type == WFST_BF16) am_product_forward<bf16>(p, tile, st);
+    else am_product_forward<f8>(p, tile, st);
     return hipGetLastError();
 }
 

@@ -4,21 +4,21 @@
 namespace wfd {
 
 template <>
-void am_product_forward<f16>(const AmProduct &p, hipStream_t st)
+void am_product_forward<f16>(const AmProduct &p, int32_t tile, hipStream_t st)
 {
-    am_product<f16, false, false>(p, st);
+    am_product<f16, false, false>(p, tile, st);
 }
 
 template <>
-void am_product_dx<f16>(const AmProduct &p, hipStream_t st)
+void am_product_dx<f16>(const AmProduct &p, int32_t tile, hipStream_t st)
 {
-    am_product<f16, false, true>(p, st);
+    am_product<f16, false, true>(p, tile, st);
 }
 
 template <>
-void am_product_dw<f16>(const AmProduct &p, hipStream_t st)
+void am_product_dw<f16>(const AmProduct &p, int32_t tile, hipStream_t st)
 {
-    am_product<f16, true, true>(p, st);
+    am_product<f16, true, true>(p, tile, st);
 }
 
 }  // namespace wfd

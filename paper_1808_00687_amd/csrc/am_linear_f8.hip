@@ -4,9 +4,9 @@
 namespace wfd {
 
 template <>
-void am_product_forward<f8>(const AmProduct &p, hipStream_t st)
+void am_product_forward<f8>(const AmProduct &p, int32_t tile, hipStream_t st)
 {
-    am_product<f8, false, false>(p, st);
+    am_product<f8, false, false>(p, tile, st);
 }
 
 }  // namespace wfd

@@ -3,11 +3,16 @@
 // with each operand stored k-contiguous (rows of k) or k-major (rows of i or
 // j, one row a k).
 //
-// A workgroup computes a BM x BN tile, stage by stage: a stage holds 128 bytes
-// of k for every row of the tile (64 values of 16 bits, 128 of 8).  Two stages
-// lie in LDS; the next one is fetched while the matrix cores work on the
-// present one.  The fetch goes straight from memory to LDS (16 bytes a lane, no
-// registers); operands that are not aligned to 16 bytes go through registers.
+// A workgroup computes a BM x BN tile, stage by stage: a stage holds 64 values
+// of k for every row of the tile.  Two stages lie in LDS; the next one is fetched
+// while the matrix cores work on the present one.  The fetch goes straight from
+// memory to LDS (16 bytes a lane, no registers); operands that are not aligned to
+// 16 bytes, and 8-bit ones, go through registers.
+//
+// 8-bit operands are widened to bf16 on the way (each value exactly).  The
+// 8-bit matrix instructions would be twice as fast, but drop the low bits of
+// products far below the largest one of their 128 (errors up to 2^-12 of it); as
+// bf16 the products and their sums are kept in 32 bits.
 //
 // LDS layout.  A stage is a row of 16-byte chunks for each row of the operand
 // as stored; a chunk sits at its index XOR a function of the row, so that the
@@ -25,6 +30,9 @@
 // are dealt to the fragments so that a lane holds 4 * TJ consecutive j.
 #pragma once
 
+#include <type_traits>
+#include <utility>
+
 #include "am_device.h"
 
 namespace wfd {
@@ -36,7 +44,19 @@ using f32x4 = float __attribute__((ext_vector_type(4)));
 using f16x8 = f16 __attribute__((ext_vector_type(8)));
 using bf16x8 = bf16 __attribute__((ext_vector_type(8)));
 
-constexpr int kStageBytes = 128;   // of k, a row
+// use(0), use(1), ... use(N - 1), each with a constant
+template <int N, typename F, int... I>
+__device__ __forceinline__ void am_each(F use, std::integer_sequence<int, I...>)
+{
+    (use(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void am_each(F use)
+{
+    am_each<N>(use, std::make_integer_sequence<int, N>{});
+}
+
+constexpr int kStageK = 64;   // values of k in a stage
 
 struct AmOperand {
     const char *data;
@@ -199,14 +219,17 @@ __device__ __forceinline__ void am_tile_of(uint32_t block, uint32_t rows, uint32
 constexpr int am_log2(int x) { return x <= 1 ? 0 : 1 + am_log2(x / 2); }
 
 // One operand's part of the tile kernel: R rows (i or j), kMajor its storage,
-// kDeal > 1: rows dealt to fragments so that a lane gets kDeal runs of 4 rows.
-template <typename E, int R, int kWaves, bool kMajor, int kDeal>
+// kDeal > 1: rows dealt to fragments so that a lane gets kDeal runs of 4 rows;
+// kFar: rows so far apart that offsets inside a tile pass 31 bits.
+template <typename E, int R, int kWaves, bool kMajor, int kDeal, bool kFar>
 struct AmSide {
     static constexpr int kEl = sizeof(E);
-    static constexpr int kPerWave = R / 8 / kWaves;      // fetches of 1 KiB a wave
-    static constexpr int kRowChunks = kMajor ? R * kEl / 16 : 8;
-    static constexpr int kBytes = R * kStageBytes;
-    static_assert(R % (8 * kWaves) == 0, "a stage is whole fetches");
+    static constexpr int kRowChunks = kMajor ? R / 8 : 8;   // of 8 values, in a row of LDS
+    static constexpr int kBytes = R * kStageK * 2;
+    static constexpr int kPerWave = R / 8 / kWaves;         // KiB of LDS a wave fills
+    static constexpr int kWide = 16 / kEl;                  // values of 16 bytes in memory
+    static constexpr int kLoads = kPerWave * 8 / kWide;     // 16-byte loads a lane, through registers
+    static_assert(R % (8 * kWaves) == 0 && (kEl == 2 || (!kMajor && kPerWave % 2 == 0)), "");
 
     // chunk permutation of a stored row
     __device__ static __forceinline__ int permute(int row)
@@ -224,13 +247,12 @@ struct AmSide {
 
     int32_t voff[kPerWave];      // direct: byte offset of each fetch from the stage's base
 
-    // the row as stored, and the chunk in it, that a lane fetches
+    // the row as stored, and the chunk in it, that goes to a lane's place in LDS
     __device__ static __forceinline__ int row_of(int q, int wave, int lane) { return ((wave * kPerWave + q) * 64 + lane) / kRowChunks; }
     __device__ static __forceinline__ int chunk_of(int q, int wave, int lane)
     {
         return (lane % kRowChunks) ^ permute(row_of(q, wave, lane));
     }
-    static_assert(64 % kRowChunks == 0 || kRowChunks % 64 == 0, "");
 
     __device__ __forceinline__ void init(const AmOperand &o, int wave, int lane)
     {
@@ -250,9 +272,10 @@ struct AmSide {
                 voff[q] = chunk_of(q, wave, lane) * 16 < tail ? voff[q] : static_cast<int32_t>(0x80000000u);
     }
 
-    // Straight to LDS.  Rows past the operand's end are past the range of the
-    // buffer descriptor and read as zeros.
-    __device__ __forceinline__ void fetch(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, char *stage, int wave)
+    // Straight to LDS (16-bit values): the descriptor of a stage, then its
+    // fetches.  Rows past the operand's end are past the range of the descriptor
+    // and read as zeros, as does a stage that is not there.
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t stage_rsrc(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, bool there) const
     {
         int64_t skip, size;
         if constexpr (kMajor) {
@@ -262,33 +285,38 @@ struct AmSide {
             skip = first * o.ld + static_cast<int64_t>(k0) * kEl;
             size = (static_cast<int64_t>(o.extent) - 1) * o.ld + static_cast<int64_t>(inner) * kEl;
         }
-        const int64_t left = size - skip;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(o.data) + skip, 0,
-                                                            static_cast<int>(left < 0x7FFFFFFF ? left : 0x7FFFFFFF), 0x00027000);
-#pragma unroll
-        for (int q = 0; q < kPerWave; q++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (AM_LDS void *)((AM_LDS char *)stage + (wave * kPerWave + q) * 1024),
-                                                     16, voff[q], 0, 0, 0);
+        const int64_t left = there ? size - skip : 0;
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(o.data) + skip, 0,
+                                                 static_cast<int>(left < 0x7FFFFFFF ? left : 0x7FFFFFFF), 0x00027000);
+    }
+    __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t rsrc, int q, char *stage, int wave) const
+    {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (AM_LDS void *)((AM_LDS char *)stage + (wave * kPerWave + q) * 1024),
+                                                 16, voff[q], 0, 0, 0);
     }
 
-    // Through registers, any alignment: what is outside reads as zeros.
-    __device__ __forceinline__ void load(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, i32x4 (&r)[kPerWave], int wave, int lane)
+    // Through registers, any alignment.  Values past k's end are zeros; rows
+    // past the operand's end repeat the last one (their results are not stored).
+    __device__ __forceinline__ void load(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, i32x4 (&r)[kLoads], int wave, int lane)
     {
-        #pragma unroll
-        for (int q = 0; q < kPerWave; q++) {
-            const int row = row_of(q, wave, lane), chunk = chunk_of(q, wave, lane);
-            const int64_t k = kMajor ? k0 + row : k0 + chunk * (16 / kEl);
-            const int64_t x = kMajor ? first + chunk * (16 / kEl) : first + row;
-            const int64_t along = kMajor ? o.extent - x : inner - k;      // values left in the stored row
-            const bool inside = kMajor ? k < inner : x < o.extent;
-            const AM_GLOBAL char *p = (const AM_GLOBAL char *)o.data + (kMajor ? k * o.ld + x * kEl : x * o.ld + k * kEl);
+        using Offset = std::conditional_t<kFar, int64_t, int32_t>;
+        const AM_GLOBAL char *base = (const AM_GLOBAL char *)o.data + (kMajor ? k0 * o.ld + first * kEl : first * o.ld + static_cast<int64_t>(k0) * kEl);
+        const int32_t rows_left = o.extent - static_cast<int32_t>(first), k_left = inner - k0;
+#pragma unroll
+        for (int q = 0; q < kLoads; q++) {
+            // row as stored and first value in it, from `base` on; 8 bits: 4 loads a row of 64 values
+            int32_t row = kEl == 2 ? row_of(q, wave, lane) : ((wave * kLoads + q) * 64 + lane) / 4;
+            const int32_t at = kEl == 2 ? chunk_of(q, wave, lane) * 8 : lane % 4 * 16;
+            if constexpr (!kMajor) row = row < rows_left ? row : rows_left - 1;
+            const int32_t along = (kMajor ? rows_left : k_left) - at;   // values left in the stored row
+            const AM_GLOBAL char *p = base + (static_cast<Offset>(row) * static_cast<Offset>(o.ld) + at * kEl);
             i32x4 v = {0, 0, 0, 0};
-            if (inside && along >= 16 / kEl) {
+            if (along >= kWide && (!kMajor || row < k_left)) {
                 v = *(const AM_GLOBAL i32x4_any *)p;
-            } else if (inside && along > 0) {
+            } else if (along > 0 && (!kMajor || row < k_left)) {
                 uint32_t w[4] = {0, 0, 0, 0};
-                #pragma unroll
-                for (int e = 0; e < 16 / kEl; e++)
+#pragma unroll
+                for (int e = 0; e < kWide; e++)
                     if (e < along) {
                         uint32_t t;
                         if constexpr (kEl == 2) t = ((const AM_GLOBAL uint16_t *)p)[e];
@@ -300,41 +328,50 @@ struct AmSide {
             r[q] = v;
         }
     }
-    __device__ __forceinline__ void put(const i32x4 (&r)[kPerWave], char *stage, int wave, int lane)
+    __device__ __forceinline__ void put(const i32x4 (&r)[kLoads], char *stage, int wave, int lane)
     {
-        #pragma unroll
-        for (int q = 0; q < kPerWave; q++)
-            *reinterpret_cast<i32x4 *>(stage + ((wave * kPerWave + q) * 64 + lane) * 16) = r[q];
+#pragma unroll
+        for (int q = 0; q < kLoads; q++) {
+            if constexpr (kEl == 2) {
+                *reinterpret_cast<i32x4 *>(stage + ((wave * kPerWave + q) * 64 + lane) * 16) = r[q];
+            } else {
+                const int row = ((wave * kLoads + q) * 64 + lane) / 4, c = lane % 4 * 2;
+                i32x4 lo, hi;
+                am_widen(r[q], lo, hi);
+                *reinterpret_cast<i32x4 *>(stage + row * (kStageK * 2) + ((c ^ permute(row)) << 4)) = lo;
+                *reinterpret_cast<i32x4 *>(stage + row * (kStageK * 2) + (((c + 1) ^ permute(row)) << 4)) = hi;
+            }
+        }
     }
 
-    // Fragment f (of the wave's rows from `base` on), half kk of a stage's k (32 values of 16 bits, 64 of 8)
+    // Fragment f (of the wave's rows from `base` on), half kk of a stage's k
     __device__ __forceinline__ i32x4 fragment(const char *stage, int base, int f, int kk, int lane) const
     {
         const int g = lane >> 4, s = lane & 15;
         if constexpr (kMajor) {
             i16x4 h[2];
-            #pragma unroll
+#pragma unroll
             for (int t = 0; t < 2; t++) {
                 const int row = kk * 32 + g * 8 + t * 4 + (s >> 2), col = base + f * 16 + (s & 3) * 4;
-                const int at = row * (R * kEl) + (((col >> 3) ^ permute(row)) << 4) + (col & 7) * 2;
+                const int at = row * (R * 2) + (((col >> 3) ^ permute(row)) << 4) + (col & 7) * 2;
                 h[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AM_LDS i16x4 *)((AM_LDS char *)stage + at));
             }
             return __builtin_bit_cast(i32x4, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             const int row = kDeal > 1 ? base + (s >> 2) * (4 * kDeal) + f * 4 + (s & 3) : base + f * 16 + s;
-            return *reinterpret_cast<const i32x4 *>(stage + row * kStageBytes + (((kk * 4 + g) ^ permute(row)) << 4));
+            return *reinterpret_cast<const i32x4 *>(stage + row * (kStageK * 2) + (((kk * 4 + g) ^ permute(row)) << 4));
         }
     }
 };
 
-template <typename E, bool kMajorA, bool kMajorB, bool kDirect, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM *WN * 64, 2) void am_tile_kernel(AmProduct p)
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, int BM, int BN, int WM, int WN, bool kFar = false>
+__global__ __launch_bounds__(WM *WN * 64, BM *BN / (WM * WN) > 64 * 128 ? 1 : 2) void am_tile_kernel(AmProduct p)
 {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub alone
     constexpr int kWaves = WM * WN, TI = BM / WM / 16, TJ = BN / WN / 16;
     constexpr int kDeal = kMajorB ? 1 : TJ;
-    using SideA = AmSide<E, BM, kWaves, kMajorA, 1>;
-    using SideB = AmSide<E, BN, kWaves, kMajorB, kDeal>;
+    using SideA = AmSide<E, BM, kWaves, kMajorA, 1, kFar>;
+    using SideB = AmSide<E, BN, kWaves, kMajorB, kDeal, kFar>;
     // one object a stage, so the compiler knows that a fetch into one does not touch the other
     __shared__ __attribute__((aligned(1024))) char a0[SideA::kBytes], b0[SideB::kBytes], a1[SideA::kBytes], b1[SideB::kBytes];
 
@@ -344,7 +381,6 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void am_tile_kernel(AmProduct p)
     const int64_t i0 = static_cast<int64_t>(ti) * BM, j0 = static_cast<int64_t>(tj) * BN;
     const int wi = wave / WN * (BM / WM), wj = wave % WN * (BN / WN);
 
-    constexpr int kStageK = kStageBytes / sizeof(E);
     const int32_t stages = (p.inner + kStageK - 1) / kStageK;
     const int32_t s_first = static_cast<int32_t>(static_cast<int64_t>(stages) * blockIdx.y / p.splits);
     const int32_t s_last = static_cast<int32_t>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / p.splits);
@@ -352,111 +388,100 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void am_tile_kernel(AmProduct p)
     SideA sa;
     SideB sb;
     f32x4 acc[TI][TJ];
-    #pragma unroll
-    for (int f = 0; f < TI; f++)
-        #pragma unroll
-        for (int g = 0; g < TJ; g++) acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    am_each<TI>([&](auto f) { am_each<TJ>([&](auto g) { acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }); });
 
     // A stage is 2 TI steps of TJ products; step t has half t / TI of the
-    // stage's k and rows t % TI.  Fragments are read two steps ahead, also over
-    // the end of a stage: its last reads are done two steps before its last
-    // products, and there the waves meet, the stage after next is fetched into
-    // this one's place and the next one's first fragments are read.  The
+    // stage's k and rows t % TI.  Fragments are read kAhead steps ahead, also
+    // over the end of a stage: its last reads are done kAhead steps before its
+    // last products, and there the waves meet, the stage after next is fetched
+    // into this one's place and the next one's first fragments are read.  The
     // scheduling fences keep that order.
-    constexpr int kSteps = 2 * TI, kAhead = 2, kX = 4;   // kX divides kSteps: the next stage's first x are none of the last two
-    static_assert(TI >= 2 && kSteps % kX == 0, "");
+    using C = std::conditional_t<sizeof(E) == 1, bf16, E>;   // what the matrix cores multiply
+    constexpr int kSteps = 2 * TI, kAhead = 2, kX = 4;   // kX divides kSteps: the next stage's first x are none of the last ones
+    static_assert(TI >= kAhead && kSteps % kX == 0 && kAhead < kX, "");
     i32x4 x[kX], y[2][TJ];
-    const auto read_y = [&](const char *bs, int kk) {
-#pragma unroll
-        for (int g = 0; g < TJ; g++) y[kk][g] = sb.fragment(bs, wj, g, kk, lane);
+    const auto read_y = [&](const char *bs, auto kk) {
+        am_each<TJ>([&](auto g) { y[kk][g] = sb.fragment(bs, wj, g, kk, lane); });
     };
-    const auto read_x = [&](const char *as, int t) { x[t % kX] = sa.fragment(as, wi, t % TI, t / TI, lane); };
-    i32x4 y0[TJ], y1[TJ];   // 8 bits: y widened
-    const auto products = [&](int t) {
-        const int f = t % TI, kk = t / TI;
-        if constexpr (sizeof(E) == 1) {
-            // The 8-bit matrix instructions drop the low bits of products far below the largest one of
-            // their 128 (errors up to 2^-12 of it); as bf16 the products and their sums are kept in 32 bits
-            if (f == 0)
-#pragma unroll
-                for (int g = 0; g < TJ; g++) am_widen(y[kk][g], y0[g], y1[g]);
-            i32x4 x0, x1;
-            am_widen(x[t % kX], x0, x1);
-#pragma unroll
-            for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<bf16>(y0[g], x0, acc[f][g]);
-#pragma unroll
-            for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<bf16>(y1[g], x1, acc[f][g]);
-        } else {
-#pragma unroll
-            for (int g = 0; g < TJ; g++) acc[f][g] = am_mfma<E>(y[kk][g], x[t % kX], acc[f][g]);
-        }
-    };
+    const auto read_x = [&](const char *as, auto t) { x[t % kX] = sa.fragment(as, wi, t % TI, t / TI, lane); };
     const auto first_reads = [&](const char *as, const char *bs) {
-        read_y(bs, 0);
-#pragma unroll
-        for (int t = 0; t < kAhead; t++) read_x(as, t);
+        read_y(bs, std::integral_constant<int, 0>{});
+        am_each<kAhead>([&](auto t) { read_x(as, t); });
     };
-    // one stage; next(): what to do where the waves meet
-    const auto stage = [&](const char *as, const char *bs, auto next) {
-#pragma unroll
-        for (int t = 0; t < kSteps; t++) {
-            if (t == TI - kAhead) read_y(bs, 1);
-            if (t + kAhead < kSteps) read_x(as, t + kAhead);
-            if (t + kAhead == kSteps) next();
+    // one stage; half(): what to do after half of it, next(): where the waves
+    // meet, between(n): after the n-th product from there on
+    const auto stage = [&](const char *as, const char *bs, auto half, auto next, auto between) {
+        am_each<kSteps>([&](auto t) {
+            if constexpr (t == TI - kAhead) read_y(bs, std::integral_constant<int, 1>{});
+            if constexpr (t + kAhead < kSteps) read_x(as, std::integral_constant<int, t + kAhead>{});
+            if constexpr (t == TI) half();
+            if constexpr (t + kAhead == kSteps) next();
             __builtin_amdgcn_sched_barrier(0);
-            products(t);
+            am_each<TJ>([&](auto g) {
+                acc[t % TI][g] = am_mfma<C>(y[t / TI][g], x[t % kX], acc[t % TI][g]);
+                if constexpr (t + kAhead >= kSteps) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    between(std::integral_constant<int, (t + kAhead - kSteps) * TJ + g>{});
+                }
+            });
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
+    };
+    // the waves meet; fetches to LDS have landed (the barrier alone does not wait for those)
+    const auto meet = [] {
+        if constexpr (kDirect) __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
     };
 
     if constexpr (kDirect) {
         const int32_t tail = (p.inner % kStageK) * static_cast<int32_t>(sizeof(E));
         sa.init(p.a, wave, lane);
         sb.init(p.b, wave, lane);
-        const auto fetch = [&](char *as, char *bs, int32_t s) {
-            if (s >= s_last) return;
+        // The fetch of a stage: its descriptors, then its parts one by one.
+        __amdgpu_buffer_rsrc_t rsrc_a, rsrc_b;
+        const auto begin = [&](int32_t s) {
             if (s + 1 == stages && tail) {
                 sa.cut(tail, wave, lane);
                 sb.cut(tail, wave, lane);
             }
-            sa.fetch(p.a, i0, p.inner, s * kStageK, as, wave);
-            sb.fetch(p.b, j0, p.inner, s * kStageK, bs, wave);
+            const bool there = s >= s_first && s < s_last;
+            rsrc_a = sa.stage_rsrc(p.a, i0, p.inner, s * kStageK, there);
+            rsrc_b = sb.stage_rsrc(p.b, j0, p.inner, s * kStageK, there);
         };
-        // stages in pairs; of an odd number the first goes alone, through the second place
-        int32_t s = s_first;
-        if ((s_last - s_first) % 2) {
-            fetch(a1, b1, s);
-            fetch(a0, b0, s + 1);
-            __syncthreads();
-            first_reads(a1, b1);
-            stage(a1, b1, [&] {
-                __syncthreads();
-                first_reads(a0, b0);
-                fetch(a1, b1, s + 2);
-            });
-            s++;
-        } else {
-            fetch(a0, b0, s);
-            fetch(a1, b1, s + 1);
-            __syncthreads();
-            first_reads(a0, b0);
-        }
+        constexpr int kParts = SideA::kPerWave + SideB::kPerWave;
+        static_assert(kParts <= kAhead * TJ, "the fetches go between the products after the meeting");
+        const auto part = [&](char *as, char *bs, auto n) {
+            if constexpr (n < SideA::kPerWave) sa.fetch(rsrc_a, n, as, wave);
+            else if constexpr (n < kParts) sb.fetch(rsrc_b, n - SideA::kPerWave, bs, wave);
+        };
+        const auto whole = [&](char *as, char *bs, int32_t s) {
+            begin(s);
+            am_each<kParts>([&](auto n) { part(as, bs, n); });
+        };
+        const auto nothing = [] {};
+        // stages in pairs; an odd number begins with one of zeros
+        int32_t s = s_last - ((s_last - s_first + 1) & ~1);
+        whole(a0, b0, s);
+        whole(a1, b1, s + 1);
+        meet();
+        first_reads(a0, b0);
         for (; s < s_last; s += 2) {
-            stage(a0, b0, [&] {
-                __syncthreads();   // the next stage has landed, this one is read
+            stage(a0, b0, nothing, [&] {
+                meet();   // the next stage has landed, this one is read
                 first_reads(a1, b1);
-                fetch(a0, b0, s + 2);
-            });
-            stage(a1, b1, [&] {
-                __syncthreads();
+                begin(s + 2);
+            }, [&](auto n) { part(a0, b0, n); });
+            stage(a1, b1, nothing, [&] {
+                meet();
                 first_reads(a0, b0);
-                fetch(a1, b1, s + 3);
-            });
+                begin(s + 3);
+            }, [&](auto n) { part(a1, b1, n); });
         }
+        __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no fetch is under way when the workgroup ends
     } else {
-        i32x4 ra[SideA::kPerWave] = {}, rb[SideB::kPerWave] = {};
+        i32x4 ra[SideA::kLoads] = {}, rb[SideB::kLoads] = {};
         const auto load = [&](int32_t s) {
-            if (s >= s_last) return;
+            if (s < s_first || s >= s_last) return;
             sa.load(p.a, i0, p.inner, s * kStageK, ra, wave, lane);
             sb.load(p.b, j0, p.inner, s * kStageK, rb, wave, lane);
         };
@@ -464,61 +489,56 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void am_tile_kernel(AmProduct p)
             sa.put(ra, as, wave, lane);
             sb.put(rb, bs, wave, lane);
         };
-        int32_t s = s_first;
-        if ((s_last - s_first) % 2) {
-            load(s);
-            put(a1, b1);
-            __syncthreads();
-            load(s + 1);
-            first_reads(a1, b1);
-            stage(a1, b1, [] {});
-            put(a0, b0);
-            s++;
-        } else {
-            load(s);
-            put(a0, b0);
-        }
+        // the next stage goes to its place in the middle of this one, and the one after it on its way
+        int32_t s = s_last - ((s_last - s_first + 1) & ~1);
+        load(s);
+        put(a0, b0);
+        load(s + 1);
+        meet();
+        first_reads(a0, b0);
         for (; s < s_last; s += 2) {
-            __syncthreads();
-            load(s + 1);
-            first_reads(a0, b0);
-            stage(a0, b0, [] {});
-            put(a1, b1);
-            __syncthreads();
-            load(s + 2);
-            first_reads(a1, b1);
-            stage(a1, b1, [] {});
-            put(a0, b0);
+            stage(a0, b0, [&] {
+                put(a1, b1);
+                load(s + 2);
+            }, [&] {
+                meet();
+                first_reads(a1, b1);
+            }, [](auto) {});
+            stage(a1, b1, [&] {
+                put(a0, b0);
+                load(s + 3);
+            }, [&] {
+                meet();
+                first_reads(a0, b0);
+            }, [](auto) {});
         }
     }
 
     // a lane's runs of consecutive j: one of 4 * TJ, or TJ of 4
     constexpr int kRun = 4 * kDeal, kRuns = TJ / kDeal;
-    #pragma unroll
-    for (int t = 0; t < kRuns; t++) {
+    am_each<kRuns>([&](auto t) {
         const int64_t j = j0 + wj + (lane >> 4) * kRun + t * 16;
-        if (j >= p.b.extent) continue;
+        if (j >= p.b.extent) return;
         float b_scale[kRun], bias[kRun];
         if (p.splits == 1) am_columns(p, j, b_scale, bias);
-        #pragma unroll
-        for (int f = 0; f < TI; f++) {
+        am_each<TI>([&](auto f) {
             const int64_t i = i0 + wi + f * 16 + (lane & 15);
-            if (i >= p.a.extent) continue;
+            if (i >= p.a.extent) return;
             float v[kRun];
-            #pragma unroll
-            for (int d = 0; d < kDeal; d++)
-                #pragma unroll
-                for (int e = 0; e < 4; e++) v[d * 4 + e] = acc[f][t * kDeal + d][e];
+            am_each<kDeal>([&](auto d) {
+                const f32x4 a = acc[f][t * kDeal + d];
+                v[d * 4] = a[0], v[d * 4 + 1] = a[1], v[d * 4 + 2] = a[2], v[d * 4 + 3] = a[3];
+            });
             if (p.splits == 1) {
                 am_finish(p, i, j, v, b_scale, bias);
             } else {
                 float *o = p.partial + (static_cast<int64_t>(blockIdx.y) * p.a.extent + i) * p.b.extent + j;
-                #pragma unroll
+#pragma unroll
                 for (int e = 0; e < kRun; e++)
                     if (j + e < p.b.extent) o[e] = v[e];
             }
-        }
-    }
+        });
+    });
 #endif
 }
 
@@ -526,35 +546,56 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void am_tile_kernel(AmProduct p)
 // host side
 // --------------------------------------------------------------------------
 
-// 16-byte fetches: rows aligned, ending on 16 bytes, offsets inside a tile in 31 bits
+// offsets inside a tile of 256 rows stay in 31 bits
+inline bool am_near(const AmOperand &o) { return o.ld < (int64_t{1} << 22); }
+
+// 16-byte fetches: rows aligned and ending on 16 bytes
 inline bool am_direct(const AmOperand &o, bool major, int32_t inner, int el)
 {
     const int64_t row = static_cast<int64_t>(major ? o.extent : inner) * el;
-    return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && row % 16 == 0 && o.ld < (int64_t{1} << 22);
+    return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && row % 16 == 0 && am_near(o);
 }
 
 // sums the parts of a split product and finishes them (am_linear.hip)
 void am_launch_join(const AmProduct &p, hipStream_t st);
 
-template <typename E, bool kMajorA, bool kMajorB, bool kDirect, int BM, int BN, int WM, int WN>
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, int BM, int BN, int WM, int WN, bool kFar = false>
 void am_launch_tiles(const AmProduct &p, hipStream_t st)
 {
     const int64_t tiles = ((static_cast<int64_t>(p.a.extent) + BM - 1) / BM) * ((static_cast<int64_t>(p.b.extent) + BN - 1) / BN);
-    am_tile_kernel<E, kMajorA, kMajorB, kDirect, BM, BN, WM, WN>
+    am_tile_kernel<E, kMajorA, kMajorB, kDirect, BM, BN, WM, WN, kFar>
         <<<dim3(static_cast<unsigned>(tiles), p.splits), WM * WN * 64, 0, st>>>(p);
     if (p.splits > 1) am_launch_join(p, st);
 }
 
 constexpr int64_t kComputeUnits = 256;
 
-// Parts of k for a product without an epilogue: as many as fill the chip with
-// 64 x 64 tiles, of 4 stages at least.
-inline int32_t am_splits(int64_t rows, int64_t cols, int64_t inner)
+// Which tiles, and into how many parts k is split.
+struct AmPlan {
+    int32_t tile;     // 256, 128 or 64
+    int32_t splits;
+};
+
+inline int64_t am_tiles(int64_t rows, int64_t cols, int64_t t) { return ((rows + t - 1) / t) * ((cols + t - 1) / t); }
+
+// The largest tiles that give every second compute unit one; large tiles read
+// less LDS a product (256: 1.2 PFLOP/s over long k, 128: 0.7).  A product that
+// may be split (no epilogue, a workspace) also takes them where parts of at
+// least 16 stages fill the chip; the join of the parts moves 8 bytes a part and
+// value.  What is left gets 64 x 64 tiles, split down to 4 stages.
+inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split)
 {
-    const int64_t tiles = ((rows + 63) / 64) * ((cols + 63) / 64), stages = (inner + 63) / 64;
-    int64_t s = 2 * kComputeUnits / tiles;
+    const int64_t stages = (inner + kStageK - 1) / kStageK;
+    for (int32_t t = 256; t >= 128; t /= 2) {
+        const int64_t n = am_tiles(rows, cols, t);
+        if (n >= kComputeUnits / 2) return {t, 1};
+        const int64_t s = kComputeUnits / n;
+        if (may_split && s > 1 && s <= 16 && stages / s >= 16) return {t, static_cast<int32_t>(s)};
+    }
+    if (!may_split) return {64, 1};
+    int64_t s = 2 * kComputeUnits / am_tiles(rows, cols, 64);
     s = s < stages / 4 ? s : stages / 4;
-    return static_cast<int32_t>(s < 1 ? 1 : s > 64 ? 64 : s);
+    return {64, static_cast<int32_t>(s < 1 ? 1 : s > 64 ? 64 : s)};
 }
 
 inline int64_t am_partial_bytes(int64_t rows, int64_t cols, int32_t splits)
@@ -563,21 +604,18 @@ inline int64_t am_partial_bytes(int64_t rows, int64_t cols, int32_t splits)
 }
 
 template <typename E, bool kMajorA, bool kMajorB>
-void am_product(const AmProduct &p, hipStream_t st)
+void am_product(const AmProduct &p, int32_t tile, hipStream_t st)
 {
-    const auto tiles = [&](int64_t t) { return ((p.a.extent + t - 1) / t) * ((p.b.extent + t - 1) / t); };
-    if (am_direct(p.a, kMajorA, p.inner, sizeof(E)) && am_direct(p.b, kMajorB, p.inner, sizeof(E))) {
-        if (p.splits == 1 && tiles(256) >= kComputeUnits / 2)
-            am_launch_tiles<E, kMajorA, kMajorB, true, 256, 256, 2, 4>(p, st);
-        else if (p.splits == 1 && tiles(128) >= kComputeUnits / 2)
-            am_launch_tiles<E, kMajorA, kMajorB, true, 128, 128, 2, 2>(p, st);
-        else
-            am_launch_tiles<E, kMajorA, kMajorB, true, 64, 64, 2, 2>(p, st);
-    } else if (p.splits == 1 && tiles(128) >= kComputeUnits / 2) {
-        am_launch_tiles<E, kMajorA, kMajorB, false, 128, 128, 2, 2>(p, st);
-    } else {
-        am_launch_tiles<E, kMajorA, kMajorB, false, 64, 64, 2, 2>(p, st);
-    }
+    if constexpr (sizeof(E) == 2)
+        if (am_direct(p.a, kMajorA, p.inner, sizeof(E)) && am_direct(p.b, kMajorB, p.inner, sizeof(E))) {
+            if (tile == 256) am_launch_tiles<E, kMajorA, kMajorB, true, 256, 256, 2, 4>(p, st);
+            else if (tile == 128) am_launch_tiles<E, kMajorA, kMajorB, true, 128, 128, 2, 2>(p, st);
+            else am_launch_tiles<E, kMajorA, kMajorB, true, 64, 64, 2, 2>(p, st);
+            return;
+        }
+    if (!am_near(p.a) || !am_near(p.b)) am_launch_tiles<E, kMajorA, kMajorB, false, 64, 64, 2, 2, true>(p, st);
+    else if (tile >= 128) am_launch_tiles<E, kMajorA, kMajorB, false, 128, 128, 2, 2>(p, st);
+    else am_launch_tiles<E, kMajorA, kMajorB, false, 64, 64, 2, 2>(p, st);
 }
 
 }  // namespace wfd
