@@ -13,7 +13,9 @@ __device__ __forceinline__ float slope(float z, int32_t kind)
         const float s = __builtin_amdgcn_rcpf(1.0f + am_exp(-z));
         return s * (1.0f + z * (1.0f - s));
     }
-    return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * am_exp(-0.5f * z * z) * 0.39894228f;
+    float bell;
+    const float n = am_normal(z, bell);
+    return fmaf(z * 0.39894228f, bell, n);
 }
 
 // Sums the parts of a split product and finishes them.

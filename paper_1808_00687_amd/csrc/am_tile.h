@@ -3,25 +3,25 @@
 // with each operand stored k-contiguous (rows of k) or k-major (rows of i or
 // j, one row a k).
 //
-// A workgroup computes a BM x BN tile, stage by stage: a stage holds 64 values
-// of k for every row of the tile.  Two stages lie in LDS; the next one is fetched
-// while the matrix cores work on the present one.  The fetch goes straight from
-// memory to LDS (16 bytes a lane, no registers); operands that are not aligned to
-// 16 bytes, and 8-bit ones, go through registers.
+// A workgroup computes a BM x BN tile, stage by stage: a stage holds 64 or 128
+// bytes of k for every row of the tile.  Two to four stages lie in LDS: the later
+// ones are fetched while the matrix cores work on the present one.  The fetch goes
+// straight from memory to LDS (16 bytes a lane, no registers); operands that are
+// not aligned to 16 bytes go through registers.
 //
-// 8-bit operands are widened to bf16 on the way (each value exactly).  The
-// 8-bit matrix instructions would be twice as fast, but drop the low bits of
-// products far below the largest one of their 128 (errors up to 2^-12 of it); as
-// bf16 the products and their sums are kept in 32 bits.
+// 8-bit operands are widened to bf16 as they are read from LDS (each value
+// exactly).  The 8-bit matrix instructions would be twice as fast, but drop the
+// low bits of products far below the largest one of their 128 (errors up to
+// 2^-12 of it); as bf16 the products and their sums are kept in 32 bits.
 //
 // LDS layout.  A stage is a row of 16-byte chunks for each row of the operand
 // as stored; a chunk sits at its index XOR a function of the row, so that the
 // lanes of one read meet all banks.  The memory-to-LDS fetch writes lane after
 // lane, so the permutation is applied to the address that a lane reads.
-//   k-contiguous: a lane's fragment is one chunk (8 values of 16 bits) of its row
-//   k-major: a fragment is gathered by two transposing LDS reads; each takes 4
-//   rows (k) by 16 columns from a group of 16 lanes and hands every lane its
-//   column's 4 values
+//   k-contiguous: a lane's fragment is one chunk of its row
+//   k-major (16 bits): a fragment is gathered by two transposing LDS reads; each
+//   takes 4 rows (k) by 16 columns from a group of 16 lanes and hands every lane
+//   its column's 4 values
 // The order of k inside a fragment does not matter as long as both operands
 // have the same.
 //
@@ -56,7 +56,7 @@ __device__ __forceinline__ void am_each(F use)
     am_each<N>(use, std::make_integer_sequence<int, N>{});
 }
 
-constexpr int kStageK = 64;   // values of k in a stage
+
 
 struct AmOperand {
     const char *data;
@@ -77,7 +77,27 @@ struct AmProduct {
 
 __device__ __forceinline__ float am_silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + am_exp(-z)); }
 
-__device__ __forceinline__ float am_gelu(float z) { return 0.5f * z * (1.0f + erff(z * 0.70710678f)); }
+// The normal distribution's function at z and exp(-z^2 / 2), by Abramowitz and
+// Stegun's approximation 7.1.26 of erf (error below 1.5e-7): for x = |z| / sqrt 2,
+// 1 - erf(x) = (a1 t + ... + a5 t^5) exp(-x^2) with t = 1 / (1 + 0.3275911 x).
+// erff costs three times as much, more than the products of a short k.
+__device__ __forceinline__ float am_normal(float z, float &bell)
+{
+    const float x = fabsf(z) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    bell = __builtin_amdgcn_exp2f(x * x * -1.44269504f);
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float tail = 0.5f * p * t * bell;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+
+__device__ __forceinline__ float am_gelu(float z)
+{
+    float bell;
+    return z * am_normal(z, bell);
+}
 
 template <int N>
 __device__ __forceinline__ void am_activate(float (&v)[N], int32_t kind)
@@ -218,34 +238,37 @@ __device__ __forceinline__ void am_tile_of(uint32_t block, uint32_t rows, uint32
 
 constexpr int am_log2(int x) { return x <= 1 ? 0 : 1 + am_log2(x / 2); }
 
-// One operand's part of the tile kernel: R rows (i or j), kMajor its storage,
-// kDeal > 1: rows dealt to fragments so that a lane gets kDeal runs of 4 rows;
-// kFar: rows so far apart that offsets inside a tile pass 31 bits.
-template <typename E, int R, int kWaves, bool kMajor, int kDeal, bool kFar>
+// One operand's part of the tile kernel: R rows (i or j) of SB bytes a stage,
+// kMajor its storage, kDeal > 1: rows dealt to fragments so that a lane gets
+// kDeal runs of 4 rows; kFar: rows so far apart that offsets inside a tile pass
+// 31 bits.
+template <typename E, int R, int SB, int kWaves, bool kMajor, int kDeal, bool kFar>
 struct AmSide {
     static constexpr int kEl = sizeof(E);
-    static constexpr int kRowChunks = kMajor ? R / 8 : 8;   // of 8 values, in a row of LDS
-    static constexpr int kBytes = R * kStageK * 2;
-    static constexpr int kPerWave = R / 8 / kWaves;         // KiB of LDS a wave fills
-    static constexpr int kWide = 16 / kEl;                  // values of 16 bytes in memory
-    static constexpr int kLoads = kPerWave * 8 / kWide;     // 16-byte loads a lane, through registers
-    static_assert(R % (8 * kWaves) == 0 && (kEl == 2 || (!kMajor && kPerWave % 2 == 0)), "");
+    static constexpr int kWide = 16 / kEl;                       // values of a chunk
+    static constexpr int kRowChunks = kMajor ? R / kWide : SB / 16;
+    static constexpr int kBytes = R * SB;
+    static constexpr int kPerWave = kBytes / 1024 / kWaves;      // fetches of 1 KiB a wave
+    static constexpr int kHalves = SB / 64;                      // fragments along k
+    static_assert(kBytes % (1024 * kWaves) == 0 && (kEl == 2 || !kMajor) && (kHalves == 1 || kHalves == 2), "");
 
     // chunk permutation of a stored row
     __device__ static __forceinline__ int permute(int row)
     {
+        constexpr int kShift = 2 + am_log2(kDeal);
         if constexpr (kMajor) {
             // 16 lanes read 4 rows, 32 lanes 8: rows 0-3 and 8-11 (or 4 more), 32 bytes each
             if constexpr (kRowChunks >= 16) return ((row & 3) | ((row >> 3) & 1) << 2) << 1;
             else return (((row >> 1) & 1) | ((row >> 3) & 1) << 1) << 1;
-        } else if constexpr (kDeal > 1) {
-            return ((row >> 1) & 1) | ((row >> (2 + am_log2(kDeal))) & 3) << 1;
+        } else if constexpr (kHalves == 1) {
+            return (row >> kShift) & 3;   // 16 lanes read 16 rows: 4 neighbours, then every 4 * kDeal
         } else {
-            return (row >> 1) & 7;
+            return ((row >> 1) & 1) | ((row >> kShift) & 3) << 1;
         }
     }
 
     int32_t voff[kPerWave];      // direct: byte offset of each fetch from the stage's base
+    int32_t place[kMajor ? 1 : kHalves];   // of the lane's first fragment in a stage
 
     // the row as stored, and the chunk in it, that goes to a lane's place in LDS
     __device__ static __forceinline__ int row_of(int q, int wave, int lane) { return ((wave * kPerWave + q) * 64 + lane) / kRowChunks; }
@@ -297,16 +320,16 @@ struct AmSide {
 
     // Through registers, any alignment.  Values past k's end are zeros; rows
     // past the operand's end repeat the last one (their results are not stored).
-    __device__ __forceinline__ void load(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, i32x4 (&r)[kLoads], int wave, int lane)
+    __device__ __forceinline__ void load(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, i32x4 (&r)[kPerWave], int wave, int lane)
     {
         using Offset = std::conditional_t<kFar, int64_t, int32_t>;
         const AM_GLOBAL char *base = (const AM_GLOBAL char *)o.data + (kMajor ? k0 * o.ld + first * kEl : first * o.ld + static_cast<int64_t>(k0) * kEl);
         const int32_t rows_left = o.extent - static_cast<int32_t>(first), k_left = inner - k0;
 #pragma unroll
-        for (int q = 0; q < kLoads; q++) {
-            // row as stored and first value in it, from `base` on; 8 bits: 4 loads a row of 64 values
-            int32_t row = kEl == 2 ? row_of(q, wave, lane) : ((wave * kLoads + q) * 64 + lane) / 4;
-            const int32_t at = kEl == 2 ? chunk_of(q, wave, lane) * 8 : lane % 4 * 16;
+        for (int q = 0; q < kPerWave; q++) {
+            // row as stored and first value in it, from `base` on
+            int32_t row = row_of(q, wave, lane);
+            const int32_t at = chunk_of(q, wave, lane) * kWide;
             if constexpr (!kMajor) row = row < rows_left ? row : rows_left - 1;
             const int32_t along = (kMajor ? rows_left : k_left) - at;   // values left in the stored row
             const AM_GLOBAL char *p = base + (static_cast<Offset>(row) * static_cast<Offset>(o.ld) + at * kEl);
@@ -328,97 +351,150 @@ struct AmSide {
             r[q] = v;
         }
     }
-    __device__ __forceinline__ void put(const i32x4 (&r)[kLoads], char *stage, int wave, int lane)
+    __device__ __forceinline__ void put(const i32x4 (&r)[kPerWave], char *stage, int wave, int lane)
     {
 #pragma unroll
-        for (int q = 0; q < kLoads; q++) {
-            if constexpr (kEl == 2) {
-                *reinterpret_cast<i32x4 *>(stage + ((wave * kPerWave + q) * 64 + lane) * 16) = r[q];
-            } else {
-                const int row = ((wave * kLoads + q) * 64 + lane) / 4, c = lane % 4 * 2;
-                i32x4 lo, hi;
-                am_widen(r[q], lo, hi);
-                *reinterpret_cast<i32x4 *>(stage + row * (kStageK * 2) + ((c ^ permute(row)) << 4)) = lo;
-                *reinterpret_cast<i32x4 *>(stage + row * (kStageK * 2) + (((c + 1) ^ permute(row)) << 4)) = hi;
-            }
-        }
+        for (int q = 0; q < kPerWave; q++)
+            *reinterpret_cast<i32x4 *>(stage + ((wave * kPerWave + q) * 64 + lane) * 16) = r[q];
     }
 
-    // Fragment f (of the wave's rows from `base` on), half kk of a stage's k
-    __device__ __forceinline__ i32x4 fragment(const char *stage, int base, int f, int kk, int lane) const
+    // For the fragments of the wave's rows from `base` on.
+    __device__ __forceinline__ void init_places(int base, int lane)
     {
         const int g = lane >> 4, s = lane & 15;
         if constexpr (kMajor) {
-            i16x4 h[2];
-#pragma unroll
-            for (int t = 0; t < 2; t++) {
-                const int row = kk * 32 + g * 8 + t * 4 + (s >> 2), col = base + f * 16 + (s & 3) * 4;
-                const int at = row * (R * 2) + (((col >> 3) ^ permute(row)) << 4) + (col & 7) * 2;
-                h[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AM_LDS i16x4 *)((AM_LDS char *)stage + at));
-            }
-            return __builtin_bit_cast(i32x4, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+            const int row = g * 8 + (s >> 2);
+            place[0] = row * (R * 2) + (((base >> 3) ^ permute(row)) << 4) + (s & 3) * 8;
         } else {
-            const int row = kDeal > 1 ? base + (s >> 2) * (4 * kDeal) + f * 4 + (s & 3) : base + f * 16 + s;
-            return *reinterpret_cast<const i32x4 *>(stage + row * (kStageK * 2) + (((kk * 4 + g) ^ permute(row)) << 4));
+            const int row = base + (kDeal > 1 ? (s >> 2) * (4 * kDeal) + (s & 3) : s);
+#pragma unroll
+            for (int h = 0; h < kHalves; h++) place[h] = row * SB + (((h * 4 + g) ^ permute(row)) << 4);
+        }
+    }
+    // The compiler would keep a register for each fragment's place: they are
+    // taken anew in every stage instead.
+    __device__ __forceinline__ void renew()
+    {
+        __asm__ volatile("" : "+v"(place[0]));
+    }
+    // Fragment f in half h of a stage's k
+    template <int f, int h>
+    __device__ __forceinline__ i32x4 fragment(const char *stage) const
+    {
+        if constexpr (kMajor) {
+            i16x4 v[2];
+#pragma unroll
+            for (int t = 0; t < 2; t++)
+                v[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (AM_LDS i16x4 *)((AM_LDS char *)stage + (place[0] ^ f * 32) + (h * 32 + t * 4) * (R * 2)));
+            return __builtin_bit_cast(i32x4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            return *reinterpret_cast<const i32x4 *>(stage + place[h] + f * (kDeal > 1 ? 4 : 16) * SB);
         }
     }
 };
 
-template <typename E, bool kMajorA, bool kMajorB, bool kDirect, int BM, int BN, int WM, int WN, bool kFar = false>
-__global__ __launch_bounds__(WM *WN * 64, BM *BN / (WM * WN) > 64 * 128 ? 1 : 2) void am_tile_kernel(AmProduct p)
+// vmcnt(n): at most n of the wave's fetches and loads under way
+template <int n>
+__device__ __forceinline__ void am_wait_vm()
+{
+    __builtin_amdgcn_s_waitcnt((n & 15) | 7 << 4 | 15 << 8 | (n >> 4) << 14);
+}
+
+// kBuffers stages of SB bytes a row in LDS
+template <int BM_, int BN_, int WM_, int WN_, int SB_, int kBuffers_>
+struct AmShape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, SB = SB_, kBuffers = kBuffers_, kThreads = WM_ * WN_ * 64;
+};
+
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kFar = false>
+__global__ __launch_bounds__(S::kThreads, 2) void am_tile_kernel(AmProduct p)
 {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub alone
-    constexpr int kWaves = WM * WN, TI = BM / WM / 16, TJ = BN / WN / 16;
+    constexpr int BM = S::BM, BN = S::BN, WN = S::WN, SB = S::SB, kBuffers = S::kBuffers;
+    constexpr int kWaves = S::WM * WN, TI = BM / S::WM / 16, TJ = BN / WN / 16, kK = SB / static_cast<int>(sizeof(E));
     constexpr int kDeal = kMajorB ? 1 : TJ;
-    using SideA = AmSide<E, BM, kWaves, kMajorA, 1, kFar>;
-    using SideB = AmSide<E, BN, kWaves, kMajorB, kDeal, kFar>;
-    // one object a stage, so the compiler knows that a fetch into one does not touch the other
-    __shared__ __attribute__((aligned(1024))) char a0[SideA::kBytes], b0[SideB::kBytes], a1[SideA::kBytes], b1[SideB::kBytes];
+    using SideA = AmSide<E, BM, SB, kWaves, kMajorA, 1, kFar>;
+    using SideB = AmSide<E, BN, SB, kWaves, kMajorB, kDeal, kFar>;
+    // one object a stage, so the compiler knows that a fetch into one does not touch the others
+    __shared__ __attribute__((aligned(1024))) char a0[SideA::kBytes], a1[SideA::kBytes];
+    __shared__ __attribute__((aligned(1024))) char a2[kBuffers > 2 ? SideA::kBytes : 1], a3[kBuffers > 3 ? SideA::kBytes : 1];
+    __shared__ __attribute__((aligned(1024))) char b0[SideB::kBytes], b1[SideB::kBytes];
+    __shared__ __attribute__((aligned(1024))) char b2[kBuffers > 2 ? SideB::kBytes : 1], b3[kBuffers > 3 ? SideB::kBytes : 1];
+    const auto place_a = [&](auto n) -> char * {
+        if constexpr (n % kBuffers == 0) return a0;
+        else if constexpr (n % kBuffers == 1) return a1;
+        else if constexpr (n % kBuffers == 2) return a2;
+        else return a3;
+    };
+    const auto place_b = [&](auto n) -> char * {
+        if constexpr (n % kBuffers == 0) return b0;
+        else if constexpr (n % kBuffers == 1) return b1;
+        else if constexpr (n % kBuffers == 2) return b2;
+        else return b3;
+    };
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t ti, tj;
     am_tile_of(blockIdx.x, (p.a.extent + BM - 1) / BM, (p.b.extent + BN - 1) / BN, ti, tj);
     const int64_t i0 = static_cast<int64_t>(ti) * BM, j0 = static_cast<int64_t>(tj) * BN;
-    const int wi = wave / WN * (BM / WM), wj = wave % WN * (BN / WN);
+    const int wi = wave / WN * (BM / S::WM), wj = wave % WN * (BN / WN);
 
-    const int32_t stages = (p.inner + kStageK - 1) / kStageK;
+    const int32_t stages = (p.inner + kK - 1) / kK;
     const int32_t s_first = static_cast<int32_t>(static_cast<int64_t>(stages) * blockIdx.y / p.splits);
     const int32_t s_last = static_cast<int32_t>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / p.splits);
 
     SideA sa;
     SideB sb;
+    sa.init_places(wi, lane);
+    sb.init_places(wj, lane);
     f32x4 acc[TI][TJ];
     am_each<TI>([&](auto f) { am_each<TJ>([&](auto g) { acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }); });
 
-    // A stage is 2 TI steps of TJ products; step t has half t / TI of the
-    // stage's k and rows t % TI.  Fragments are read kAhead steps ahead, also
-    // over the end of a stage: its last reads are done kAhead steps before its
-    // last products, and there the waves meet, the stage after next is fetched
-    // into this one's place and the next one's first fragments are read.  The
-    // scheduling fences keep that order.
+    // A stage is kSteps steps of TJ products (8 bits: twice as many); step t has
+    // half t / TI of the stage's k and rows t % TI.  Fragments are read kAhead
+    // steps ahead, also over the end of a stage: its last reads are done kAhead
+    // steps before its last products, and there the waves meet, a later stage is
+    // fetched into this one's place and the next one's first fragments are read.
+    // The scheduling fences keep that order.
     using C = std::conditional_t<sizeof(E) == 1, bf16, E>;   // what the matrix cores multiply
-    constexpr int kSteps = 2 * TI, kAhead = 2, kX = 4;   // kX divides kSteps: the next stage's first x are none of the last ones
-    static_assert(TI >= kAhead && kSteps % kX == 0 && kAhead < kX, "");
-    i32x4 x[kX], y[2][TJ];
-    const auto read_y = [&](const char *bs, auto kk) {
-        am_each<TJ>([&](auto g) { y[kk][g] = sb.fragment(bs, wj, g, kk, lane); });
+    constexpr int kHalves = SB / 64, kSteps = kHalves * TI, kAhead = 2, kX = 4;
+    // kX divides kSteps: the next stage's first x are none of the last ones
+    static_assert(kSteps % kX == 0 && 2 * kAhead <= kX && kAhead <= TI, "");
+    i32x4 x[kX], y[2][TJ], y_lo[TJ], y_hi[TJ];
+    // n: which stage, in turn; its half h has y in y[(n * kHalves + h) % 2]
+    const auto read_y = [&](auto n, auto h) {
+        am_each<TJ>([&](auto g) { y[(n * kHalves + h) % 2][g] = sb.template fragment<g, h % kHalves>(place_b(n)); });
     };
-    const auto read_x = [&](const char *as, auto t) { x[t % kX] = sa.fragment(as, wi, t % TI, t / TI, lane); };
-    const auto first_reads = [&](const char *as, const char *bs) {
-        read_y(bs, std::integral_constant<int, 0>{});
-        am_each<kAhead>([&](auto t) { read_x(as, t); });
+    const auto read_x = [&](auto n, auto t) { x[t % kX] = sa.template fragment<t % TI, t / TI>(place_a(n)); };
+    const auto first_reads = [&](auto n) {
+        sa.renew();
+        sb.renew();
+        read_y(n, std::integral_constant<int, 0>{});
+        am_each<kAhead>([&](auto t) { read_x(n, t); });
     };
-    // one stage; half(): what to do after half of it, next(): where the waves
-    // meet, between(n): after the n-th product from there on
-    const auto stage = [&](const char *as, const char *bs, auto half, auto next, auto between) {
+    // half(): what to do after half of a stage, next(): where the waves meet,
+    // between(m): after the m-th products from there on
+    const auto stage = [&](auto n, auto half, auto next, auto between) {
         am_each<kSteps>([&](auto t) {
-            if constexpr (t == TI - kAhead) read_y(bs, std::integral_constant<int, 1>{});
-            if constexpr (t + kAhead < kSteps) read_x(as, std::integral_constant<int, t + kAhead>{});
-            if constexpr (t == TI) half();
+            if constexpr (kHalves == 2 && t == TI - kAhead) read_y(n, std::integral_constant<int, 1>{});
+            if constexpr (t + kAhead < kSteps) read_x(n, std::integral_constant<int, t + kAhead>{});
+            if constexpr (t == kSteps / 2) half();
             if constexpr (t + kAhead == kSteps) next();
             __builtin_amdgcn_sched_barrier(0);
+            constexpr int f = t % TI, in = (n * kHalves + t / TI) % 2;
+            i32x4 x_lo, x_hi;
+            if constexpr (sizeof(E) == 1) {
+                if constexpr (f == 0) am_each<TJ>([&](auto g) { am_widen(y[in][g], y_lo[g], y_hi[g]); });
+                am_widen(x[t % kX], x_lo, x_hi);
+            }
             am_each<TJ>([&](auto g) {
-                acc[t % TI][g] = am_mfma<C>(y[t / TI][g], x[t % kX], acc[t % TI][g]);
+                if constexpr (sizeof(E) == 1) {
+                    acc[f][g] = am_mfma<C>(y_lo[g], x_lo, acc[f][g]);
+                    acc[f][g] = am_mfma<C>(y_hi[g], x_hi, acc[f][g]);
+                } else {
+                    acc[f][g] = am_mfma<C>(y[in][g], x[t % kX], acc[f][g]);
+                }
                 if constexpr (t + kAhead >= kSteps) {
                     __builtin_amdgcn_sched_barrier(0);
                     between(std::integral_constant<int, (t + kAhead - kSteps) * TJ + g>{});
@@ -427,91 +503,99 @@ __global__ __launch_bounds__(WM *WN * 64, BM *BN / (WM * WN) > 64 * 128 ? 1 : 2)
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    // the waves meet; fetches to LDS have landed (the barrier alone does not wait for those)
-    const auto meet = [] {
-        if constexpr (kDirect) __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr int kPeriod = kBuffers % 2 ? 2 * kBuffers : kBuffers;   // stages until places and y repeat
+    // go(n) does a stage and says whether another one follows.  With k-major
+    // operands the loop is left only after whole periods (the stages past the end
+    // are zeros): every exit more costs the compiler registers, and there it
+    // runs out of them.
+    int32_t s = s_first;
+    const auto all = [&](auto go) {
+        [&]<int... n>(std::integer_sequence<int, n...>) {
+            if constexpr (kMajorB) {
+                do {
+                    (go(std::integral_constant<int, n>{}), ...);
+                } while (s < s_last);
+            } else {
+                while ((go(std::integral_constant<int, n>{}) && ...)) {
+                }
+            }
+        }(std::make_integer_sequence<int, kPeriod>{});
     };
 
     if constexpr (kDirect) {
-        const int32_t tail = (p.inner % kStageK) * static_cast<int32_t>(sizeof(E));
+        const int32_t tail = (p.inner % kK) * static_cast<int32_t>(sizeof(E));
         sa.init(p.a, wave, lane);
         sb.init(p.b, wave, lane);
-        // The fetch of a stage: its descriptors, then its parts one by one.
+        // The fetch of a stage: its descriptors, then its parts one by one.  A
+        // stage that is not there is fetched from empty ranges, so that the
+        // number of fetches under way is always known.
         __amdgpu_buffer_rsrc_t rsrc_a, rsrc_b;
         const auto begin = [&](int32_t s) {
             if (s + 1 == stages && tail) {
                 sa.cut(tail, wave, lane);
                 sb.cut(tail, wave, lane);
             }
-            const bool there = s >= s_first && s < s_last;
-            rsrc_a = sa.stage_rsrc(p.a, i0, p.inner, s * kStageK, there);
-            rsrc_b = sb.stage_rsrc(p.b, j0, p.inner, s * kStageK, there);
+            rsrc_a = sa.stage_rsrc(p.a, i0, p.inner, s * kK, s < s_last);
+            rsrc_b = sb.stage_rsrc(p.b, j0, p.inner, s * kK, s < s_last);
         };
-        constexpr int kParts = SideA::kPerWave + SideB::kPerWave;
-        static_assert(kParts <= kAhead * TJ, "the fetches go between the products after the meeting");
-        const auto part = [&](char *as, char *bs, auto n) {
-            if constexpr (n < SideA::kPerWave) sa.fetch(rsrc_a, n, as, wave);
-            else if constexpr (n < kParts) sb.fetch(rsrc_b, n - SideA::kPerWave, bs, wave);
+        constexpr int kParts = SideA::kPerWave + SideB::kPerWave, kEach = (kParts + kAhead * TJ - 1) / (kAhead * TJ);
+        const auto part = [&](auto n, auto m) {
+            if constexpr (m < SideA::kPerWave) sa.fetch(rsrc_a, m, place_a(n), wave);
+            else if constexpr (m < kParts) sb.fetch(rsrc_b, m - SideA::kPerWave, place_b(n), wave);
         };
-        const auto whole = [&](char *as, char *bs, int32_t s) {
-            begin(s);
-            am_each<kParts>([&](auto n) { part(as, bs, n); });
-        };
-        const auto nothing = [] {};
-        // stages in pairs; an odd number begins with one of zeros
-        int32_t s = s_last - ((s_last - s_first + 1) & ~1);
-        whole(a0, b0, s);
-        whole(a1, b1, s + 1);
-        meet();
-        first_reads(a0, b0);
-        for (; s < s_last; s += 2) {
-            stage(a0, b0, nothing, [&] {
-                meet();   // the next stage has landed, this one is read
-                first_reads(a1, b1);
-                begin(s + 2);
-            }, [&](auto n) { part(a0, b0, n); });
-            stage(a1, b1, nothing, [&] {
-                meet();
-                first_reads(a0, b0);
-                begin(s + 3);
-            }, [&](auto n) { part(a1, b1, n); });
-        }
-        __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no fetch is under way when the workgroup ends
+        am_each<kBuffers>([&](auto n) {
+            begin(s + n);
+            am_each<kParts>([&](auto m) { part(n, m); });
+        });
+        am_wait_vm<(kBuffers - 1) * kParts>();
+        __syncthreads();
+        first_reads(first);
+        if (s < s_last)
+            all([&](auto n) {
+                stage(n, [] {}, [&] {
+                    // the waves meet: the next stage has landed, later ones may be on their way
+                    am_wait_vm<(kBuffers - 2) * kParts>();
+                    __syncthreads();
+                    first_reads(std::integral_constant<int, n + 1>{});
+                    begin(s + kBuffers);
+                }, [&](auto m) { am_each<kEach>([&](auto e) { part(n, std::integral_constant<int, m * kEach + e>{}); }); });
+                return ++s < s_last;
+            });
+        am_wait_vm<0>();   // no fetch is under way when the workgroup ends
     } else {
-        i32x4 ra[SideA::kLoads] = {}, rb[SideB::kLoads] = {};
+        i32x4 ra[SideA::kPerWave], rb[SideB::kPerWave];
         const auto load = [&](int32_t s) {
-            if (s < s_first || s >= s_last) return;
-            sa.load(p.a, i0, p.inner, s * kStageK, ra, wave, lane);
-            sb.load(p.b, j0, p.inner, s * kStageK, rb, wave, lane);
+            if (s >= s_last) {
+                am_each<SideA::kPerWave>([&](auto q) { ra[q] = i32x4{0, 0, 0, 0}; });
+                am_each<SideB::kPerWave>([&](auto q) { rb[q] = i32x4{0, 0, 0, 0}; });
+                return;
+            }
+            sa.load(p.a, i0, p.inner, s * kK, ra, wave, lane);
+            sb.load(p.b, j0, p.inner, s * kK, rb, wave, lane);
         };
-        const auto put = [&](char *as, char *bs) {
-            sa.put(ra, as, wave, lane);
-            sb.put(rb, bs, wave, lane);
+        const auto put = [&](auto n) {
+            sa.put(ra, place_a(n), wave, lane);
+            sb.put(rb, place_b(n), wave, lane);
         };
-        // the next stage goes to its place in the middle of this one, and the one after it on its way
-        int32_t s = s_last - ((s_last - s_first + 1) & ~1);
         load(s);
-        put(a0, b0);
+        put(first);
         load(s + 1);
-        meet();
-        first_reads(a0, b0);
-        for (; s < s_last; s += 2) {
-            stage(a0, b0, [&] {
-                put(a1, b1);
-                load(s + 2);
-            }, [&] {
-                meet();
-                first_reads(a1, b1);
-            }, [](auto) {});
-            stage(a1, b1, [&] {
-                put(a0, b0);
-                load(s + 3);
-            }, [&] {
-                meet();
-                first_reads(a0, b0);
-            }, [](auto) {});
-        }
+        __syncthreads();
+        first_reads(first);
+        if (s < s_last)
+            all([&](auto n) {
+                // the next stage goes to its place in the middle of this one, and the one after it on its way
+                constexpr std::integral_constant<int, n + 1> next{};
+                stage(n, [&] {
+                    put(next);
+                    load(s + 2);
+                }, [&] {
+                    __syncthreads();
+                    first_reads(next);
+                }, [](auto) {});
+                return ++s < s_last;
+            });
     }
 
     // a lane's runs of consecutive j: one of 4 * TJ, or TJ of 4
@@ -556,17 +640,26 @@ inline bool am_direct(const AmOperand &o, bool major, int32_t inner, int el)
     return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && row % 16 == 0 && am_near(o);
 }
 
+inline int64_t am_tiles(int64_t rows, int64_t cols, int64_t m, int64_t n) { return ((rows + m - 1) / m) * ((cols + n - 1) / n); }
+
 // sums the parts of a split product and finishes them (am_linear.hip)
 void am_launch_join(const AmProduct &p, hipStream_t st);
 
-template <typename E, bool kMajorA, bool kMajorB, bool kDirect, int BM, int BN, int WM, int WN, bool kFar = false>
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kFar = false>
 void am_launch_tiles(const AmProduct &p, hipStream_t st)
 {
-    const int64_t tiles = ((static_cast<int64_t>(p.a.extent) + BM - 1) / BM) * ((static_cast<int64_t>(p.b.extent) + BN - 1) / BN);
-    am_tile_kernel<E, kMajorA, kMajorB, kDirect, BM, BN, WM, WN, kFar>
-        <<<dim3(static_cast<unsigned>(tiles), p.splits), WM * WN * 64, 0, st>>>(p);
+    const int64_t tiles = am_tiles(p.a.extent, p.b.extent, S::BM, S::BN);
+    am_tile_kernel<E, kMajorA, kMajorB, kDirect, S, kFar><<<dim3(static_cast<unsigned>(tiles), p.splits), S::kThreads, 0, st>>>(p);
     if (p.splits > 1) am_launch_join(p, st);
 }
+
+using AmLarge = AmShape<256, 256, 2, 4, 128, 2>;
+using AmLarge8 = AmShape<256, 128, 2, 2, 64, 3>;   // two workgroups a CU
+using AmMedium = AmShape<128, 128, 2, 2, 64, 3>;
+using AmMediumMajor = AmShape<128, 128, 2, 2, 64, 4>;
+using AmSmall = AmShape<64, 64, 1, 4, 128, 4>;
+using AmMediumStaged = AmShape<128, 128, 2, 2, 64, 2>;
+using AmSmallStaged = AmShape<64, 64, 1, 4, 128, 2>;
 
 constexpr int64_t kComputeUnits = 256;
 
@@ -576,24 +669,18 @@ struct AmPlan {
     int32_t splits;
 };
 
-inline int64_t am_tiles(int64_t rows, int64_t cols, int64_t t) { return ((rows + t - 1) / t) * ((cols + t - 1) / t); }
 
-// The largest tiles that give every second compute unit one; large tiles read
-// less LDS a product (256: 1.2 PFLOP/s over long k, 128: 0.7).  A product that
-// may be split (no epilogue, a workspace) also takes them where parts of at
-// least 16 stages fill the chip; the join of the parts moves 8 bytes a part and
-// value.  What is left gets 64 x 64 tiles, split down to 4 stages.
 inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split)
 {
-    const int64_t stages = (inner + kStageK - 1) / kStageK;
+    const int64_t stages = (inner + 63) / 64;
     for (int32_t t = 256; t >= 128; t /= 2) {
-        const int64_t n = am_tiles(rows, cols, t);
+        const int64_t n = am_tiles(rows, cols, t, t);
         if (n >= kComputeUnits / 2) return {t, 1};
         const int64_t s = kComputeUnits / n;
         if (may_split && s > 1 && s <= 16 && stages / s >= 16) return {t, static_cast<int32_t>(s)};
     }
     if (!may_split) return {64, 1};
-    int64_t s = 2 * kComputeUnits / am_tiles(rows, cols, 64);
+    int64_t s = 2 * kComputeUnits / am_tiles(rows, cols, 64, 64);
     s = s < stages / 4 ? s : stages / 4;
     return {64, static_cast<int32_t>(s < 1 ? 1 : s > 64 ? 64 : s)};
 }
@@ -606,16 +693,17 @@ inline int64_t am_partial_bytes(int64_t rows, int64_t cols, int32_t splits)
 template <typename E, bool kMajorA, bool kMajorB>
 void am_product(const AmProduct &p, int32_t tile, hipStream_t st)
 {
-    if constexpr (sizeof(E) == 2)
-        if (am_direct(p.a, kMajorA, p.inner, sizeof(E)) && am_direct(p.b, kMajorB, p.inner, sizeof(E))) {
-            if (tile == 256) am_launch_tiles<E, kMajorA, kMajorB, true, 256, 256, 2, 4>(p, st);
-            else if (tile == 128) am_launch_tiles<E, kMajorA, kMajorB, true, 128, 128, 2, 2>(p, st);
-            else am_launch_tiles<E, kMajorA, kMajorB, true, 64, 64, 2, 2>(p, st);
-            return;
-        }
-    if (!am_near(p.a) || !am_near(p.b)) am_launch_tiles<E, kMajorA, kMajorB, false, 64, 64, 2, 2, true>(p, st);
-    else if (tile >= 128) am_launch_tiles<E, kMajorA, kMajorB, false, 128, 128, 2, 2>(p, st);
-    else am_launch_tiles<E, kMajorA, kMajorB, false, 64, 64, 2, 2>(p, st);
+    if (am_direct(p.a, kMajorA, p.inner, sizeof(E)) && am_direct(p.b, kMajorB, p.inner, sizeof(E))) {
+        if (tile == 256) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<sizeof(E) == 1, AmLarge8, AmLarge>>(p, st);
+        else if (tile == 128) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<kMajorB, AmMediumMajor, AmMedium>>(p, st);
+        else am_launch_tiles<E, kMajorA, kMajorB, true, AmSmall>(p, st);
+    } else if (!am_near(p.a) || !am_near(p.b)) {
+        am_launch_tiles<E, kMajorA, kMajorB, false, AmSmallStaged, true>(p, st);
+    } else if (tile >= 128) {
+        am_launch_tiles<E, kMajorA, kMajorB, false, AmMediumStaged>(p, st);
+    } else {
+        am_launch_tiles<E, kMajorA, kMajorB, false, AmSmallStaged>(p, st);
+    }
 }
 
 }  // namespace wfd
