@@ -7,9 +7,10 @@ the library's HIP kernels.  Operands are torch tensors on one GPU.  A matrix
 is two-dimensional; its rows may lie any distance apart (an input whose
 columns are not adjacent, or whose rows overlap, is copied first; an output
 like that is refused).  Vectors (bias, gain, scales, weights) are float32.
-The calls only enqueue, on ``stream`` or else torch's current stream, and
-take their results from torch's allocator on that stream (none where ``out``
-is given), so they can be captured into a graph.  Arguments that the library
+The calls only enqueue, on the ``stream`` that each takes by name (a torch
+stream or a raw handle) or else torch's current stream, and take their results
+from torch's allocator on that stream (none where ``out`` is given), so they
+can be captured into a graph.  Arguments that the library
 refuses raise WfstError (WFST_EINVAL) with its message.
 """
 from __future__ import annotations
@@ -87,8 +88,13 @@ for _n in ("linear_backward", "norm_backward"):
     _f.restype = C.c_int
 
 
-def _matrix(t: torch.Tensor, name: str, device: int) -> tuple:
-    """A tensor as a wfst_matrix; an output, or an input that is laid out as one."""
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_DENSE = torch.contiguous_format
+
+
+def _matrix(t: torch.Tensor, name: str, device: int, keep: Optional[list] = None) -> tuple:
+    """A tensor as a wfst_matrix.  An input (``keep`` given) that is not laid
+    out as one is copied, and the copy kept until the call is made."""
     code = _TYPES.get(t.dtype)
     if code is None:
         raise TypeError("%s: type %s is not taken" % (name, t.dtype))
@@ -99,17 +105,12 @@ def _matrix(t: torch.Tensor, name: str, device: int) -> tuple:
     if rows <= 1:
         step = cols
     if (inner != 1 and cols > 1) or step < cols:
-        raise ValueError("%s must have adjacent columns and rows that do not overlap" % name)
+        if keep is None:
+            raise ValueError("%s must have adjacent columns and rows that do not overlap" % name)
+        t = t.contiguous()
+        keep.append(t)
+        step = cols
     return t.data_ptr(), rows, cols, step, code, 0
-
-
-def _input(t: torch.Tensor, name: str, device: int, keep: list) -> tuple:
-    if t.dim() == 2 and t.numel():
-        step, inner = t.stride()
-        if (inner != 1 and t.shape[1] > 1) or (step < t.shape[1] and t.shape[0] > 1):
-            t = t.contiguous()
-            keep.append(t)
-    return _matrix(t, name, device)
 
 
 def _vector(t: Optional[torch.Tensor], name: str, n: int, device: int, dtype=torch.float32) -> int:
@@ -127,29 +128,35 @@ def _device(t: torch.Tensor, name: str) -> int:
 
 
 class _On:
-    """The device, and the stream whose allocator and queue a call uses."""
+    """Inside, the operands' device and the given stream are torch's current ones."""
 
     def __init__(self, device: int, stream):
-        self.device, self.stream = device, stream
-        self.guards: list = []
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=device)
+        self.guards = [torch.cuda.device(device)] + ([] if stream is None else [torch.cuda.stream(stream)])
 
-    def __enter__(self) -> int:
-        if self.device != torch.cuda.current_device():
-            g = torch.cuda.device(self.device)
+    def __enter__(self):
+        for g in self.guards:
             g.__enter__()
-            self.guards.append(g)
-        if self.stream is not None:
-            s = self.stream
-            if not isinstance(s, torch.cuda.Stream):
-                s = torch.cuda.ExternalStream(int(s), device=self.device)
-            g = torch.cuda.stream(s)
-            g.__enter__()
-            self.guards.append(g)
-        return torch._C._cuda_getCurrentRawStream(self.device)
 
     def __exit__(self, *exc):
-        while self.guards:
-            self.guards.pop().__exit__(*exc)
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+
+
+def _here(f):
+    """f, which works on the current device and stream, with a ``stream``
+    argument and on the device of its first argument."""
+    def call(first, *args, stream=None, **kw):
+        if stream is None and (not isinstance(first, torch.Tensor) or not first.is_cuda
+                               or first.get_device() == torch._C._cuda_getDevice()):
+            return f(first, *args, **kw)
+        with _On(_device(first, "the first operand"), stream):
+            return f(first, *args, **kw)
+
+    call.__name__, call.__qualname__, call.__doc__ = f.__name__, f.__qualname__, f.__doc__
+    call.__wrapped__ = f
+    return call
 
 
 def _call(name: str, packed: bytes, stream: int) -> None:
@@ -172,63 +179,64 @@ def _activation(name: str) -> int:
     return ACTIVATIONS[name]
 
 
+@_here
 def wfst_am_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
                    activation: str = "none", residual: Optional[torch.Tensor] = None,
                    x_scale: Optional[torch.Tensor] = None, w_scale: Optional[torch.Tensor] = None,
                    pre: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                   out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+                   out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """act(x w^T [* x_scale w_scale] + bias) + residual: x [M x K], w [N x K]
     -> [M x N] (wfst_am_linear).  ``out_dtype``: that of ``out``, else the
     residual's, else x's (bfloat16 for 8-bit x).  ``pre`` receives the value
     before the activation, for the gradient; ``residual`` may be ``out``."""
     d, keep = _device(x, "x"), []
-    with _On(d, stream) as st:
-        mx, mw = _input(x, "x", d, keep), _input(w, "w", d, keep)
-        if out is None:
-            dt = out_dtype or (residual.dtype if residual is not None else
-                               torch.bfloat16 if x.dtype == torch.float8_e4m3fn else x.dtype)
-            out = torch.empty((mx[1], mw[1]), dtype=dt, device=x.device)
-        elif out_dtype is not None and out_dtype != out.dtype:
-            raise ValueError("out_dtype differs from out's")
-        _call("wfst_am_linear", _PACK["linear"].pack(
-            *mx, *mw, *(_NONE if residual is None else _input(residual, "residual", d, keep)),
-            *(_NONE if pre is None else _matrix(pre, "pre", d)), *_matrix(out, "out", d),
-            _vector(x_scale, "x_scale", mx[1], d), _vector(w_scale, "w_scale", mw[1], d),
-            _vector(bias, "bias", mw[1], d), _activation(activation), 0), st)
+    mx, mw = _matrix(x, "x", d, keep), _matrix(w, "w", d, keep)
+    if out is None:
+        dt = out_dtype or (residual.dtype if residual is not None else
+                           torch.bfloat16 if x.dtype == torch.float8_e4m3fn else x.dtype)
+        out = x.new_empty((mx[1], mw[1]), dtype=dt)
+    elif out_dtype is not None and out_dtype != out.dtype:
+        raise ValueError("out_dtype differs from out's")
+    _call("wfst_am_linear", _PACK["linear"].pack(
+        *mx, *mw, *(_NONE if residual is None else _matrix(residual, "residual", d, keep)),
+        *(_NONE if pre is None else _matrix(pre, "pre", d)), *_matrix(out, "out", d),
+        _vector(x_scale, "x_scale", mx[1], d), _vector(w_scale, "w_scale", mw[1], d),
+        _vector(bias, "bias", mw[1], d), _activation(activation), 0), _raw_stream(d))
     return out
 
 
+@_here
 def wfst_am_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[torch.Tensor], *,
                             activation: str = "none", pre: Optional[torch.Tensor] = None,
-                            bias_gradient: bool = True, weight_dtype: Optional[torch.dtype] = None, stream=None
+                            bias_gradient: bool = True, weight_dtype: Optional[torch.dtype] = None
                             ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
     """(dx, dw, dbias) of wfst_am_linear with a 16-bit x (the residual's
     gradient is dy).  ``w`` None leaves out dx, ``x`` None dw.
     ``weight_dtype``: dw's type, dy's by default."""
     d, keep = _device(dy, "dy"), []
     act = _activation(activation)
-    with _On(d, stream) as st:
-        mdy = _input(dy, "dy", d, keep)
-        if act and pre is None:
-            raise ValueError("the activation's gradient needs pre")
-        mpre = _input(pre, "pre", d, keep) if act else _NONE
-        mx = _NONE if x is None else _input(x, "x", d, keep)
-        mw = _NONE if w is None else _input(w, "w", d, keep)
-        dx = None if w is None else torch.empty((mdy[1], mw[2]), dtype=dy.dtype, device=dy.device)
-        dw = None if x is None else torch.empty((mdy[2], mx[2]), dtype=weight_dtype or dy.dtype, device=dy.device)
-        db = torch.empty(mdy[2], dtype=torch.float32, device=dy.device) if bias_gradient else None
-        head = (*mdy, *mpre, *mx, *mw, *(_NONE if dx is None else _matrix(dx, "dx", d)),
-                *(_NONE if dw is None else _matrix(dw, "dw", d)), 0 if db is None else db.data_ptr())
-        pack = _PACK["linear_backward"].pack
-        need = _bytes_for("wfst_am_linear_backward_workspace", pack(*head, 0, 0, act, 0))
-        work = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
-        _call("wfst_am_linear_backward", pack(*head, work.data_ptr() if need else 0, need, act, 0), st)
+    mdy = _matrix(dy, "dy", d, keep)
+    if act and pre is None:
+        raise ValueError("the activation's gradient needs pre")
+    mpre = _matrix(pre, "pre", d, keep) if act else _NONE
+    mx = _NONE if x is None else _matrix(x, "x", d, keep)
+    mw = _NONE if w is None else _matrix(w, "w", d, keep)
+    dx = None if w is None else dy.new_empty((mdy[1], mw[2]))
+    dw = None if x is None else dy.new_empty((mdy[2], mx[2]), dtype=weight_dtype or dy.dtype)
+    db = dy.new_empty(mdy[2], dtype=torch.float32) if bias_gradient else None
+    head = (*mdy, *mpre, *mx, *mw, *(_NONE if dx is None else _matrix(dx, "dx", d)),
+            *(_NONE if dw is None else _matrix(dw, "dw", d)), 0 if db is None else db.data_ptr())
+    pack = _PACK["linear_backward"].pack
+    need = _bytes_for("wfst_am_linear_backward_workspace", pack(*head, 0, 0, act, 0))
+    work = dy.new_empty(need, dtype=torch.uint8) if need else None
+    _call("wfst_am_linear_backward", pack(*head, work.data_ptr() if need else 0, need, act, 0), _raw_stream(d))
     return dx, dw, db
 
 
+@_here
 def wfst_am_norm(x: torch.Tensor, gain: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None,
                  eps: float = 1e-6, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
-                 sum_out: Optional[torch.Tensor] = None, stream=None
+                 sum_out: Optional[torch.Tensor] = None
                  ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
     """(y, y_scale, sum): the root-mean-square norm of x + residual times
     ``gain`` (wfst_am_norm).  With ``out_dtype`` torch.float8_e4m3fn, y_scale
@@ -236,91 +244,90 @@ def wfst_am_norm(x: torch.Tensor, gain: Optional[torch.Tensor] = None, *, residu
     (None without a residual), in ``sum_out`` where given, which may be x or
     residual."""
     d, keep = _device(x, "x"), []
-    with _On(d, stream) as st:
-        mx = _input(x, "x", d, keep)
-        mr = _NONE if residual is None else _input(residual, "residual", d, keep)
-        if out is None:
-            out = torch.empty((mx[1], mx[2]), dtype=out_dtype or x.dtype, device=x.device)
-        elif out_dtype is not None and out_dtype != out.dtype:
-            raise ValueError("out_dtype differs from out's")
-        if sum_out is None and residual is not None:
-            sum_out = torch.empty((mx[1], mx[2]), dtype=x.dtype, device=x.device)
-        scale = torch.empty(mx[1], dtype=torch.float32, device=x.device) if out.dtype == torch.float8_e4m3fn else None
-        _call("wfst_am_norm", _PACK["norm"].pack(
-            *mx, *mr, *(_NONE if sum_out is None else _matrix(sum_out, "sum_out", d)), *_matrix(out, "out", d),
-            _vector(gain, "gain", mx[2], d), 0 if scale is None else scale.data_ptr(), eps, 0), st)
+    mx = _matrix(x, "x", d, keep)
+    mr = _NONE if residual is None else _matrix(residual, "residual", d, keep)
+    if out is None:
+        out = torch.empty_like(x, dtype=out_dtype or x.dtype, memory_format=_DENSE)
+    elif out_dtype is not None and out_dtype != out.dtype:
+        raise ValueError("out_dtype differs from out's")
+    if sum_out is None and residual is not None:
+        sum_out = torch.empty_like(x, memory_format=_DENSE)
+    scale = x.new_empty(mx[1], dtype=torch.float32) if out.dtype == torch.float8_e4m3fn else None
+    _call("wfst_am_norm", _PACK["norm"].pack(
+        *mx, *mr, *(_NONE if sum_out is None else _matrix(sum_out, "sum_out", d)), *_matrix(out, "out", d),
+        _vector(gain, "gain", mx[2], d), 0 if scale is None else scale.data_ptr(), eps, 0), _raw_stream(d))
     return out, scale, sum_out
 
 
+@_here
 def wfst_am_norm_backward(dy: torch.Tensor, s: torch.Tensor, gain: Optional[torch.Tensor] = None, *,
-                          dsum: Optional[torch.Tensor] = None, eps: float = 1e-6, gain_gradient: bool = True,
-                          stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+                          dsum: Optional[torch.Tensor] = None, eps: float = 1e-6, gain_gradient: bool = True
+                          ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """(dx, dgain) of wfst_am_norm at its sum ``s`` (x itself without a
     residual); dx is the gradient of x and of residual.  ``dsum``: the
     gradient that reaches the sum past the norm."""
     d, keep = _device(dy, "dy"), []
-    with _On(d, stream) as st:
-        mdy, ms = _input(dy, "dy", d, keep), _input(s, "s", d, keep)
-        dx = torch.empty((ms[1], ms[2]), dtype=s.dtype, device=s.device)
-        dg = torch.empty(ms[2], dtype=torch.float32, device=s.device) if gain_gradient else None
-        head = (*mdy, *ms, *(_NONE if dsum is None else _input(dsum, "dsum", d, keep)), *_matrix(dx, "dx", d),
-                _vector(gain, "gain", ms[2], d), 0 if dg is None else dg.data_ptr())
-        pack = _PACK["norm_backward"].pack
-        need = _bytes_for("wfst_am_norm_backward_workspace", pack(*head, 0, 0, eps, 0))
-        work = torch.empty(need, dtype=torch.uint8, device=s.device) if need else None
-        _call("wfst_am_norm_backward", pack(*head, work.data_ptr() if need else 0, need, eps, 0), st)
+    mdy, ms = _matrix(dy, "dy", d, keep), _matrix(s, "s", d, keep)
+    dx = torch.empty_like(s, memory_format=_DENSE)
+    dg = s.new_empty(ms[2], dtype=torch.float32) if gain_gradient else None
+    head = (*mdy, *ms, *(_NONE if dsum is None else _matrix(dsum, "dsum", d, keep)), *_matrix(dx, "dx", d),
+            _vector(gain, "gain", ms[2], d), 0 if dg is None else dg.data_ptr())
+    pack = _PACK["norm_backward"].pack
+    need = _bytes_for("wfst_am_norm_backward_workspace", pack(*head, 0, 0, eps, 0))
+    work = s.new_empty(need, dtype=torch.uint8) if need else None
+    _call("wfst_am_norm_backward", pack(*head, work.data_ptr() if need else 0, need, eps, 0), _raw_stream(d))
     return dx, dg
 
 
+@_here
 def wfst_am_distill(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, *,
                     temperature: float = 1.0, weight: Optional[torch.Tensor] = None, gradient: bool = False,
-                    dlogits: Optional[torch.Tensor] = None, stream=None
+                    dlogits: Optional[torch.Tensor] = None
                     ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
     """(loss [M], lse [M], dlogits): the loss of the student's logits [M x L]
     against the teacher's top entries (top_index [M x k] int32, top_logit
     [M x k]), and with ``gradient`` (or a tensor for it in ``dlogits``, which
     may be logits) the gradient of the summed loss (wfst_am_distill)."""
     d, keep = _device(logits, "logits"), []
-    with _On(d, stream) as st:
-        mx, mt = _input(logits, "logits", d, keep), _input(top_logit, "top_logit", d, keep)
-        loss = torch.empty(mx[1], dtype=torch.float32, device=logits.device)
-        lse = torch.empty(mx[1], dtype=torch.float32, device=logits.device)
-        if dlogits is None and gradient:
-            dlogits = torch.empty((mx[1], mx[2]), dtype=logits.dtype, device=logits.device)
-        _call("wfst_am_distill", _PACK["distill"].pack(
-            *mx, *mt, *(_NONE if dlogits is None else _matrix(dlogits, "dlogits", d)),
-            _vector(top_index, "top_index", mt[1] * mt[2], d, torch.int32), _vector(weight, "weight", mx[1], d),
-            loss.data_ptr(), lse.data_ptr(), temperature, 0), st)
+    mx, mt = _matrix(logits, "logits", d, keep), _matrix(top_logit, "top_logit", d, keep)
+    loss = logits.new_empty(mx[1], dtype=torch.float32)
+    lse = torch.empty_like(loss)
+    if dlogits is None and gradient:
+        dlogits = torch.empty_like(logits, memory_format=_DENSE)
+    _call("wfst_am_distill", _PACK["distill"].pack(
+        *mx, *mt, *(_NONE if dlogits is None else _matrix(dlogits, "dlogits", d)),
+        _vector(top_index, "top_index", mt[1] * mt[2], d, torch.int32), _vector(weight, "weight", mx[1], d),
+        loss.data_ptr(), lse.data_ptr(), temperature, 0), _raw_stream(d))
     return loss, lse, dlogits
 
 
+@_here
 def wfst_am_distill_backward(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor,
                              lse: torch.Tensor, *, temperature: float = 1.0, weight: Optional[torch.Tensor] = None,
-                             dlogits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                             dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dlogits alone, from the forward call's lse (wfst_am_distill_backward);
     ``weight``: the gradient that reaches each row's loss, times the forward
     call's weight."""
     d, keep = _device(logits, "logits"), []
-    with _On(d, stream) as st:
-        mx, mt = _input(logits, "logits", d, keep), _input(top_logit, "top_logit", d, keep)
-        if dlogits is None:
-            dlogits = torch.empty((mx[1], mx[2]), dtype=logits.dtype, device=logits.device)
-        _call("wfst_am_distill_backward", _PACK["distill"].pack(
-            *mx, *mt, *_matrix(dlogits, "dlogits", d),
-            _vector(top_index, "top_index", mt[1] * mt[2], d, torch.int32), _vector(weight, "weight", mx[1], d),
-            0, _vector(lse, "lse", mx[1], d), temperature, 0), st)
+    mx, mt = _matrix(logits, "logits", d, keep), _matrix(top_logit, "top_logit", d, keep)
+    if dlogits is None:
+        dlogits = torch.empty_like(logits, memory_format=_DENSE)
+    _call("wfst_am_distill_backward", _PACK["distill"].pack(
+        *mx, *mt, *_matrix(dlogits, "dlogits", d),
+        _vector(top_index, "top_index", mt[1] * mt[2], d, torch.int32), _vector(weight, "weight", mx[1], d),
+        0, _vector(lse, "lse", mx[1], d), temperature, 0), _raw_stream(d))
     return dlogits
 
 
+@_here
 def wfst_am_loglikes(logits: torch.Tensor, log_prior: Optional[torch.Tensor] = None, *, scale: float = 1.0,
-                     out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """scale * (log softmax(logits) - log_prior), float32 [M x L]: rows for
     wfst_decode (wfst_am_loglikes)."""
     d, keep = _device(logits, "logits"), []
-    with _On(d, stream) as st:
-        mx = _input(logits, "logits", d, keep)
-        if out is None:
-            out = torch.empty((mx[1], mx[2]), dtype=torch.float32, device=logits.device)
-        _call("wfst_am_loglikes", _PACK["loglikes"].pack(
-            *mx, *_matrix(out, "out", d), _vector(log_prior, "log_prior", mx[2], d), scale, 0), st)
+    mx = _matrix(logits, "logits", d, keep)
+    if out is None:
+        out = torch.empty_like(logits, dtype=torch.float32, memory_format=_DENSE)
+    _call("wfst_am_loglikes", _PACK["loglikes"].pack(
+        *mx, *_matrix(out, "out", d), _vector(log_prior, "log_prior", mx[2], d), scale, 0), _raw_stream(d))
     return out
