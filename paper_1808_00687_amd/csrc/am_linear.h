@@ -5,7 +5,7 @@
 
 namespace wfd {
 
-// out = a b^T, both k-contiguous (am_linear_f16.hip, am_linear_bf16.hip, am_linear_f8.hip)
+// out = a b^T, both k-contiguous; tile 0: without tiles (am_thin.h) (am_linear_f16.hip, am_linear_bf16.hip, am_linear_f8.hip)
 template <typename E>
 void am_product_forward(const AmProduct &p, int32_t tile, hipStream_t st);
 // dx[m][k] = sum_n dz[m][n] w[n][k]: w is k-major

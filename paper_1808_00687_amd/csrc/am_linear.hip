@@ -130,7 +130,11 @@ hipError_t am_launch_linear(const wfst_am_linear_args &a, hipStream_t st)
     p.residual = a.residual, p.pre = a.pre, p.out = a.y;
     p.activation = a.activation;
     p.vec = am_rows_aligned(a.y) && (!a.residual.data || am_rows_aligned(a.residual)) && (!a.pre.data || am_rows_aligned(a.pre));
-    const int32_t tile = am_plan(a.x.rows, a.w.rows, a.x.cols, false).tile;
+    // Few rows, or tiles for less than half of the chip: a tile waits for memory once a
+    // stage, the thin kernel hardly at all ((1, 1024, 6000): 5.1 us against 10.0, (400, 1024, 1024),
+    // 112 tiles: 8.8 against 11.1); with more it reads too much ((1500, 512, 640), 240 tiles: 8.8 against 7.7)
+    const bool thin = a.x.rows <= 32 || am_tiles(a.x.rows, a.w.rows, 64, 64) <= kComputeUnits / 2;
+    const int32_t tile = thin ? 0 : am_plan(a.x.rows, a.w.rows, a.x.cols, false).tile;
     if (a.x.type == WFST_F16) am_product_forward<f16>(p, tile, st);
     else if (a.x.type == WFST_BF16) am_product_forward<bf16>(p, tile, st);
     else am_product_forward<f8>(p, tile, st);
