@@ -15,11 +15,6 @@ void am_product_dx(const AmProduct &p, int32_t tile, hipStream_t st);
 template <typename E>
 void am_product_dw(const AmProduct &p, int32_t tile, hipStream_t st);
 
-inline bool am_rows_aligned(const wfst_matrix &m)
-{
-    return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && m.row_stride * am_type_bytes(m.type) % 16 == 0;
-}
-
 // row stride of dz in the workspace: rows on 16 bytes
 constexpr int64_t am_dz_stride(int64_t n) { return (n + 7) & ~int64_t{7}; }
 

@@ -94,7 +94,6 @@ void launch_backward(const wfst_am_linear_backward_args &a, hipStream_t st)
         p.splits = plan.dx.splits;
         p.partial = partial;
         p.out = a.dx;
-        p.vec = am_rows_aligned(p.out);
         am_product_dx<T>(p, plan.dx.tile, st);
     }
     if (a.dw.data) {
@@ -105,7 +104,6 @@ void launch_backward(const wfst_am_linear_backward_args &a, hipStream_t st)
         p.splits = plan.dw.splits;
         p.partial = partial;   // the other product's parts are joined by now
         p.out = a.dw;
-        p.vec = am_rows_aligned(p.out);
         am_product_dw<T>(p, plan.dw.tile, st);
     }
 }
@@ -129,7 +127,6 @@ hipError_t am_launch_linear(const wfst_am_linear_args &a, hipStream_t st)
     p.a_scale = a.x_scale, p.b_scale = a.w_scale, p.bias = a.bias;
     p.residual = a.residual, p.pre = a.pre, p.out = a.y;
     p.activation = a.activation;
-    p.vec = am_rows_aligned(a.y) && (!a.residual.data || am_rows_aligned(a.residual)) && (!a.pre.data || am_rows_aligned(a.pre));
     // Few rows, or tiles for less than half of the chip: a tile waits for memory once a
     // stage, the thin kernel hardly at all ((1, 1024, 6000): 5.1 us against 10.0, (400, 1024, 1024),
     // 112 tiles: 8.8 against 11.1); with more it reads too much ((1500, 512, 640), 240 tiles: 8.8 against 7.7)

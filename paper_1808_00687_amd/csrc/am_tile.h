@@ -72,7 +72,6 @@ struct AmProduct {
     const float *a_scale, *b_scale, *bias;
     wfst_matrix residual, pre, out;
     int32_t activation;
-    int32_t vec;               // out, residual and pre have 16-byte aligned rows
 };
 
 __device__ __forceinline__ float am_silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + am_exp(-z)); }
@@ -113,13 +112,14 @@ __device__ __forceinline__ void am_activate(float (&v)[N], int32_t kind)
         for (int i = 0; i < N; i++) v[i] = am_gelu(v[i]);
 }
 
-// N consecutive values of row i from column j on; `full`: all inside, rows 16-byte aligned
+// N consecutive values of row i from column j on; `full`: all inside.  Rows
+// need no alignment (wide accesses go to any address)
 template <typename T, int N>
 __device__ __forceinline__ void am_store_row(const wfst_matrix &m, int64_t i, int64_t j, const float (&v)[N], bool full)
 {
     T *p = static_cast<T *>(m.data) + i * m.row_stride + j;
     constexpr int kStep = N * sizeof(T) >= 16 ? 16 / sizeof(T) : N;
-    using V = T __attribute__((ext_vector_type(kStep)));
+    using V = T __attribute__((ext_vector_type(kStep), aligned(sizeof(T))));
     if (full) {
         #pragma unroll
         for (int s = 0; s < N; s += kStep) {
@@ -148,7 +148,7 @@ __device__ __forceinline__ void am_add_row(const wfst_matrix &m, int64_t i, int6
 {
     const T *p = static_cast<const T *>(m.data) + i * m.row_stride + j;
     constexpr int kStep = N * sizeof(T) >= 16 ? 16 / sizeof(T) : N;
-    using V = T __attribute__((ext_vector_type(kStep)));
+    using V = T __attribute__((ext_vector_type(kStep), aligned(sizeof(T))));
     if (full) {
         #pragma unroll
         for (int s = 0; s < N; s += kStep) {
@@ -176,7 +176,7 @@ template <int N>
 __device__ __forceinline__ void am_finish(const AmProduct &p, int64_t i, int64_t j, float (&v)[N],
                                           const float (&b_scale)[N], const float (&bias)[N])
 {
-    const bool full = p.vec && j + N <= p.b.extent;
+    const bool full = j + N <= p.b.extent;
     if (p.a_scale) {
         const float s = p.a_scale[i];
         #pragma unroll
