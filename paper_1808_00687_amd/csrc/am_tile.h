@@ -223,6 +223,17 @@ __device__ __forceinline__ void am_widen(i32x4 v, i32x4 &lo, i32x4 &hi)
     }
 }
 
+template <int e>
+__device__ __forceinline__ uint32_t am_bits(const f32x4 &v)
+{
+    return __float_as_uint(v[e]);
+}
+template <int e>
+__device__ __forceinline__ void am_set(f32x4 &v, uint32_t bits)
+{
+    v[e] = __uint_as_float(bits);
+}
+
 // Tile (ti, tj) of workgroup `block` of `count`.  Workgroups go to the 8
 // chiplets in turn; each chiplet gets a run of consecutive tiles, and runs go
 // through blocks of 8 rows of tiles, so a chiplet's L2 sees few rows and columns.
@@ -598,30 +609,39 @@ __global__ __launch_bounds__(S::kThreads, 2) void am_tile_kernel(AmProduct p)
             });
     }
 
-    // a lane's runs of consecutive j: one of 4 * TJ, or TJ of 4
-    constexpr int kRun = 4 * kDeal, kRuns = TJ / kDeal;
-    am_each<kRuns>([&](auto t) {
-        const int64_t j = j0 + wj + (lane >> 4) * kRun + t * 16;
-        if (j >= p.b.extent) return;
-        float b_scale[kRun], bias[kRun];
-        if (p.splits == 1) am_columns(p, j, b_scale, bias);
+    // A lane's run of consecutive j.  With dealt rows it has 4 * TJ already; else
+    // 4 fragments' values change places between the 4 groups of 16 lanes, so that
+    // group g gets fragment g: a run of 16 again.
+    constexpr int kRun = 4 * TJ;
+    static_assert(kDeal > 1 || TJ == 4 || TJ == 1, "");
+    if constexpr (kDeal == 1 && TJ == 4)
         am_each<TI>([&](auto f) {
-            const int64_t i = i0 + wi + f * 16 + (lane & 15);
-            if (i >= p.a.extent) return;
-            float v[kRun];
-            am_each<kDeal>([&](auto d) {
-                const f32x4 a = acc[f][t * kDeal + d];
-                v[d * 4] = a[0], v[d * 4 + 1] = a[1], v[d * 4 + 2] = a[2], v[d * 4 + 3] = a[3];
+            am_each<4>([&](auto e) {
+                const auto lo = __builtin_amdgcn_permlane32_swap(am_bits<e>(acc[f][0]), am_bits<e>(acc[f][2]), false, false);
+                const auto hi = __builtin_amdgcn_permlane32_swap(am_bits<e>(acc[f][1]), am_bits<e>(acc[f][3]), false, false);
+                const auto u = __builtin_amdgcn_permlane16_swap(lo[0], hi[0], false, false);
+                const auto w = __builtin_amdgcn_permlane16_swap(lo[1], hi[1], false, false);
+                am_set<e>(acc[f][0], u[0]);
+                am_set<e>(acc[f][1], u[1]);
+                am_set<e>(acc[f][2], w[0]);
+                am_set<e>(acc[f][3], w[1]);
             });
-            if (p.splits == 1) {
-                am_finish(p, i, j, v, b_scale, bias);
-            } else {
-                float *o = p.partial + (static_cast<int64_t>(blockIdx.y) * p.a.extent + i) * p.b.extent + j;
-#pragma unroll
-                for (int e = 0; e < kRun; e++)
-                    if (j + e < p.b.extent) o[e] = v[e];
-            }
         });
+    const int64_t j = j0 + wj + (lane >> 4) * kRun;
+    if (j >= p.b.extent) return;
+    float b_scale[kRun], bias[kRun];
+    if (p.splits == 1) am_columns(p, j, b_scale, bias);
+    const wfst_matrix partial{p.partial + static_cast<int64_t>(blockIdx.y) * p.a.extent * p.b.extent, p.a.extent, p.b.extent, p.b.extent, WFST_F32, 0};
+    am_each<TI>([&](auto f) {
+        const int64_t i = i0 + wi + f * 16 + (lane & 15);
+        if (i >= p.a.extent) return;
+        float v[kRun];
+        am_each<TJ>([&](auto d) {
+            const f32x4 a = acc[f][d];
+            v[d * 4] = a[0], v[d * 4 + 1] = a[1], v[d * 4 + 2] = a[2], v[d * 4 + 3] = a[3];
+        });
+        if (p.splits == 1) am_finish(p, i, j, v, b_scale, bias);
+        else am_store_row<float>(partial, i, j, v, j + kRun <= p.b.extent);
     });
 #endif
 }
@@ -669,20 +689,30 @@ struct AmPlan {
     int32_t splits;
 };
 
-
+// By an estimate of the time: rounds of workgroups over the chip times stages
+// times what a stage of 64 values of k takes (measured, in microseconds, with as
+// many workgroups a CU as fit; a CU with fewer is done with them sooner, but not
+// in proportion).  A product that may be split (no epilogue, a workspace) also
+// pays the join of its parts: 8 bytes a part and value, and a launch.
 inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split)
 {
+    constexpr struct {
+        int32_t tile;
+        int64_t fit;
+        double stage;
+    } kinds[] = {{256, 1, 1.45}, {128, 3, 2.3}, {64, 2, 0.55}};
     const int64_t stages = (inner + 63) / 64;
-    for (int32_t t = 256; t >= 128; t /= 2) {
-        const int64_t n = am_tiles(rows, cols, t, t);
-        if (n >= kComputeUnits / 2) return {t, 1};
-        const int64_t s = kComputeUnits / n;
-        if (may_split && s > 1 && s <= 16 && stages / s >= 16) return {t, static_cast<int32_t>(s)};
-    }
-    if (!may_split) return {64, 1};
-    int64_t s = 2 * kComputeUnits / am_tiles(rows, cols, 64, 64);
-    s = s < stages / 4 ? s : stages / 4;
-    return {64, static_cast<int32_t>(s < 1 ? 1 : s > 64 ? 64 : s)};
+    AmPlan best{64, 1};
+    double least = 1e30;
+    for (const auto &k : kinds)
+        for (int32_t s = 1; s <= (may_split ? 64 : 1) && (s == 1 || stages / s >= 4); s *= 2) {
+            const int64_t n = am_tiles(rows, cols, k.tile, k.tile) * s, at_once = kComputeUnits * k.fit;
+            const double share = n >= at_once || k.fit == 1 ? 1.0 : n <= kComputeUnits ? 0.5 : 0.75;
+            double t = static_cast<double>((n + at_once - 1) / at_once) * share * static_cast<double>((stages + s - 1) / s) * k.stage;
+            if (s > 1) t += 5.0 + static_cast<double>(rows) * static_cast<double>(cols) * 8.0 * s / 4e6;
+            if (t < least) least = t, best = {k.tile, s};
+        }
+    return best;
 }
 
 inline int64_t am_partial_bytes(int64_t rows, int64_t cols, int32_t splits)
