@@ -55,13 +55,17 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
     if constexpr (S::kWaves > 1) __syncthreads();
 
     // what a row needs from memory is fetched while the row before it is worked on
+    // (a forward row's logits give way to their exponentials, and the next row's
+    // are fetched in their place; the other forms keep them to the end)
+    constexpr bool kKeep = !kBackward && S::kNv > 0;
     RowPart<S, T> x, next;
     int32_t unit[kEntries], unit_next[kEntries];
     float top[kEntries], top_next[kEntries], at_unit[kEntries], at_next[kEntries];
+    const auto hold_row = [&](int64_t r) {
+        if (r < M) (kKeep ? x : next).hold(row<T>(a.logits, r), L, t, low);
+    };
     const auto hold = [&](int64_t r) {
-        if (r >= M) return;
-        next.hold(row<T>(a.logits, r), L, t, low);
-        if (t >= 64) return;
+        if (r >= M || t >= 64) return;
 #pragma unroll
         for (int i = 0; i < kEntries; i++) {
             const int j = i * 64 + t;
@@ -78,10 +82,14 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
     };
 
     int64_t m = static_cast<int64_t>(blockIdx.x) * S::kRows + sub;
+    hold_row(m);
     hold(m);
     hold_units(m);
     for (; m < M; m += step) {
-        x = next;
+        if constexpr (!kKeep) {
+            x = next;
+            hold_row(m + step);
+        }
 #pragma unroll
         for (int i = 0; i < kEntries; i++) unit[i] = unit_next[i], top[i] = top_next[i], at_unit[i] = at_next[i];
         hold(m + step);
@@ -167,6 +175,7 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
             lse = lse_of(stat);
             if (a.lse && t == 0) a.lse[m] = lse;
         }
+        if constexpr (kKeep) hold_row(m + step);
         if constexpr (S::kWaves == 1) wave_sync();
         const bool live = w != 0.0f && tab.used;
         if constexpr (!kBackward)
@@ -182,25 +191,25 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
         if (d) {
             const float scale = w * temp;
             // q = 2^(y - own) * over, or e^(x / temperature - lse)
-            const float over = kBackward ? 0.0f : __builtin_amdgcn_exp2f(stat.own - stat.top) / stat.sum;
+            const float over = kBackward ? 0.0f : scale * (__builtin_amdgcn_exp2f(stat.own - stat.top) / stat.sum);
             if (live) {
+                const int32_t own = head;
                 S::each(L, t, [&](int v, int64_t c, int64_t left) {
                     float g[S::kC];
-                    if constexpr (kBackward || S::kNv == 0) {
-                        get_x(v, c, left, g);
-#pragma unroll
-                        for (int e = 0; e < S::kC; e++) g[e] = am_exp(g[e] * inv_t - lse);
-                    } else {
+                    if constexpr (kKeep) {
 #pragma unroll
                         for (int e = 0; e < S::kC; e++) g[e] = kept[v][e] * over;
+                    } else {
+                        get_x(v, c, left, g);
+#pragma unroll
+                        for (int e = 0; e < S::kC; e++) g[e] = scale * am_exp(g[e] * inv_t - lse);
                     }
-                    for (int j = head; j >= 0; j = tab.next[j]) {
+                    for (int j = own; j >= 0; j = tab.next[j]) {
                         const int64_t at = tab.unit[j] - c;
+                        const float mass = tab.mass[j] * scale;
 #pragma unroll
-                        for (int e = 0; e < S::kC; e++) g[e] -= at == e ? tab.mass[j] : 0.0f;
+                        for (int e = 0; e < S::kC; e++) g[e] -= at == e ? mass : 0.0f;
                     }
-#pragma unroll
-                    for (int e = 0; e < S::kC; e++) g[e] *= scale;
                     store_floats(d + c, left, g);
                 });
                 head = -1;
