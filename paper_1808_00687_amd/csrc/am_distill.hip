@@ -38,7 +38,7 @@ __device__ __forceinline__ void wave_sync()
 
 // kEntries: entries a lane of the row's first wave takes care of
 template <typename T, typename S, bool kBackward, int kEntries>
-__global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_args a)
+__global__ __launch_bounds__(S::kThreads, kBackward && S::kTpr == 1024 && S::kNv * S::kC <= 16 ? 8 : 1) void distill_kernel(wfst_am_distill_args a)
 {
     __shared__ RowScratch scratch;
     // Two sets, used in turn: the first wave fills one for its next row while
@@ -128,23 +128,25 @@ __global__ __launch_bounds__(S::kThreads) void distill_kernel(wfst_am_distill_ar
             if (d) {
                 // a unit's whole share, from the entries in order; they go round the wave by lane reads
                 float mass[kEntries] = {};
-                bool first[kEntries];
-#pragma unroll
-                for (int i = 0; i < kEntries; i++) first[i] = unit[i] >= 0;
+                int32_t before[kEntries] = {};   // earlier entries of the same unit
 #pragma unroll
                 for (int o = 0; o < kEntries; o++) {
                     const int n = k - o * 64 < 64 ? k - o * 64 : 64;
                     for (int l = 0; l < n; l++) {
                         const int32_t u = __builtin_amdgcn_readlane(unit[o], l);
                         const float p = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share[o]), l));
+                        const int32_t j = o * 64 + l;
 #pragma unroll
-                        for (int i = 0; i < kEntries; i++)
-                            if (unit[i] == u) {
-                                mass[i] += p;
-                                first[i] = first[i] && o * 64 + l >= i * 64 + t;
-                            }
+                        for (int i = 0; i < kEntries; i++) {
+                            const bool same = unit[i] == u;
+                            mass[i] += same ? p : 0.0f;
+                            before[i] += same && j < i * 64 + t ? 1 : 0;
+                        }
                     }
                 }
+                bool first[kEntries];
+#pragma unroll
+                for (int i = 0; i < kEntries; i++) first[i] = unit[i] >= 0 && before[i] == 0;
 #pragma unroll
                 for (int i = 0; i < kEntries; i++)
                     if (first[i]) {

@@ -66,12 +66,13 @@ void am_row_shape_lean(int64_t D, F go)
     else am_row_shape<C>(D, go);
 }
 
-// Workgroups for M rows: all of them up to `most`, which then take several.
+// Workgroups for M rows: at most `most`, about as many as the chip holds at
+// once, each with the same number of turns.
 template <typename S>
 unsigned am_row_blocks(int64_t M, int64_t most)
 {
-    const int64_t n = (M + S::kRows - 1) / S::kRows;
-    return static_cast<unsigned>(n < most ? n : most);
+    const int64_t n = (M + S::kRows - 1) / S::kRows, turns = (n + most - 1) / most;
+    return static_cast<unsigned>(n ? (n + turns - 1) / turns : 0);
 }
 
 // A thread's chunks of one row, held or read when asked for.

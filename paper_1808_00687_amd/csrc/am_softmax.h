@@ -69,6 +69,6 @@ __device__ __forceinline__ RowStat row_stat(int64_t cols, int t, float c, G get,
 // log sum exp of x / temperature; -inf for a row of -inf
 __device__ __forceinline__ float lse_of(const RowStat &s) { return s.top * kLn2 + logf(s.sum); }
 
-constexpr int64_t kSoftmaxBlocks = 256 * 8;
+constexpr int64_t kSoftmaxBlocks = 256 * 4;
 
 }  // namespace wfd
