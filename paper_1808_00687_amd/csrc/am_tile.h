@@ -677,9 +677,11 @@ using AmLarge = AmShape<256, 256, 2, 4, 128, 2>;
 using AmLarge8 = AmShape<256, 128, 2, 2, 64, 3>;   // two workgroups a CU
 using AmMedium = AmShape<128, 128, 2, 2, 64, 3>;
 using AmMediumMajor = AmShape<128, 128, 2, 2, 64, 4>;
-using AmSmall = AmShape<64, 64, 1, 4, 128, 4>;
+using AmSmall = AmShape<64, 64, 2, 2, 128, 4>;
+using AmSmallMajor = AmShape<64, 64, 1, 4, 128, 4>;
 using AmMediumStaged = AmShape<128, 128, 2, 2, 64, 2>;
-using AmSmallStaged = AmShape<64, 64, 1, 4, 128, 2>;
+using AmSmallStaged = AmShape<64, 64, 2, 2, 128, 2>;
+using AmSmallMajorStaged = AmShape<64, 64, 1, 4, 128, 2>;
 
 constexpr int64_t kComputeUnits = 256;
 
@@ -726,13 +728,13 @@ void am_product(const AmProduct &p, int32_t tile, hipStream_t st)
     if (am_direct(p.a, kMajorA, p.inner, sizeof(E)) && am_direct(p.b, kMajorB, p.inner, sizeof(E))) {
         if (tile == 256) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<sizeof(E) == 1, AmLarge8, AmLarge>>(p, st);
         else if (tile == 128) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<kMajorB, AmMediumMajor, AmMedium>>(p, st);
-        else am_launch_tiles<E, kMajorA, kMajorB, true, AmSmall>(p, st);
+        else am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<kMajorB, AmSmallMajor, AmSmall>>(p, st);
     } else if (!am_near(p.a) || !am_near(p.b)) {
-        am_launch_tiles<E, kMajorA, kMajorB, false, AmSmallStaged, true>(p, st);
+        am_launch_tiles<E, kMajorA, kMajorB, false, std::conditional_t<kMajorB, AmSmallMajorStaged, AmSmallStaged>, true>(p, st);
     } else if (tile >= 128) {
         am_launch_tiles<E, kMajorA, kMajorB, false, AmMediumStaged>(p, st);
     } else {
-        am_launch_tiles<E, kMajorA, kMajorB, false, AmSmallStaged>(p, st);
+        am_launch_tiles<E, kMajorA, kMajorB, false, std::conditional_t<kMajorB, AmSmallMajorStaged, AmSmallStaged>>(p, st);
     }
 }
 
