@@ -24,7 +24,14 @@ __global__ __launch_bounds__(256) void join_kernel(AmProduct p)
     const int64_t n = static_cast<int64_t>(p.a.extent) * p.b.extent;
     for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < n; at += static_cast<int64_t>(gridDim.x) * 256) {
         float v[1] = {0.0f}, b_scale[1], bias[1];
-        for (int s = 0; s < p.splits; s++) v[0] += p.partial[s * n + at];
+        int s = 0;
+        for (; s + 4 <= p.splits; s += 4) {   // 4 loads under way, added in order
+            float u[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) u[e] = p.partial[(s + e) * n + at];
+            v[0] = v[0] + u[0] + u[1] + u[2] + u[3];
+        }
+        for (; s < p.splits; s++) v[0] += p.partial[s * n + at];
         const int64_t i = at / p.b.extent, j = at % p.b.extent;
         am_columns(p, j, b_scale, bias);
         am_finish(p, i, j, v, b_scale, bias);

@@ -692,25 +692,26 @@ struct AmPlan {
 };
 
 // By an estimate of the time: rounds of workgroups over the chip times stages
-// times what a stage of 64 values of k takes (measured, in microseconds, with as
-// many workgroups a CU as fit; a CU with fewer is done with them sooner, but not
-// in proportion).  A product that may be split (no epilogue, a workspace) also
-// pays the join of its parts: 8 bytes a part and value, and a launch.
+// times what a stage of 64 values of k takes (measured, in microseconds, with one,
+// two, ... workgroups on a CU, as many as fit).  A product that may be split (no
+// epilogue, a workspace) also pays the join of its parts: 8 bytes a part and value,
+// and a launch.
 inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split)
 {
     constexpr struct {
         int32_t tile;
         int64_t fit;
-        double stage;
-    } kinds[] = {{256, 1, 1.45}, {128, 3, 2.3}, {64, 2, 0.55}};
+        double stage[3];
+    } kinds[] = {{256, 1, {1.45}}, {128, 3, {1.5, 1.9, 2.3}}, {64, 2, {0.5, 0.55}}};
     const int64_t stages = (inner + 63) / 64;
     AmPlan best{64, 1};
     double least = 1e30;
     for (const auto &k : kinds)
         for (int32_t s = 1; s <= (may_split ? 64 : 1) && (s == 1 || stages / s >= 4); s *= 2) {
-            const int64_t n = am_tiles(rows, cols, k.tile, k.tile) * s, at_once = kComputeUnits * k.fit;
-            const double share = n >= at_once || k.fit == 1 ? 1.0 : n <= kComputeUnits ? 0.5 : 0.75;
-            double t = static_cast<double>((n + at_once - 1) / at_once) * share * static_cast<double>((stages + s - 1) / s) * k.stage;
+            const int64_t n = am_tiles(rows, cols, k.tile, k.tile) * s, at_once = kComputeUnits * k.fit, rest = n % at_once;
+            double t = static_cast<double>(n / at_once) * k.stage[k.fit - 1];
+            if (rest) t += k.stage[(rest - 1) / kComputeUnits];
+            t *= static_cast<double>((stages + s - 1) / s);
             if (s > 1) t += 5.0 + static_cast<double>(rows) * static_cast<double>(cols) * 8.0 * s / 4e6;
             if (t < least) least = t, best = {k.tile, s};
         }
