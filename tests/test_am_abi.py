@@ -123,7 +123,8 @@ REFUSED = [
     ("linear", {"x.type": 0, "w.type": 0}), ("linear", {"w.type": 1}), ("linear", {"x.type": 9}),
     ("linear", {"x.type": -1}), ("linear", {"y.type": 3}), ("linear", {"w.cols": 15}), ("linear", {"y.rows": 5}),
     ("linear", {"y.cols": 7}), ("linear", {"x.rows": -1}), ("linear", {"x.rows": 1 << 31}), ("linear", {"x.cols": 0}),
-    ("linear", {"w.rows": 0}), ("linear", {"x.row_stride": 15}), ("linear", {"y.row_stride": 1 << 60}),
+    ("linear", {"w.rows": 0}), ("linear", {"x.rows": (1 << 30) + 1}), ("linear", {"x.cols": (1 << 30) + 1}),
+    ("linear_backward", {"dy.cols": (1 << 30) + 1}), ("linear", {"x.row_stride": 15}), ("linear", {"y.row_stride": 1 << 60}),
     ("linear", {"x.data": A[0] + 1}), ("linear", {"bias": A[5] + 2}), ("linear", {"residual.type": 2}),
     ("linear", {"residual.rows": 3}), ("linear", {"pre.cols": 9}), ("linear", {"activation": 4}),
     ("linear", {"activation": -1}), ("linear", {"x_scale": A[6]}), ("linear", {"w_scale": A[6]}),

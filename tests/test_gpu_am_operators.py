@@ -619,6 +619,50 @@ def test_loglikes_masked_units(am, n):
 
 
 # --------------------------------------------------------------------------
+# rows far apart: byte offsets past 32 bits
+# --------------------------------------------------------------------------
+
+def far(buffer, t):
+    """t's values in rows 2^26 bytes apart."""
+    step = (1 << 26) // t.element_size()
+    v = buffer.view(t.dtype).as_strided(t.shape, (step, 1))
+    v.copy_(t)
+    return v
+
+
+def test_rows_far_apart(am):
+    m, k, n = 70, 72, 64 * 66
+    g = rng(21)
+    a, b, c = (torch.empty((m << 26) + (1 << 20), dtype=torch.uint8, device="cuda") for _ in range(3))
+    x, w = normal(g, m, k).to(BF16), normal(g, n, k, std=k ** -0.5).to(BF16)
+    y = am.wfst_am_linear(far(a, x), w.cuda(), out_dtype=F32)          # more tiles than half the chip
+    want, _, err = R.linear(x, w, None, "none", None)
+    R.close(y, want, err + 2 * R.U32 * want.abs(), "far linear")
+    few = w[:50].contiguous().cuda()
+    assert torch.equal(am.wfst_am_linear(far(a, x), few), am.wfst_am_linear(x.cuda(), few))
+    dy = normal(g, m, 130).to(BF16)
+    w2 = normal(g, 130, k).to(BF16).cuda()
+    dx, dw, db = am.wfst_am_linear_backward(far(b, dy), far(a, x), w2)
+    for got, left, right in ((dx, R.d(dy), R.d(w2)), (dw, R.d(dy).t(), R.d(x)), (db[:, None], R.d(dy).t(), torch.ones(m, 1).double())):
+        want, err = left @ right, R.sum_bound(left.shape[1], left.abs() @ right.abs())
+        R.close(got, want, err + R.U[got.dtype] * (want.abs() + err), "far backward")
+    h, res = normal(g, m, 300).to(BF16), normal(g, m, 300).to(BF16)
+    out = c.view(BF16).as_strided((m, 300), ((1 << 26) // 2, 1))
+    got = am.wfst_am_norm(far(a, h), residual=far(b, res), sum_out=out, out_dtype=F8)
+    for u, v in zip(got, am.wfst_am_norm(h.cuda(), residual=res.cuda(), out_dtype=F8)):
+        assert torch.equal(u.float(), v.float())
+    got = am.wfst_am_norm_backward(far(a, h), far(b, res))
+    for u, v in zip(got, am.wfst_am_norm_backward(h.cuda(), res.cuda())):
+        assert torch.equal(u, v)
+    idx, top = top_entries(g, m, 300, 4)
+    got = am.wfst_am_distill(far(a, h), idx.cuda(), top.cuda(), dlogits=out)
+    for u, v in zip(got, am.wfst_am_distill(h.cuda(), idx.cuda(), top.cuda(), gradient=True)):
+        assert torch.equal(u, v)
+    assert torch.equal(am.wfst_am_loglikes(far(a, h), out=c.view(F32).as_strided((m, 300), ((1 << 26) // 4, 1))),
+                       am.wfst_am_loglikes(h.cuda()))
+
+
+# --------------------------------------------------------------------------
 # streams, graphs, repeats
 # --------------------------------------------------------------------------
 
