@@ -338,44 +338,61 @@ struct AmSide {
                                                  16, voff[q], 0, 0, 0);
     }
 
-    // Through registers, any alignment.  Values past k's end are zeros; rows
-    // past the operand's end repeat the last one (their results are not stored).
+    // Through registers, any alignment.  A chunk over its row's end is the 16
+    // bytes that end there (put() moves them into place), so the loads have no
+    // branch; only rows shorter than a chunk are taken value by value.  Values
+    // past k's end become zeros; of a k-contiguous operand, rows past the end
+    // repeat the last one, of a k-major one what follows a row's end is zeros
+    // (results from neither are stored).
     __device__ __forceinline__ void load(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, i32x4 (&r)[kPerWave], int wave, int lane)
     {
-        using Offset = std::conditional_t<kFar, int64_t, int32_t>;
-        const AM_GLOBAL char *base = (const AM_GLOBAL char *)o.data + (kMajor ? k0 * o.ld + first * kEl : first * o.ld + static_cast<int64_t>(k0) * kEl);
-        const int32_t rows_left = o.extent - static_cast<int32_t>(first), k_left = inner - k0;
+        using Offset = std::conditional_t<kFar, int64_t, uint32_t>;
+        const AM_GLOBAL char *base = (const AM_GLOBAL char *)o.data + (kMajor ? k0 : first) * o.ld;
+        const int32_t from = kMajor ? static_cast<int32_t>(first) : k0, length = kMajor ? o.extent : inner;
+        const int32_t last = kMajor ? inner - k0 - 1 : o.extent - static_cast<int32_t>(first) - 1;
 #pragma unroll
         for (int q = 0; q < kPerWave; q++) {
-            // row as stored and first value in it, from `base` on
-            int32_t row = row_of(q, wave, lane);
-            const int32_t at = chunk_of(q, wave, lane) * kWide;
-            if constexpr (!kMajor) row = row < rows_left ? row : rows_left - 1;
-            const int32_t along = (kMajor ? rows_left : k_left) - at;   // values left in the stored row
-            const AM_GLOBAL char *p = base + (static_cast<Offset>(row) * static_cast<Offset>(o.ld) + at * kEl);
-            i32x4 v = {0, 0, 0, 0};
-            if (along >= kWide && (!kMajor || row < k_left)) {
-                v = *(const AM_GLOBAL i32x4_any *)p;
-            } else if (along > 0 && (!kMajor || row < k_left)) {
+            int32_t row = row_of(q, wave, lane), at = from + chunk_of(q, wave, lane) * kWide;
+            row = row < last ? row : last;
+            const AM_GLOBAL char *p = base + static_cast<Offset>(row) * static_cast<Offset>(o.ld);
+            if (length >= kWide) {
+                at = at < length - kWide ? at : length - kWide;
+                r[q] = *(const AM_GLOBAL i32x4_any *)(base + (static_cast<Offset>(row) * static_cast<Offset>(o.ld) + static_cast<Offset>(at) * kEl));
+            } else {
                 uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (int e = 0; e < kWide; e++)
-                    if (e < along) {
+                    if (at + e < length) {
                         uint32_t t;
-                        if constexpr (kEl == 2) t = ((const AM_GLOBAL uint16_t *)p)[e];
-                        else t = ((const AM_GLOBAL uint8_t *)p)[e];
+                        if constexpr (kEl == 2) t = ((const AM_GLOBAL uint16_t *)p)[at + e];
+                        else t = ((const AM_GLOBAL uint8_t *)p)[at + e];
                         w[e * kEl / 4] |= t << (e * kEl % 4 * 8);
                     }
-                v = i32x4{static_cast<int>(w[0]), static_cast<int>(w[1]), static_cast<int>(w[2]), static_cast<int>(w[3])};
+                r[q] = i32x4{static_cast<int>(w[0]), static_cast<int>(w[1]), static_cast<int>(w[2]), static_cast<int>(w[3])};
             }
-            r[q] = v;
         }
     }
-    __device__ __forceinline__ void put(const i32x4 (&r)[kPerWave], char *stage, int wave, int lane)
+    // `first`, `inner` and `k0` as for the load of r
+    __device__ __forceinline__ void put(const AmOperand &o, int64_t first, int32_t inner, int32_t k0, const i32x4 (&r)[kPerWave], char *stage,
+                                        int wave, int lane)
     {
+        constexpr int32_t kRows = kBytes / 16 / kRowChunks;
+        const int32_t from = kMajor ? static_cast<int32_t>(first) : k0, length = kMajor ? o.extent : inner;
+        const int32_t k_left = inner - k0;
+        const bool whole = from + kRowChunks * kWide <= length && (!kMajor || kRows <= k_left);
 #pragma unroll
-        for (int q = 0; q < kPerWave; q++)
-            *reinterpret_cast<i32x4 *>(stage + ((wave * kPerWave + q) * 64 + lane) * 16) = r[q];
+        for (int q = 0; q < kPerWave; q++) {
+            i32x4 v = r[q];
+            if (!whole) {
+                // how many of the chunk's values lie before its place
+                const int32_t row = row_of(q, wave, lane), at = from + chunk_of(q, wave, lane) * kWide;
+                int32_t before = length >= kWide ? at - (length - kWide) : 0;
+                before = before < 0 ? 0 : before;
+                if (before >= kWide || (kMajor && row >= k_left)) v = i32x4{0, 0, 0, 0};
+                else v = __builtin_bit_cast(i32x4, __builtin_bit_cast(unsigned __int128, v) >> (before * kEl * 8));
+            }
+            *reinterpret_cast<i32x4 *>(stage + ((wave * kPerWave + q) * 64 + lane) * 16) = v;
+        }
     }
 
     // For the fragments of the wave's rows from `base` on.
@@ -594,12 +611,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void am_tile_kernel(AmProduct p)
             sa.load(p.a, i0, p.inner, s * kK, ra, wave, lane);
             sb.load(p.b, j0, p.inner, s * kK, rb, wave, lane);
         };
-        const auto put = [&](auto n) {
-            sa.put(ra, place_a(n), wave, lane);
-            sb.put(rb, place_b(n), wave, lane);
+        const auto put = [&](auto n, int32_t s) {
+            sa.put(p.a, i0, p.inner, s * kK, ra, place_a(n), wave, lane);
+            sb.put(p.b, j0, p.inner, s * kK, rb, place_b(n), wave, lane);
         };
         load(s);
-        put(first);
+        put(first, s);
         load(s + 1);
         __syncthreads();
         first_reads(first);
@@ -608,7 +625,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void am_tile_kernel(AmProduct p)
                 // the next stage goes to its place in the middle of this one, and the one after it on its way
                 constexpr std::integral_constant<int, n + 1> next{};
                 stage(n, [&] {
-                    put(next);
+                    put(next, s + 1);
                     load(s + 2);
                 }, [&] {
                     __syncthreads();
