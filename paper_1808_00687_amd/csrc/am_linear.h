@@ -38,13 +38,14 @@ inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a)
     if (p.strips < 1) p.strips = 1;
     if (a.dbias && p.strips > 1) p.partial_bytes = (p.strips * N * 4 + 255) & ~int64_t{255};
     if (a.activation != WFST_ACT_NONE && (a.dx.data || a.dw.data)) p.dz_bytes = (M * am_dz_stride(N) * 2 + 255) & ~int64_t{255};
+    const bool whole = N % 8 == 0;   // rows of dz are
     if (a.dx.data) {
-        p.dx = am_plan(M, a.dx.cols, N, true);
+        p.dx = am_plan(M, a.dx.cols, N, true, whole && a.dx.cols % 8 == 0);
         const int64_t b = am_partial_bytes(M, a.dx.cols, p.dx.splits);
         p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
     }
     if (a.dw.data) {
-        p.dw = am_plan(N, a.dw.cols, M, true);
+        p.dw = am_plan(N, a.dw.cols, M, true, whole && a.dw.cols % 8 == 0);
         const int64_t b = am_partial_bytes(N, a.dw.cols, p.dw.splits);
         p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
     }

@@ -442,10 +442,12 @@ __device__ __forceinline__ void am_wait_vm()
 template <int BM_, int BN_, int WM_, int WN_, int SB_, int kBuffers_>
 struct AmShape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, SB = SB_, kBuffers = kBuffers_, kThreads = WM_ * WN_ * 64;
+    // one workgroup a CU by its LDS may have all registers
+    static constexpr int kWavesASimd = kThreads == 256 && (BM + BN) * SB * kBuffers > 80 * 1024 ? 1 : 2;
 };
 
 template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kFar = false>
-__global__ __launch_bounds__(S::kThreads, 2) void am_tile_kernel(AmProduct p)
+__global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(AmProduct p)
 {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub alone
     constexpr int BM = S::BM, BN = S::BN, WN = S::WN, SB = S::SB, kBuffers = S::kBuffers;
@@ -703,6 +705,7 @@ using AmLarge = AmShape<256, 256, 2, 4, 128, 2>;
 using AmLarge8 = AmShape<256, 128, 2, 2, 64, 3>;   // two workgroups a CU
 using AmMedium = AmShape<128, 128, 2, 2, 64, 3>;
 using AmMediumMajor = AmShape<128, 128, 2, 2, 64, 4>;
+using AmMediumDeep = AmShape<128, 128, 2, 2, 128, 4>;   // one workgroup a CU
 using AmSmall = AmShape<64, 64, 2, 2, 128, 4>;
 using AmSmallMajor = AmShape<64, 64, 1, 4, 128, 4>;
 using AmMediumStaged = AmShape<128, 128, 2, 2, 64, 2>;
@@ -721,20 +724,25 @@ struct AmPlan {
 // times what a stage of 64 values of k takes (measured, in microseconds, with one,
 // two, ... workgroups on a CU, as many as fit).  A product that may be split (no
 // epilogue, a workspace) also pays the join of its parts: 8 bytes a part and value,
-// and a launch.
-inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split)
+// and a launch.  128 x 128 tiles that are at most one a CU have stages of twice the
+// length, four of them: with the shorter ones a CU waits for memory ((4096, 1024,
+// 1024) 19.4 us, so 16.2; (2048, 1024, 2048) 18.6 and 15.8; the gradient of x of
+// (3000, 1024, 2048) 34.1 and 27.9).  Where rows are no multiple of 16 bytes (not
+// `whole`) stages go through registers and that does not hold.
+inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split, bool whole)
 {
     constexpr struct {
         int32_t tile;
-        int64_t fit;
+        int64_t fit, most;   // workgroups on a CU, and on the chip
         double stage[3];
-    } kinds[] = {{256, 1, {1.45}}, {128, 3, {1.5, 1.9, 2.3}}, {64, 2, {0.5, 0.55}}};
+    } kinds[] = {{256, 1, INT64_MAX, {1.45}}, {128, 1, kComputeUnits, {0.95}}, {128, 3, INT64_MAX, {1.5, 1.9, 2.3}}, {64, 2, INT64_MAX, {0.5, 0.55}}};
     const int64_t stages = (inner + 63) / 64;
     AmPlan best{64, 1};
     double least = 1e30;
     for (const auto &k : kinds)
         for (int32_t s = 1; s <= (may_split ? 64 : 1) && (s == 1 || stages / s >= 4); s *= 2) {
             const int64_t n = am_tiles(rows, cols, k.tile, k.tile) * s, at_once = kComputeUnits * k.fit, rest = n % at_once;
+            if (n > k.most || (!whole && k.most == kComputeUnits)) break;
             double t = static_cast<double>(n / at_once) * k.stage[k.fit - 1];
             if (rest) t += k.stage[(rest - 1) / kComputeUnits];
             t *= static_cast<double>((stages + s - 1) / s);
@@ -754,6 +762,8 @@ void am_product(const AmProduct &p, int32_t tile, hipStream_t st)
 {
     if (am_direct(p.a, kMajorA, p.inner, sizeof(E)) && am_direct(p.b, kMajorB, p.inner, sizeof(E))) {
         if (tile == 256) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<sizeof(E) == 1, AmLarge8, AmLarge>>(p, st);
+        else if (tile == 128 && am_tiles(p.a.extent, p.b.extent, 128, 128) * p.splits <= kComputeUnits)
+            am_launch_tiles<E, kMajorA, kMajorB, true, AmMediumDeep>(p, st);
         else if (tile == 128) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<kMajorB, AmMediumMajor, AmMedium>>(p, st);
         else am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<kMajorB, AmSmallMajor, AmSmall>>(p, st);
     } else if (!am_near(p.a) || !am_near(p.b)) {

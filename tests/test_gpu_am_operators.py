@@ -154,6 +154,27 @@ def test_linear_backward_large_tiles(am, m, k, n, dt):
     backward_case(am, m, k, n, dt, "none", 4, pad=8, weight_dtype=F32)
 
 
+# at most one 128 x 128 tile a compute unit, in each of the three products; 8, 9 and 29 stages of k, the last one not full
+@pytest.mark.parametrize("dt", [BF16, F16, F8])
+@pytest.mark.parametrize("m,k,n", [(2040, 456, 1960), (2048, 1816, 1928), (1912, 520, 2032)])
+def test_linear_one_tile_a_unit(am, m, k, n, dt):
+    linear_case(am, m, k, n, dt, "relu", F32, 13, pre=True, pad=16)
+    if dt != F8:
+        backward_case(am, m, n, k, dt, "none", 14, pad=8)   # inner size k in dx
+        backward_case(am, k, n, m, dt, "relu", 15)          # and in dw
+
+
+# rows that are no whole number of 16-byte chunks, around the lengths of a chunk, a tile and a stage
+@pytest.mark.parametrize("dt", [BF16, F16, F8])
+@pytest.mark.parametrize("width", [1, 7, 9, 15, 17, 63, 71, 127, 129, 145])
+def test_linear_ends_of_rows(am, width, dt):
+    linear_case(am, 700, width, 900, dt, "none", F32, width, pad=3)
+    linear_case(am, 700, 72, 900 + width, dt, "none", F32, width, offset=1)
+    if dt != F8:
+        for m, k, n in ((300, 264, width), (300, width, 264), (width, 129, 135)):
+            backward_case(am, m, k, n, dt, "none", width, pad=3)
+
+
 @pytest.mark.parametrize("m", [4, 300])
 @pytest.mark.parametrize("dt", [BF16, F16, F8])
 def test_linear_infinity_and_nan_stay_in_their_rows(am, m, dt):
