@@ -7,7 +7,8 @@
 // bytes of k for every row of the tile.  Two to four stages lie in LDS: the later
 // ones are fetched while the matrix cores work on the present one.  The fetch goes
 // straight from memory to LDS (16 bytes a lane, no registers); operands that are
-// not aligned to 16 bytes go through registers.
+// not aligned to 16 bytes go through registers ((16384, 1001, 2048) forward, both
+// gradients: 121, 111, 127 us; with 1024 aligned columns 75, 60, 93).
 //
 // 8-bit operands are widened to bf16 as they are read from LDS (each value
 // exactly).  The 8-bit matrix instructions would be twice as fast, but drop the
