@@ -506,7 +506,7 @@ int wfst_set_debug_opts(const wfst_debug_opts *opts);
  *
  * Sums, statistics and everything between the inputs and an output are held
  * in float32; an output in fewer bits is rounded once, to nearest, ties to
- * even, on its way out (wfst_am_linear_backward states the one exception).
+ * even, on its way out (wfst_am_linear_backward states what its products read).
  * An infinity or NaN reaches the outputs that depend on it by the formula.
  */
 #define WFST_F32 0
@@ -571,8 +571,14 @@ int wfst_am_linear(const wfst_am_linear_args *args, void *hip_stream);
  *   workspace  at least wfst_am_linear_backward_workspace bytes, 256-byte
  *            aligned
  *
- * The matrix products read dz in the 16-bit type (the matrix cores multiply
- * 16-bit operands); dbias sums the unrounded dz.  M = 0 gives zero dw, dbias.
+ *   round_dz  0 or 1 (below)
+ *
+ * The matrix cores multiply 16-bit operands.  The products read the dz of a
+ * silu or gelu as the sum of two 16-bit values, within 2^-16 (WFST_BF16) or
+ * 2^-22 (WFST_F16, or 2^-35 if that is more) of it; round_dz = 1 makes it one,
+ * rounded to nearest (dx and dw 1.4 times as far from the exact ones, a little over
+ * half the time).  Other dz are dy, or 0, and exact.  dbias sums the float32 dz.
+ * M = 0 gives zero dw, dbias.
  * Sizes as for wfst_am_linear.
  * Errors: WFST_EINVAL (also a workspace that is too small), WFST_EDEVICE.
  */
@@ -582,12 +588,12 @@ typedef struct wfst_am_linear_backward_args {
     void *workspace;
     int64_t workspace_bytes;
     int32_t activation;
-    int32_t reserved;
+    int32_t round_dz;
 } wfst_am_linear_backward_args;
 
 /* The workspace that args needs (its workspace fields and data pointers are
-   only tested for NULL); it depends on sizes, types and which outputs are
-   asked for. */
+   only tested for NULL); it depends on sizes, types, the activation, round_dz
+   and which outputs are asked for. */
 int wfst_am_linear_backward_workspace(const wfst_am_linear_backward_args *args, int64_t *bytes);
 int wfst_am_linear_backward(const wfst_am_linear_backward_args *args, void *hip_stream);
 

@@ -45,7 +45,7 @@ class _LinearArgs(C.Structure):
 class _LinearBackwardArgs(C.Structure):
     _fields_ = [("dy", _Matrix), ("pre", _Matrix), ("x", _Matrix), ("w", _Matrix), ("dx", _Matrix), ("dw", _Matrix),
                 ("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
-                ("activation", C.c_int32), ("reserved", C.c_int32)]
+                ("activation", C.c_int32), ("round_dz", C.c_int32)]
 
 
 class _NormArgs(C.Structure):
@@ -209,13 +209,15 @@ def wfst_am_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor
 @_here
 def wfst_am_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[torch.Tensor], *,
                             activation: str = "none", pre: Optional[torch.Tensor] = None,
-                            bias_gradient: bool = True, weight_dtype: Optional[torch.dtype] = None
-                            ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
+                            bias_gradient: bool = True, weight_dtype: Optional[torch.dtype] = None,
+                            round_dz: bool = False) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
     """(dx, dw, dbias) of wfst_am_linear with a 16-bit x (the residual's
     gradient is dy).  ``w`` None leaves out dx, ``x`` None dw.
-    ``weight_dtype``: dw's type, dy's by default."""
+    ``weight_dtype``: dw's type, dy's by default.  ``round_dz``: dx and dw from
+    a silu's or gelu's dz rounded to 16 bits, faster, where two 16-bit values
+    hold it otherwise."""
     d, keep = _device(dy, "dy"), []
-    act = _activation(activation)
+    act, rounded = _activation(activation), int(bool(round_dz))
     mdy = _matrix(dy, "dy", d, keep)
     if act and pre is None:
         raise ValueError("the activation's gradient needs pre")
@@ -228,9 +230,9 @@ def wfst_am_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Opti
     head = (*mdy, *mpre, *mx, *mw, *(_NONE if dx is None else _matrix(dx, "dx", d)),
             *(_NONE if dw is None else _matrix(dw, "dw", d)), 0 if db is None else db.data_ptr())
     pack = _PACK["linear_backward"].pack
-    need = _bytes_for("wfst_am_linear_backward_workspace", pack(*head, 0, 0, act, 0))
+    need = _bytes_for("wfst_am_linear_backward_workspace", pack(*head, 0, 0, act, rounded))
     work = dy.new_empty(need, dtype=torch.uint8) if need else None
-    _call("wfst_am_linear_backward", pack(*head, work.data_ptr() if need else 0, need, act, 0), _raw_stream(d))
+    _call("wfst_am_linear_backward", pack(*head, work.data_ptr() if need else 0, need, act, rounded), _raw_stream(d))
     return dx, dw, db
 
 

@@ -135,6 +135,7 @@ bool check_sizes(Checks &c, const wfst_am_linear_backward_args &a)
 {
     const int64_t M = a.dy.rows, N = a.dy.cols;
     if (!c.product_dims(M, N) || !c.need(good_activation(a.activation), "unknown activation")) return false;
+    if (!c.need(a.round_dz == 0 || a.round_dz == 1, "round_dz must be 0 or 1")) return false;
     if (!c.need(a.dy.type == WFST_F16 || a.dy.type == WFST_BF16, "dy has a type that is not taken here")) return false;
     if (a.dx.data && !c.product_dims(M, a.dx.cols)) return false;
     return !a.dw.data || c.product_dims(N, a.dw.cols);

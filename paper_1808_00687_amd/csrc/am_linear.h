@@ -18,10 +18,19 @@ void am_product_dw(const AmProduct &p, int32_t tile, hipStream_t st);
 // row stride of dz in the workspace: rows on 16 bytes
 constexpr int64_t am_dz_stride(int64_t n) { return (n + 7) & ~int64_t{7}; }
 
-// The workspace: dz (where the activation has a slope), then room that the
-// column sums and each product's parts use one after the other.
+// Is dz held in two 16-bit parts?  One holds all of dy times a slope of 0 or 1.
+inline bool am_dz_in_parts(const wfst_am_linear_backward_args &a)
+{
+    return !a.round_dz && (a.activation == WFST_ACT_SILU || a.activation == WFST_ACT_GELU);
+}
+
+// The workspace: dz (where the activation has a slope; the low parts behind the
+// high ones), then room that the column sums and each product's parts use one
+// after the other.
 struct BackwardPlan {
-    int64_t dz_bytes, partial_bytes;
+    int64_t dz_bytes;   // of one part
+    int32_t dz_parts;
+    int64_t partial_bytes;
     AmPlan dx, dw;
     int32_t across;   // threads side by side in the pass over dy
     int64_t strips;   // of rows, in that pass
@@ -30,7 +39,7 @@ struct BackwardPlan {
 inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a)
 {
     const int64_t M = a.dy.rows, N = a.dy.cols;
-    BackwardPlan p{0, 0, {64, 1}, {64, 1}, 1, 1};
+    BackwardPlan p{0, am_dz_in_parts(a) ? 2 : 1, 0, {64, 1}, {64, 1}, 1, 1};
     while (p.across < 64 && p.across * 8 < N) p.across *= 2;
     // 4 rows a thread at least, about 1,024 workgroups at most
     const int64_t wide = (N + p.across * 8 - 1) / (p.across * 8), tall = M * p.across / 1024, most = 1024 / wide;
@@ -40,12 +49,12 @@ inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a)
     if (a.activation != WFST_ACT_NONE && (a.dx.data || a.dw.data)) p.dz_bytes = (M * am_dz_stride(N) * 2 + 255) & ~int64_t{255};
     const bool whole = N % 8 == 0;   // rows of dz are
     if (a.dx.data) {
-        p.dx = am_plan(M, a.dx.cols, N, true, whole && a.dx.cols % 8 == 0);
+        p.dx = am_plan(M, a.dx.cols, N * p.dz_parts, true, whole && a.dx.cols % 8 == 0);
         const int64_t b = am_partial_bytes(M, a.dx.cols, p.dx.splits);
         p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
     }
     if (a.dw.data) {
-        p.dw = am_plan(N, a.dw.cols, M, true, whole && a.dw.cols % 8 == 0);
+        p.dw = am_plan(N, a.dw.cols, M * p.dz_parts, true, whole && a.dw.cols % 8 == 0);
         const int64_t b = am_partial_bytes(N, a.dw.cols, p.dw.splits);
         p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
     }

@@ -38,12 +38,12 @@ __global__ __launch_bounds__(256) void join_kernel(AmProduct p)
     }
 }
 
-// dz = dy * act'(pre) in the operands' type, and sums of the unrounded dz over
-// a strip of rows.  8 columns a thread; `across` threads (a power of two) side
+// dz = dy * act'(pre) in the operands' type, or in two values of it (dz_low is
+// not NULL), and sums of the unrounded dz over a strip of rows.  8 columns a thread; `across` threads (a power of two) side
 // by side, 256 / across rows at a time.  sums: [strips][N].  Bound by memory:
 // (16384, 4096) bf16 85 us, 403 MB, 4.7 TB/s.
 template <typename T>
-__global__ __launch_bounds__(256) void slope_kernel(wfst_am_linear_backward_args a, T *dz, float *sums, int across)
+__global__ __launch_bounds__(256) void slope_kernel(wfst_am_linear_backward_args a, T *dz, T *dz_low, float *sums, int across)
 {
     __shared__ float part[256][9];
     const int64_t M = a.dy.rows, N = a.dy.cols, ld = am_dz_stride(N);
@@ -60,7 +60,19 @@ __global__ __launch_bounds__(256) void slope_kernel(wfst_am_linear_backward_args
                 load_floats(static_cast<const T *>(a.pre.data) + m * a.pre.row_stride + n, N - n, z);
 #pragma unroll
                 for (int e = 0; e < 8; e++) g[e] *= slope(z[e], a.activation);
-                if (dz) store_floats(dz + m * ld + n, N - n, g);
+                if (dz_low) {
+                    float high[8], low[8];
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        high[e] = g[e] * (1.0f / AmParts<T>::kHigh);
+                        const float held = static_cast<float>(static_cast<T>(high[e])) * AmParts<T>::kHigh;
+                        low[e] = fabsf(held) < INFINITY ? (g[e] - held) * (1.0f / AmParts<T>::kLow) : 0.0f;
+                    }
+                    store_floats(dz + m * ld + n, N - n, high);
+                    store_floats(dz_low + m * ld + n, N - n, low);
+                } else if (dz) {
+                    store_floats(dz + m * ld + n, N - n, g);
+                }
             }
 #pragma unroll
             for (int e = 0; e < 8; e++) sum[e] += g[e];
@@ -85,18 +97,21 @@ void launch_backward(const wfst_am_linear_backward_args &a, hipStream_t st)
     const BackwardPlan plan = am_backward_plan(a);
     char *work = static_cast<char *>(a.workspace);
     T *dz = plan.dz_bytes ? reinterpret_cast<T *>(work) : nullptr;
-    float *sums = a.dbias ? plan.strips > 1 ? reinterpret_cast<float *>(work + plan.dz_bytes) : a.dbias : nullptr;
+    T *dz_low = dz && plan.dz_parts > 1 ? reinterpret_cast<T *>(work + plan.dz_bytes) : nullptr;
+    work += plan.dz_bytes * plan.dz_parts;
+    float *sums = a.dbias ? plan.strips > 1 ? reinterpret_cast<float *>(work) : a.dbias : nullptr;
     if (a.dbias || dz) {
         const dim3 grid(static_cast<unsigned>((N + plan.across * 8 - 1) / (plan.across * 8)), static_cast<unsigned>(plan.strips));
-        slope_kernel<T><<<grid, 256, 0, st>>>(a, dz, sums, plan.across);
+        slope_kernel<T><<<grid, 256, 0, st>>>(a, dz, dz_low, sums, plan.across);
         if (sums && plan.strips > 1) am_launch_column_join(sums, plan.strips, N, a.dbias, st);
     }
     const char *g = dz ? reinterpret_cast<const char *>(dz) : static_cast<const char *>(a.dy.data);
     const int64_t ld = (dz ? am_dz_stride(N) : a.dy.row_stride) * static_cast<int64_t>(sizeof(T));
-    float *partial = reinterpret_cast<float *>(work + plan.dz_bytes);   // the column sums are joined by then
+    float *partial = reinterpret_cast<float *>(work);   // the column sums are joined by then
     if (a.dx.data && M > 0) {
         AmProduct p{};
         p.a = {g, ld, static_cast<int32_t>(M)};
+        p.a_low = reinterpret_cast<const char *>(dz_low);
         p.b = {static_cast<const char *>(a.w.data), a.w.row_stride * 2, static_cast<int32_t>(a.dx.cols)};
         p.inner = static_cast<int32_t>(N);
         p.splits = plan.dx.splits;
@@ -107,6 +122,7 @@ void launch_backward(const wfst_am_linear_backward_args &a, hipStream_t st)
     if (a.dw.data) {
         AmProduct p{};
         p.a = {g, ld, static_cast<int32_t>(N)};
+        p.a_low = reinterpret_cast<const char *>(dz_low);
         p.b = {static_cast<const char *>(a.x.data), a.x.row_stride * 2, static_cast<int32_t>(a.dw.cols)};
         p.inner = static_cast<int32_t>(M);
         p.splits = plan.dw.splits;
@@ -149,7 +165,7 @@ hipError_t am_launch_linear(const wfst_am_linear_args &a, hipStream_t st)
 int64_t am_linear_backward_bytes(const wfst_am_linear_backward_args &a)
 {
     const BackwardPlan plan = am_backward_plan(a);
-    return plan.dz_bytes + plan.partial_bytes;
+    return plan.dz_bytes * plan.dz_parts + plan.partial_bytes;
 }
 
 hipError_t am_launch_linear_backward(const wfst_am_linear_backward_args &a, hipStream_t st)

@@ -76,12 +76,23 @@ struct AmOperand {
 
 struct AmProduct {
     AmOperand a, b;
+    const char *a_low;         // a's low parts (AmParts), laid out as a; NULL: a is all there is
     int32_t inner;             // k
     int32_t splits;            // parts of k, one workgroup each per tile; > 1: sums go to `partial`
     float *partial;            // [splits][a.extent][b.extent]
     const float *a_scale, *b_scale, *bias;
     wfst_matrix residual, pre, out;
     int32_t activation;
+};
+
+// A float32 operand of a product as two 16-bit values: high * kHigh + low * kLow,
+// within 2^-16 of it (bf16) or 2^-22 (f16, or 2^-35 if that is more).  f16's factors
+// keep a value times a slope (at most 1.13) below the type's largest, and the low
+// part of a small one above its smallest.
+template <typename E>
+struct AmParts {
+    static constexpr float kHigh = __is_same(E, f16) ? 2.0f : 1.0f;
+    static constexpr float kLow = __is_same(E, f16) ? 0x1p-10f : 1.0f;
 };
 
 __device__ __forceinline__ float am_silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + am_exp(-z)); }
@@ -447,7 +458,9 @@ struct AmShape {
     static constexpr int kWavesASimd = kThreads == 256 && (BM + BN) * SB * kBuffers > 80 * 1024 ? 1 : 2;
 };
 
-template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kFar = false>
+// kTwice: a is in two parts.  The whole of k is gone through twice into the same
+// sums: the low parts, a change of scale, the high parts.
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kFar, bool kTwice>
 __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(AmProduct p)
 {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub alone
@@ -474,7 +487,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
         else return b3;
     };
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane_ = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t ti, tj;
     am_tile_of(blockIdx.x, (p.a.extent + BM - 1) / BM, (p.b.extent + BN - 1) / BN, ti, tj);
     const int64_t i0 = static_cast<int64_t>(ti) * BM, j0 = static_cast<int64_t>(tj) * BN;
@@ -486,8 +499,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
 
     SideA sa;
     SideB sb;
-    sa.init_places(wi, lane);
-    sb.init_places(wj, lane);
+    sa.init_places(wi, lane_);
+    sb.init_places(wj, lane_);
     f32x4 acc[TI][TJ];
     am_each<TI>([&](auto f) { am_each<TJ>([&](auto g) { acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }); });
 
@@ -549,7 +562,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
     // operands the loop is left only after whole periods (the stages past the end
     // are zeros): every exit more costs the compiler registers, and there it
     // runs out of them.
-    int32_t s = s_first;
+    int32_t s;
     const auto all = [&](auto go) {
         [&]<int... n>(std::integer_sequence<int, n...>) {
             if constexpr (kMajorB) {
@@ -563,9 +576,15 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
         }(std::make_integer_sequence<int, kPeriod>{});
     };
 
+#pragma clang loop unroll(disable)
+    for (int part = kTwice ? 0 : 1; part < 2; part++) {
+    const AmOperand a{part ? p.a.data : p.a_low, p.a.ld, p.a.extent};
+    s = s_first;
+    int lane = lane_;   // what follows from it is computed anew for the other parts: kept, it would cost registers
+    if constexpr (kTwice) __asm__ volatile("" : "+v"(lane));
     if constexpr (kDirect) {
         const int32_t tail = (p.inner % kK) * static_cast<int32_t>(sizeof(E));
-        sa.init(p.a, wave, lane);
+        sa.init(a, wave, lane);
         sb.init(p.b, wave, lane);
         // The fetch of a stage: its descriptors, then its parts one by one.  A
         // stage that is not there is fetched from empty ranges, so that the
@@ -576,7 +595,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
                 sa.cut(tail, wave, lane);
                 sb.cut(tail, wave, lane);
             }
-            rsrc_a = sa.stage_rsrc(p.a, i0, p.inner, s * kK, s < s_last);
+            rsrc_a = sa.stage_rsrc(a, i0, p.inner, s * kK, s < s_last);
             rsrc_b = sb.stage_rsrc(p.b, j0, p.inner, s * kK, s < s_last);
         };
         constexpr int kParts = SideA::kPerWave + SideB::kPerWave, kEach = (kParts + kAhead * TJ - 1) / (kAhead * TJ);
@@ -611,11 +630,11 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
                 am_each<SideB::kPerWave>([&](auto q) { rb[q] = i32x4{0, 0, 0, 0}; });
                 return;
             }
-            sa.load(p.a, i0, p.inner, s * kK, ra, wave, lane);
+            sa.load(a, i0, p.inner, s * kK, ra, wave, lane);
             sb.load(p.b, j0, p.inner, s * kK, rb, wave, lane);
         };
         const auto put = [&](auto n, int32_t s) {
-            sa.put(p.a, i0, p.inner, s * kK, ra, place_a(n), wave, lane);
+            sa.put(a, i0, p.inner, s * kK, ra, place_a(n), wave, lane);
             sb.put(p.b, j0, p.inner, s * kK, rb, place_b(n), wave, lane);
         };
         load(s);
@@ -637,6 +656,20 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
                 return ++s < s_last;
             });
     }
+    if constexpr (kTwice) {
+        // The low parts' sums in units of the high parts.  One that is not finite has
+        // met an infinity or a NaN of b (low parts are finite), as the high parts will.
+        const float unit = part ? AmParts<E>::kHigh : AmParts<E>::kLow / AmParts<E>::kHigh;
+        am_each<TI>([&](auto f) {
+            am_each<TJ>([&](auto g) {
+                const f32x4 v = acc[f][g] * unit;
+                const auto held = [&](float u) { return part || fabsf(u) < INFINITY ? u : 0.0f; };
+                acc[f][g] = f32x4{held(v[0]), held(v[1]), held(v[2]), held(v[3])};
+            });
+        });
+        __syncthreads();   // no wave reads a stage of these any more
+    }
+    }
 
     // A lane's run of consecutive j.  With dealt rows it has 4 * TJ already; else
     // 4 fragments' values change places between the 4 groups of 16 lanes, so that
@@ -656,13 +689,13 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
                 am_set<e>(acc[f][3], w[1]);
             });
         });
-    const int64_t j = j0 + wj + (lane >> 4) * kRun;
+    const int64_t j = j0 + wj + (lane_ >> 4) * kRun;
     if (j >= p.b.extent) return;
     float b_scale[kRun], bias[kRun];
     if (p.splits == 1) am_columns(p, j, b_scale, bias);
     const wfst_matrix partial{p.partial + static_cast<int64_t>(blockIdx.y) * p.a.extent * p.b.extent, p.a.extent, p.b.extent, p.b.extent, WFST_F32, 0};
     am_each<TI>([&](auto f) {
-        const int64_t i = i0 + wi + f * 16 + (lane & 15);
+        const int64_t i = i0 + wi + f * 16 + (lane_ & 15);
         if (i >= p.a.extent) return;
         float v[kRun];
         am_each<TJ>([&](auto d) {
@@ -694,11 +727,11 @@ inline int64_t am_tiles(int64_t rows, int64_t cols, int64_t m, int64_t n) { retu
 // sums the parts of a split product and finishes them (am_linear.hip)
 void am_launch_join(const AmProduct &p, hipStream_t st);
 
-template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kFar = false>
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kTwice, bool kFar = false>
 void am_launch_tiles(const AmProduct &p, hipStream_t st)
 {
     const int64_t tiles = am_tiles(p.a.extent, p.b.extent, S::BM, S::BN);
-    am_tile_kernel<E, kMajorA, kMajorB, kDirect, S, kFar><<<dim3(static_cast<unsigned>(tiles), p.splits), S::kThreads, 0, st>>>(p);
+    am_tile_kernel<E, kMajorA, kMajorB, kDirect, S, kFar, kTwice><<<dim3(static_cast<unsigned>(tiles), p.splits), S::kThreads, 0, st>>>(p);
     if (p.splits > 1) am_launch_join(p, st);
 }
 
@@ -758,21 +791,23 @@ inline int64_t am_partial_bytes(int64_t rows, int64_t cols, int32_t splits)
     return splits > 1 ? (rows * cols * splits * 4 + 255) & ~int64_t{255} : 0;
 }
 
-template <typename E, bool kMajorA, bool kMajorB>
+template <typename E, bool kMajorA, bool kMajorB, bool kTwice = false>
 void am_product(const AmProduct &p, int32_t tile, hipStream_t st)
 {
+    if constexpr (kMajorB && !kTwice)
+        if (p.a_low) return am_product<E, kMajorA, kMajorB, true>(p, tile, st);
     if (am_direct(p.a, kMajorA, p.inner, sizeof(E)) && am_direct(p.b, kMajorB, p.inner, sizeof(E))) {
-        if (tile == 256) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<sizeof(E) == 1, AmLarge8, AmLarge>>(p, st);
+        if (tile == 256) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<sizeof(E) == 1, AmLarge8, AmLarge>, kTwice>(p, st);
         else if (tile == 128 && am_tiles(p.a.extent, p.b.extent, 128, 128) * p.splits <= kComputeUnits)
-            am_launch_tiles<E, kMajorA, kMajorB, true, AmMediumDeep>(p, st);
-        else if (tile == 128) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<kMajorB, AmMediumMajor, AmMedium>>(p, st);
-        else am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<kMajorB, AmSmallMajor, AmSmall>>(p, st);
+            am_launch_tiles<E, kMajorA, kMajorB, true, AmMediumDeep, kTwice>(p, st);
+        else if (tile == 128) am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<kMajorB, AmMediumMajor, AmMedium>, kTwice>(p, st);
+        else am_launch_tiles<E, kMajorA, kMajorB, true, std::conditional_t<kMajorB, AmSmallMajor, AmSmall>, kTwice>(p, st);
     } else if (!am_near(p.a) || !am_near(p.b)) {
-        am_launch_tiles<E, kMajorA, kMajorB, false, std::conditional_t<kMajorB, AmSmallMajorStaged, AmSmallStaged>, true>(p, st);
+        am_launch_tiles<E, kMajorA, kMajorB, false, std::conditional_t<kMajorB, AmSmallMajorStaged, AmSmallStaged>, kTwice, true>(p, st);
     } else if (tile >= 128) {
-        am_launch_tiles<E, kMajorA, kMajorB, false, AmMediumStaged>(p, st);
+        am_launch_tiles<E, kMajorA, kMajorB, false, AmMediumStaged, kTwice>(p, st);
     } else {
-        am_launch_tiles<E, kMajorA, kMajorB, false, std::conditional_t<kMajorB, AmSmallMajorStaged, AmSmallStaged>>(p, st);
+        am_launch_tiles<E, kMajorA, kMajorB, false, std::conditional_t<kMajorB, AmSmallMajorStaged, AmSmallStaged>, kTwice>(p, st);
     }
 }
 
