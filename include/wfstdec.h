@@ -671,7 +671,8 @@ int wfst_am_norm_backward(const wfst_am_norm_backward_args *args, void *hip_stre
  *   weight    [M] float32 or NULL (ones); temperature > 0, finite
  *   loss      [M] float32 output, optional
  *   lse       [M] float32 output, optional: log sum exp(logits / temperature),
- *             which wfst_am_distill_backward reads
+ *             which wfst_am_distill_backward reads; the largest finite value
+ *             where finite logits over a temperature below 1 leave the type
  *   dlogits   [M x L] output, optional, of the logits' type; may be logits
  *             itself (same data and stride)
  *
@@ -693,7 +694,9 @@ int wfst_am_distill(const wfst_am_distill_args *args, void *hip_stream);
 
 /* The gradient alone, for a loss whose weights are known only after it
    (weight[m] = the gradient that reaches loss[m], times the forward call's
-   weight): reads lse, writes dlogits; loss is not touched. */
+   weight): reads lse, writes dlogits; loss is not touched.  q is
+   exp(logits / temperature - lse) here, so its relative error is that of lse,
+   2^-24 |lse|; wfst_am_distill's own dlogits do not depend on a row's offset. */
 int wfst_am_distill_backward(const wfst_am_distill_args *args, void *hip_stream);
 
 /*

@@ -167,7 +167,7 @@ __global__ __launch_bounds__(S::kThreads, kBackward && S::kTpr == 1024 && S::kNv
         // comes after the last read of the row from memory.
         float kept[S::kHeld][S::kC];
         RowStat stat{0.0f, 0.0f, 1.0f};
-        float lse = 0.0f;
+        float lse = 0.0f, log_sum = 0.0f;
         if constexpr (kBackward) {
             lse = a.lse[m];
             if (w != 0.0f) {
@@ -179,8 +179,8 @@ __global__ __launch_bounds__(S::kThreads, kBackward && S::kTpr == 1024 && S::kNv
 #pragma unroll
                     for (int i = 0; i < S::kC; i++) kept[v][i] = e[i];
             }, scratch, turn);
-            lse = lse_of(stat);
-            if (a.lse && t == 0) a.lse[m] = lse;
+            log_sum = logf(stat.sum);
+            if (a.lse && t == 0) a.lse[m] = lse_of(stat, inv_t);
         }
         if constexpr (kKeep) hold_row(m + step);
         if constexpr (S::kWaves == 1) wave_sync();
@@ -191,14 +191,14 @@ __global__ __launch_bounds__(S::kThreads, kBackward && S::kTpr == 1024 && S::kNv
                 if (live)
 #pragma unroll
                     for (int i = 0; i < kEntries; i++)   // a masked unit whose share has underflowed is worth nothing
-                        if (share[i] != 0.0f) sum += share[i] * ((top[i] - log_z) - (at_unit[i] * inv_t - lse));
+                        if (share[i] != 0.0f) sum += w * temp * share[i] * (temp * ((top[i] - log_z) + log_sum) - (at_unit[i] - stat.top));
                 sum = wave_sum(sum);
-                if (t == 0) a.loss[m] = live ? w * temp * temp * sum : 0.0f;
+                if (t == 0) a.loss[m] = live ? sum : 0.0f;
             }
         if (d) {
             const float scale = w * temp;
-            // q = 2^(y - own) * over, or e^(x / temperature - lse)
-            const float over = kBackward ? 0.0f : scale * (__builtin_amdgcn_exp2f(stat.own - stat.top) / stat.sum);
+            // q = e^((x - own) / temperature) * over (kept), e^((x - top) / temperature) * over, or e^(x / temperature - lse)
+            const float over = scale * ((kKeep ? __builtin_amdgcn_exp2f((stat.own - stat.top) * c2) : 1.0f) / stat.sum);
             if (live) {
                 const int32_t own = head;
                 S::each(L, t, [&](int v, int64_t c, int64_t left) {
@@ -209,7 +209,8 @@ __global__ __launch_bounds__(S::kThreads, kBackward && S::kTpr == 1024 && S::kNv
                     } else {
                         get_x(v, c, left, g);
 #pragma unroll
-                        for (int e = 0; e < S::kC; e++) g[e] = scale * am_exp(g[e] * inv_t - lse);
+                        for (int e = 0; e < S::kC; e++)
+                            g[e] = kBackward ? scale * am_exp(tempered(g[e], inv_t) - lse) : __builtin_amdgcn_exp2f((g[e] - stat.top) * c2) * over;
                     }
                     for (int j = own; j >= 0; j = tab.next[j]) {
                         const int64_t at = tab.unit[j] - c;

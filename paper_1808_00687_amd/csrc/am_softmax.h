@@ -11,16 +11,19 @@ __device__ __forceinline__ const T *row(const wfst_matrix &m, int64_t r)
     return static_cast<const T *>(m.data) + r * m.row_stride;
 }
 
-constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+constexpr float kLog2e = 1.44269504f;
+constexpr float kFloatMax = 3.40282347e38f;
 
-// A row's softmax statistics in base 2, with y = x * c and c = log2(e) / temperature:
+// A row's softmax statistics.  The maximum is subtracted before anything is scaled,
+// so they do not change with an offset of the row, however large: its exponent is 0.
 struct RowStat {
-    float top;    // largest y; 0 for a row of -inf
-    float own;    // largest y of the thread's wave, likewise: what `keep` got is relative to it
-    float sum;    // of 2^(y - top)
+    float top;    // largest x; 0 for a row of -inf
+    float own;    // largest x of the thread's wave, likewise: what `keep` got is relative to it
+    float sum;    // of e^((x - top) / temperature)
 };
 
-// get(v, column, left, x): a chunk, -inf beyond the row.  keep(v, e): 2^(y - own) of the chunk.
+// get(v, column, left, x): a chunk, -inf beyond the row.  c: log2(e) / temperature.
+// keep(v, e): e^((x - own) / temperature) of the chunk.
 template <typename S, typename G, typename K>
 __device__ __forceinline__ RowStat row_stat(int64_t cols, int t, float c, G get, K keep, RowScratch &r, int &turn)
 {
@@ -31,7 +34,7 @@ __device__ __forceinline__ RowStat row_stat(int64_t cols, int t, float c, G get,
 #pragma unroll
         for (int e = 0; e < S::kC; e++) top = fmaxf(top, x[e]);
     });
-    top = wave_max(top) * c;
+    top = wave_max(top);
     RowStat o;
     o.own = top == -INFINITY ? 0.0f : top;
     float s = 0.0f;
@@ -40,7 +43,7 @@ __device__ __forceinline__ RowStat row_stat(int64_t cols, int t, float c, G get,
         get(v, at, left, x);
 #pragma unroll
         for (int e = 0; e < S::kC; e++) {
-            x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], c, -o.own));
+            x[e] = __builtin_amdgcn_exp2f((x[e] - o.own) * c);
             s += x[e];
         }
         keep(v, x);
@@ -57,7 +60,7 @@ __device__ __forceinline__ RowStat row_stat(int64_t cols, int t, float c, G get,
         s = 0.0f;
 #pragma unroll
         for (int i = 0; i < S::kWaves; i++)   // a wave of -inf has sum 0
-            s += r.a[turn][i] == -INFINITY ? r.b[turn][i] : r.b[turn][i] * __builtin_amdgcn_exp2f(r.a[turn][i] - o.top);
+            s += r.a[turn][i] == -INFINITY ? r.b[turn][i] : r.b[turn][i] * __builtin_amdgcn_exp2f((r.a[turn][i] - o.top) * c);
         turn ^= 1;
     } else {
         o.top = o.own;
@@ -66,8 +69,15 @@ __device__ __forceinline__ RowStat row_stat(int64_t cols, int t, float c, G get,
     return o;
 }
 
+// x / temperature; of a finite x never an infinity (a mask's lowest value, a temperature below 1)
+__device__ __forceinline__ float tempered(float x, float inv_t)
+{
+    const float y = x * inv_t;
+    return fabsf(x) <= kFloatMax ? fminf(fmaxf(y, -kFloatMax), kFloatMax) : y;
+}
+
 // log sum exp of x / temperature; -inf for a row of -inf
-__device__ __forceinline__ float lse_of(const RowStat &s) { return s.top * kLn2 + logf(s.sum); }
+__device__ __forceinline__ float lse_of(const RowStat &s, float inv_t) { return tempered(s.top, inv_t) + logf(s.sum); }
 
 constexpr int64_t kSoftmaxBlocks = 256 * 4;
 
