@@ -51,13 +51,12 @@ def check_distill(am, x, idx, top, t, tag):
     log_q = (y - log_sum).gather(1, at)
     want = t * t * (torch.xlogy(p, p) - torch.where(p > 0, p * log_q, torch.zeros_like(p))).sum(1)
     dl = t * (q.scatter_add(1, at, -p))
-    want = torch.where(want > MOST, torch.full_like(want, INF), want)   # the loss is a float32
     loss, lse, got = am.wfst_am_distill(inside(x), idx.cuda(), inside(top), temperature=t, gradient=True)
     e_p = R.U32 * (16 * (R.d(top).abs().amax(1, keepdim=True) / t + 1) + R.LAMBDA * math.sqrt(idx.shape[1]))
     e_q = err + 4 * R.U32 * (y.abs() + 1)
     bound = t * t * (2 * (p * (e_p + e_q.gather(1, at)) + 4 * e_p * p * (log_q.abs() + 1 + torch.log(p).abs().nan_to_num(0, 0, 0))).sum(1))
     bound = bound + R.U32 * want.abs()
-    loss = torch.where((loss.cpu() == INF) & (want + bound > MOST), want, loss.cpu())   # what the bound allows may overflow
+    loss = torch.where((loss.cpu() == INF) & (want + bound > MOST), want, loss.cpu().double())   # the loss is a float32
     R.close(loss, want, bound, tag + " loss")
     bound = t * (2 * q * e_q + 4 * R.U32 * (q + dl.abs() / t) + torch.zeros_like(q).scatter_add(1, at, 2 * e_p * p + R.U32 * p))
     R.close(got, dl, bound + R.U[x.dtype] * (dl.abs() + bound) + R.TINY[x.dtype], tag + " dlogits")
