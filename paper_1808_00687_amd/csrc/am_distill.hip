@@ -76,7 +76,7 @@ __global__ __launch_bounds__(S::kThreads, kBackward && S::kTpr == 1024 && S::kNv
             const int j = i * 64 + t;
             if (i * 64 >= k) continue;
             unit_next[i] = j < k ? a.top_index[r * k + j] : -1;
-            top_next[i] = j < k ? load_any(a.top_logit, r, j) * inv_t : -INFINITY;
+            top_next[i] = j < k ? load_any(a.top_logit, r, j) : -INFINITY;
         }
     };
     const auto hold_units = [&](int64_t r) {
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(S::kThreads, kBackward && S::kTpr == 1024 && S::kNv
                 share[i] = 0.0f;
                 if (unit[i] < 0) continue;
                 used = true;
-                top[i] -= best;
+                top[i] = (top[i] - best) * inv_t;
                 share[i] = am_exp(top[i]);
                 z += share[i];
             }

@@ -125,3 +125,29 @@ def test_filled_rows_are_rows_that_the_search_takes(am):
     r = wfstdec.wfst_decode(graph, am.wfst_am_loglikes(x), wl.opts.beam, max_active=300, lattice_beam=6.0)
     graph.free()
     assert r.status == 0 and math.isfinite(r.cost) and r.num_decoded == 20
+
+
+@pytest.mark.parametrize("k", [5, 70])
+@pytest.mark.parametrize("t", [1.0, 0.25, 3.0])
+def test_teacher_logits_far_from_zero(am, t, k):
+    # what the entries add up to does not change with their offset, which these sums hold exactly
+    g = rng(k)
+    n = 300
+    x = normal(g, 1, n).expand(5, n).contiguous()
+    idx = top_entries(g, 1, n, k)[0].expand(5, k).contiguous()
+    top = torch.randint(-9, 10, (1, k), generator=g).float() + torch.tensor([[0.0], [-2.0 ** 20], [2.0 ** 22], [-77.0], [5e5]])
+    loss, _, dl = am.wfst_am_distill(x.cuda(), idx.cuda(), top.cuda(), temperature=t, gradient=True)
+    for m in range(1, 5):
+        assert torch.equal(loss[m], loss[0]) and torch.equal(dl[m], dl[0]), m
+    # entries of one finite value share alike, the type's lowest and largest among them
+    top = torch.tensor([0.0, torch.finfo(F32).min, MOST, -1e12, 3e38])[:, None].expand(5, k).contiguous()
+    loss, _, dl = am.wfst_am_distill(x.cuda(), idx.cuda(), top.cuda(), temperature=t, gradient=True)
+    assert float(loss[0]) > 0
+    for m in range(1, 5):
+        assert torch.equal(loss[m], loss[0]) and torch.equal(dl[m], dl[0]), m
+    # masked by the lowest value, one left
+    top[:, :] = torch.finfo(F32).min
+    top[:, 3] = 1.0
+    loss, _, dl = am.wfst_am_distill(x.cuda(), idx.cuda(), top.cuda(), temperature=t, gradient=True)
+    one = am.wfst_am_distill(x.cuda(), idx[:, 3:4].contiguous().cuda(), top[:, 3:4].contiguous().cuda(), temperature=t, gradient=True)
+    assert torch.equal(loss, one[0]) and torch.equal(dl, one[2])
