@@ -668,7 +668,7 @@ int wfst_am_norm_backward(const wfst_am_norm_backward_args *args, void *hip_stre
  *   logits    [M x L] WFST_F32, WFST_F16 or WFST_BF16; M >= 0, L >= 1
  *   top_logit [M x k] of any of these types, 1 <= k <= 256
  *   top_index [M x k] int32, dense
- *   weight    [M] float32 or NULL (ones); temperature > 0, finite
+ *   weight    [M] float32 or NULL (ones); temperature > 0, finite, not subnormal
  *   loss      [M] float32 output, optional
  *   lse       [M] float32 output, optional: log sum exp(logits / temperature),
  *             which wfst_am_distill_backward reads; the largest finite value

@@ -223,7 +223,8 @@ bool check(Checks &c, const wfst_am_distill_args &a, bool backward)
 {
     const int64_t M = a.logits.rows, L = a.logits.cols, k = a.top_logit.cols;
     if (!c.dims(M, L)) return false;
-    if (!c.need(std::isfinite(a.temperature) && a.temperature > 0.0f, "temperature must be positive and finite")) return false;
+    // (the reciprocal of a subnormal one is no float32)
+    if (!c.need(std::isnormal(a.temperature) && a.temperature > 0.0f, "temperature must be positive, finite and normal")) return false;
     if (!c.need(k >= 1 && k <= WFST_AM_MAX_TOP, "the teacher's entries must be 1 to 256 a row")) return false;
     if (!c.matrix(a.logits, "logits", M, L, kFloats) || !c.matrix(a.top_logit, "top_logit", M, k, kFloats)) return false;
     if ((backward || a.dlogits.data) && !c.matrix(a.dlogits, "dlogits", M, L, 1u << a.logits.type)) return false;

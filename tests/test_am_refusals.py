@@ -19,3 +19,8 @@ def refused(am, name, **change):  # noqa: F811
 @pytest.mark.parametrize("value", [-1, 2])
 def test_round_dz_is_zero_or_one(am, value):  # noqa: F811
     assert refused(am, "linear_backward", round_dz=value)
+
+
+@pytest.mark.parametrize("name", ["distill", "distill_backward"])
+def test_temperature_has_a_reciprocal(am, name):  # noqa: F811
+    assert refused(am, name, temperature=2.0 ** -127)
