@@ -74,7 +74,8 @@ __global__ __launch_bounds__(S::kThreads) void norm_kernel(wfst_am_norm_args a)
             for (int e = 0; e < S::kC; e++) ss = fmaf(s[e], s[e], ss);
         });
         const float rho = 1.0f / sqrtf(row_sum<S>(ss, scratch, turn) / static_cast<float>(D) + a.eps);
-        float inv = 1.0f;
+        float scale = 1.0f, inv = 1.0f;
+        bool whole = false;   // is a quotient formed by a division?
         if constexpr (k8Bits) {
             uint32_t top = 0;
             S::each(D, t, [&](int v, int64_t c, int64_t left) {
@@ -89,9 +90,13 @@ __global__ __launch_bounds__(S::kThreads) void norm_kernel(wfst_am_norm_args a)
                     top = e < left && b > top ? b : top;
                 }
             });
-            float scale = __uint_as_float(row_max_u32<S>(top, scratch, turn)) / kE4m3Max;
+            scale = __uint_as_float(row_max_u32<S>(top, scratch, turn)) / kE4m3Max;
             scale = scale < 1.17549435e-38f ? 1.17549435e-38f : scale;   // a NaN stays one
+            // A product with the rounded reciprocal, corrected once, is the rounded quotient
+            // (Markstein 1990) unless the divisor's bits are all ones or something leaves the
+            // range; 72.8 us for (53274, 1024) bf16, 74.5 with divisions.
             inv = 1.0f / scale;
+            whole = __builtin_amdgcn_readfirstlane(!(scale >= 0x1p-90f && scale <= 0x1p90f) || (__float_as_uint(scale) & 0x7FFFFFu) == 0x7FFFFFu) != 0;
             if (t == 0) a.y_scale[m] = scale;
         }
         S::each(D, t, [&](int v, int64_t c, int64_t left) {
@@ -102,8 +107,15 @@ __global__ __launch_bounds__(S::kThreads) void norm_kernel(wfst_am_norm_args a)
             for (int e = 0; e < S::kC; e++) s[e] *= rho;
             times_gain(v, c, left, s);
             if constexpr (k8Bits) {
+                if (whole)
 #pragma unroll
-                for (int e = 0; e < S::kC; e++) s[e] *= inv;
+                    for (int e = 0; e < S::kC; e++) s[e] /= scale;
+                else
+#pragma unroll
+                    for (int e = 0; e < S::kC; e++) {
+                        const float q = s[e] * inv;   // alone it would move ties of e4m3
+                        s[e] = fmaf(fmaf(-q, scale, s[e]), inv, q);
+                    }
                 store_floats(row_out<f8>(a.y, m) + c, left, s);
             } else if (a.y.type == WFST_BF16) {
                 store_floats(row_out<bf16>(a.y, m) + c, left, s);
