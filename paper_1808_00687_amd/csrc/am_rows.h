@@ -2,9 +2,10 @@
 // reductions over a row.
 //
 // A row belongs to TPR threads (a wave, 256 or 1024), C consecutive columns at
-// a time: chunk c is thread c % TPR's.  C is 8 where every matrix has 16-bit
-// elements and 4 where one has 32-bit ones, so that no access is wider than 16
-// bytes and neighbouring lanes' accesses touch.  With NV > 0 a thread holds its
+// a time: chunk c is thread c % TPR's.  C is 8 where every matrix has at most 16-bit
+// elements and 4 where one has 32-bit ones, so that no access to a matrix is wider
+// than 16 bytes and neighbouring lanes' accesses touch.  (Vectors are 32-bit in
+// either case; a workgroup reads them once.)  With NV > 0 a thread holds its
 // NV chunks in registers, as they are in memory, so a row is read once; with
 // NV = 0 the row is too long for that and every pass reads it again.
 #pragma once
