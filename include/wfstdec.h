@@ -538,7 +538,8 @@ typedef struct wfst_matrix {
  *   y[m][n] = act(z[m][n]) + residual[m][n]
  *
  *   x        [M x K], w [N x K], of one type: WFST_F16, WFST_BF16 or
- *            WFST_F8E4M3; M >= 0, K >= 1, N >= 1, each at most 2^30
+ *            WFST_F8E4M3; M >= 0, K >= 1, N >= 1, each at most 2^30, and no
+ *            matrix of more than 2^40 elements
  *   residual [M x N] optional, of y's type; may be y itself (same data,
  *            stride and type)
  *   pre      [M x N] optional output: z, of y's type (for the gradient)

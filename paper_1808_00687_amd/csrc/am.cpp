@@ -47,11 +47,12 @@ struct Checks {
         return need(rows >= 0 && rows <= INT32_MAX && cols >= 1 && cols <= INT32_MAX,
                     "rows must be in [0, 2^31) and columns in [1, 2^31)");
     }
-    // of a product: tiles past the end stay in 31 bits
+    // of a product: rows and columns of tiles past the end, and the tiles' number, stay in 31 bits
     bool product_dims(int64_t rows, int64_t cols)
     {
-        constexpr int64_t kMost = int64_t{1} << 30;
-        return dims(rows, cols) && need(rows <= kMost && cols <= kMost, "rows and columns of a product must be at most 2^30");
+        constexpr int64_t kMost = int64_t{1} << 30, kValues = int64_t{1} << 40;
+        return dims(rows, cols) && need(rows <= kMost && cols <= kMost, "rows and columns of a product must be at most 2^30") &&
+               need(rows * cols <= kValues, "a matrix of a product must have at most 2^40 elements");
     }
     bool vector(const void *p, const char *name, bool wanted)
     {
@@ -111,7 +112,7 @@ bool check(Checks &c, const wfst_am_linear_args &a)
 {
     const int64_t M = a.x.rows, K = a.x.cols, N = a.w.rows;
     const bool f8 = a.x.type == WFST_F8E4M3;
-    if (!c.product_dims(M, K) || !c.product_dims(M, N)) return false;
+    if (!c.product_dims(M, K) || !c.product_dims(M, N) || !c.product_dims(N, K)) return false;
     if (!c.need(good_activation(a.activation), "unknown activation")) return false;
     if (!c.matrix(a.x, "x", M, K, kHalves | 1u << WFST_F8E4M3)) return false;
     if (!c.matrix(a.w, "w", N, K, 1u << a.x.type)) return false;

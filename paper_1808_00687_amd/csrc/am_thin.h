@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void am_thin_kernel(AmProduct p
     __shared__ float part[kThinWaves][kRows][kCols + 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, s = lane & 15;
     const int64_t tiles_j = (static_cast<int64_t>(p.b.extent) + kCols - 1) / kCols;
-    const int64_t i0 = blockIdx.x / tiles_j * kRows, j0 = blockIdx.x % tiles_j * kCols;
+    const int64_t block = p.first + blockIdx.x, i0 = block / tiles_j * kRows, j0 = block % tiles_j * kCols;
 
     int64_t row_a[TI], row_b[TJ];   // past the end: the last row again, whose results are not stored
     am_each<TI>([&](auto f) { row_a[f] = i0 + f * 16 + s < p.a.extent ? i0 + f * 16 + s : p.a.extent - 1; });
@@ -110,8 +110,11 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void am_thin_kernel(AmProduct p
 template <typename E, int TI, int TJ>
 void am_launch_thin(const AmProduct &p, hipStream_t st)
 {
-    const int64_t n = am_tiles(p.a.extent, p.b.extent, TI * 16, TJ * 16);
-    am_thin_kernel<E, TI, TJ><<<static_cast<unsigned>(n), kThinWaves * 64, 0, st>>>(p);
+    am_in_launches(am_tiles(p.a.extent, p.b.extent, TI * 16, TJ * 16), [&](uint32_t first, uint32_t blocks) {
+        AmProduct part = p;
+        part.first = first;
+        am_thin_kernel<E, TI, TJ><<<blocks, kThinWaves * 64, 0, st>>>(part);
+    });
 }
 
 // The fragments of a workgroup: a CU takes in about 45 bytes a nanosecond

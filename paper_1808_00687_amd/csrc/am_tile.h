@@ -46,6 +46,7 @@
 #include <utility>
 
 #include "am_device.h"
+#include "am_plan.h"
 
 namespace wfd {
 
@@ -68,12 +69,6 @@ __device__ __forceinline__ void am_each(F use)
     am_each<N>(use, std::make_integer_sequence<int, N>{});
 }
 
-struct AmOperand {
-    const char *data;
-    int64_t ld;        // bytes between rows as stored
-    int32_t extent;    // i or j
-};
-
 struct AmProduct {
     AmOperand a, b;
     const char *a_low;         // a's low parts (AmParts), laid out as a; NULL: a is all there is
@@ -83,6 +78,7 @@ struct AmProduct {
     const float *a_scale, *b_scale, *bias;
     wfst_matrix residual, pre, out;
     int32_t activation;
+    uint32_t first;            // tile of the launch's first workgroup
 };
 
 // A float32 operand of a product as two 16-bit values: high * kHigh + low * kLow,
@@ -492,7 +488,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
 
     const int lane_ = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t ti, tj;
-    am_tile_of(blockIdx.x, (p.a.extent + BM - 1) / BM, (p.b.extent + BN - 1) / BN, ti, tj);
+    am_tile_of(p.first + blockIdx.x, (p.a.extent + BM - 1) / BM, (p.b.extent + BN - 1) / BN, ti, tj);
     const int64_t i0 = static_cast<int64_t>(ti) * BM, j0 = static_cast<int64_t>(tj) * BN;
     const int wi = wave / WN * (BM / S::WM), wj = wave % WN * (BN / WN);
 
@@ -715,26 +711,17 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
 // host side
 // --------------------------------------------------------------------------
 
-// offsets inside a tile of 256 rows stay in 31 bits
-inline bool am_near(const AmOperand &o) { return o.ld < (int64_t{1} << 22); }
-
-// 16-byte fetches: rows aligned and ending on 16 bytes
-inline bool am_direct(const AmOperand &o, bool major, int32_t inner, int el)
-{
-    const int64_t row = static_cast<int64_t>(major ? o.extent : inner) * el;
-    return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && row % 16 == 0 && am_near(o);
-}
-
-inline int64_t am_tiles(int64_t rows, int64_t cols, int64_t m, int64_t n) { return ((rows + m - 1) / m) * ((cols + n - 1) / n); }
-
 // sums the parts of a split product and finishes them (am_linear.hip)
 void am_launch_join(const AmProduct &p, hipStream_t st);
 
 template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kTwice, bool kFar = false>
 void am_launch_tiles(const AmProduct &p, hipStream_t st)
 {
-    const int64_t tiles = am_tiles(p.a.extent, p.b.extent, S::BM, S::BN);
-    am_tile_kernel<E, kMajorA, kMajorB, kDirect, S, kFar, kTwice><<<dim3(static_cast<unsigned>(tiles), p.splits), S::kThreads, 0, st>>>(p);
+    am_in_launches(am_tiles(p.a.extent, p.b.extent, S::BM, S::BN), [&](uint32_t first, uint32_t blocks) {
+        AmProduct part = p;
+        part.first = first;
+        am_tile_kernel<E, kMajorA, kMajorB, kDirect, S, kFar, kTwice><<<dim3(blocks, p.splits), S::kThreads, 0, st>>>(part);
+    });
     if (p.splits > 1) am_launch_join(p, st);
 }
 
@@ -748,51 +735,6 @@ using AmSmallMajor = AmShape<64, 64, 1, 4, 128, 4>;
 using AmMediumStaged = AmShape<128, 128, 2, 2, 64, 2>;
 using AmSmallStaged = AmShape<64, 64, 2, 2, 128, 2>;
 using AmSmallMajorStaged = AmShape<64, 64, 1, 4, 128, 2>;
-
-constexpr int64_t kComputeUnits = 256;
-
-// Which tiles, and into how many parts k is split.
-struct AmPlan {
-    int32_t tile;     // 256, 128 or 64
-    int32_t splits;
-};
-
-// By an estimate of the time: rounds of workgroups over the chip times stages
-// times what a stage of 64 values of k takes (measured, in microseconds, with one,
-// two, ... workgroups on a CU, as many as fit).  A product that may be split (no
-// epilogue, a workspace) also pays the join of its parts: 8 bytes a part and value,
-// and a launch.  128 x 128 tiles that are at most one a CU have stages of twice the
-// length, four of them: with the shorter ones a CU waits for memory ((4096, 1024,
-// 1024) 19.4 us, so 16.2; (2048, 1024, 2048) 18.6 and 15.8; the gradient of x of
-// (3000, 1024, 2048) 34.1 and 27.9).  Where rows are no multiple of 16 bytes (not
-// `whole`) stages go through registers and that does not hold.
-inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split, bool whole)
-{
-    constexpr struct {
-        int32_t tile;
-        int64_t fit, most;   // workgroups on a CU, and on the chip
-        double stage[3];
-    } kinds[] = {{256, 1, INT64_MAX, {1.45}}, {128, 1, kComputeUnits, {0.95}}, {128, 3, INT64_MAX, {1.5, 1.9, 2.3}}, {64, 2, INT64_MAX, {0.5, 0.55}}};
-    const int64_t stages = (inner + 63) / 64;
-    AmPlan best{64, 1};
-    double least = 1e30;
-    for (const auto &k : kinds)
-        for (int32_t s = 1; s <= (may_split ? 64 : 1) && (s == 1 || stages / s >= 4); s *= 2) {
-            const int64_t n = am_tiles(rows, cols, k.tile, k.tile) * s, at_once = kComputeUnits * k.fit, rest = n % at_once;
-            if (n > k.most || (!whole && k.most == kComputeUnits)) break;
-            double t = static_cast<double>(n / at_once) * k.stage[k.fit - 1];
-            if (rest) t += k.stage[(rest - 1) / kComputeUnits];
-            t *= static_cast<double>((stages + s - 1) / s);
-            if (s > 1) t += 5.0 + static_cast<double>(rows) * static_cast<double>(cols) * 8.0 * s / 4e6;
-            if (t < least) least = t, best = {k.tile, s};
-        }
-    return best;
-}
-
-inline int64_t am_partial_bytes(int64_t rows, int64_t cols, int32_t splits)
-{
-    return splits > 1 ? (rows * cols * splits * 4 + 255) & ~int64_t{255} : 0;
-}
 
 template <typename E, bool kMajorA, bool kMajorB, bool kTwice = false>
 void am_product(const AmProduct &p, int32_t tile, hipStream_t st)

@@ -24,3 +24,11 @@ def test_round_dz_is_zero_or_one(am, value):  # noqa: F811
 @pytest.mark.parametrize("name", ["distill", "distill_backward"])
 def test_temperature_has_a_reciprocal(am, name):  # noqa: F811
     assert refused(am, name, temperature=2.0 ** -127)
+
+
+def test_products_of_more_elements_than_any_memory(am):  # noqa: F811
+    for change in ({"x__rows": 1 << 30, "y__rows": 1 << 30, "w__rows": 1 << 11, "y__cols": 1 << 11, "y__row_stride": 1 << 11},
+                   {"w__rows": 1 << 30, "x__rows": 1 << 11, "y__rows": 1 << 11, "y__cols": 1 << 30, "y__row_stride": 1 << 30}):
+        assert refused(am, "linear", residual__data=None, pre__data=None, **change)
+        from paper_1808_00687_amd import wfstdec
+        assert "2^40" in wfstdec.wfst_last_error()
