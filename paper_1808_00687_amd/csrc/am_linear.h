@@ -47,15 +47,21 @@ inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a)
     if (p.strips < 1) p.strips = 1;
     if (a.dbias && p.strips > 1) p.partial_bytes = (p.strips * N * 4 + 255) & ~int64_t{255};
     if (a.activation != WFST_ACT_NONE && (a.dx.data || a.dw.data)) p.dz_bytes = (M * am_dz_stride(N) * 2 + 255) & ~int64_t{255};
-    const bool whole = N % 8 == 0;   // rows of dz are
+    // dz in the workspace is aligned whatever its address
+    const AmOperand dz = p.dz_bytes ? AmOperand{nullptr, am_dz_stride(N) * 2, 0}
+                                    : AmOperand{static_cast<const char *>(a.dy.data), a.dy.row_stride * 2, 0};
+    const auto rows_of = [](AmOperand o, int64_t extent) { return AmOperand{o.data, o.ld, static_cast<int32_t>(extent)}; };
+    const auto other = [](const wfst_matrix &m, int64_t cols) {
+        return AmOperand{static_cast<const char *>(m.data), m.row_stride * 2, static_cast<int32_t>(cols)};
+    };
     if (a.dx.data) {
-        p.dx = am_plan(M, a.dx.cols, N * p.dz_parts, true, whole && a.dx.cols % 8 == 0);
-        const int64_t b = am_partial_bytes(M, a.dx.cols, p.dx.splits);
+        p.dx = am_plan(rows_of(dz, M), false, other(a.w, a.dx.cols), true, N, 2, p.dz_parts, true);
+        const int64_t b = am_most_partial_bytes(M, a.dx.cols, N * p.dz_parts);
         p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
     }
     if (a.dw.data) {
-        p.dw = am_plan(N, a.dw.cols, M * p.dz_parts, true, whole && a.dw.cols % 8 == 0);
-        const int64_t b = am_partial_bytes(N, a.dw.cols, p.dw.splits);
+        p.dw = am_plan(rows_of(dz, N), true, other(a.x, a.dw.cols), true, M, 2, p.dz_parts, true);
+        const int64_t b = am_most_partial_bytes(N, a.dw.cols, M * p.dz_parts);
         p.partial_bytes = b > p.partial_bytes ? b : p.partial_bytes;
     }
     return p;

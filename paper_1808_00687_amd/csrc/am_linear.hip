@@ -155,7 +155,7 @@ hipError_t am_launch_linear(const wfst_am_linear_args &a, hipStream_t st)
     // stage, the thin kernel hardly at all ((1, 1024, 6000): 5.1 us against 10.0, (400, 1024, 1024),
     // 112 tiles: 8.8 against 11.1); with more it reads too much ((1500, 512, 640), 240 tiles: 8.8 against 7.7)
     const bool thin = a.x.rows <= 32 || am_tiles(a.x.rows, a.w.rows, 64, 64) <= kComputeUnits / 2;
-    const int32_t tile = thin ? 0 : am_plan(a.x.rows, a.w.rows, a.x.cols, false, p.inner * el % 16 == 0).tile;
+    const int32_t tile = thin ? 0 : am_plan(p.a, false, p.b, false, p.inner, static_cast<int>(el), 1, false).tile;
     if (a.x.type == WFST_F16) am_product_forward<f16>(p, tile, st);
     else if (a.x.type == WFST_BF16) am_product_forward<bf16>(p, tile, st);
     else am_product_forward<f8>(p, tile, st);

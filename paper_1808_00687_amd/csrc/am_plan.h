@@ -50,34 +50,58 @@ struct AmPlan {
 // and a launch.  128 x 128 tiles that are at most one a CU have stages of twice the
 // length, four of them: with the shorter ones a CU waits for memory ((4096, 1024,
 // 1024) 19.4 us, so 16.2; (2048, 1024, 2048) 18.6 and 15.8; the gradient of x of
-// (3000, 1024, 2048) 34.1 and 27.9).  Where rows are no multiple of 16 bytes (not
-// `whole`) stages go through registers and that does not hold.
+// (3000, 1024, 2048) 34.1 and 27.9).  Operands that are not `whole` (fetched straight
+// to LDS) go through registers, in tiles and at times of their own: forward of (4096,
+// 1024, 1024) with rows 2 bytes off 21 us in tiles of 128 and 29 of 64, gradient of x
+// of (3000, 1024, 2048) 40 and 30, of w 56 and 35.
 inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split, bool whole)
 {
-    constexpr struct {
+    struct Kind {
         int32_t tile;
         int64_t fit, most;   // workgroups on a CU, and on the chip
-        double stage[3];
-    } kinds[] = {{256, 1, INT64_MAX, {1.45}}, {128, 1, kComputeUnits, {0.95}}, {128, 3, INT64_MAX, {1.5, 1.9, 2.3}}, {64, 2, INT64_MAX, {0.5, 0.55}}};
+        double stage[4];
+    };
+    constexpr Kind direct[] = {{256, 1, INT64_MAX, {1.45}}, {128, 1, kComputeUnits, {0.95}}, {128, 3, INT64_MAX, {1.5, 1.9, 2.3}},
+                               {64, 2, INT64_MAX, {0.5, 0.55}}};
+    // forward, and with k-major operands (the gradients' products, those that may be split)
+    constexpr Kind staged[2][2] = {{{128, 4, INT64_MAX, {1.2, 1.5, 2.2, 2.9}}, {64, 4, INT64_MAX, {0.58, 0.72, 1.2, 1.6}}},
+                                   {{128, 4, INT64_MAX, {1.2, 1.4, 2.1, 2.85}}, {64, 4, INT64_MAX, {0.58, 0.7, 0.85, 1.15}}}};
     const int64_t stages = (inner + 63) / 64;
     AmPlan best{64, 1};
     double least = 1e30;
-    for (const auto &k : kinds)
+    for (int i = 0; i < (whole ? 4 : 2); i++) {
+        const Kind &k = whole ? direct[i] : staged[may_split][i];
         for (int32_t s = 1; s <= (may_split ? 64 : 1) && (s == 1 || stages / s >= 4); s *= 2) {
             const int64_t n = am_tiles(rows, cols, k.tile, k.tile) * s, at_once = kComputeUnits * k.fit, rest = n % at_once;
-            if (n > k.most || (!whole && k.most == kComputeUnits)) break;
+            if (n > k.most) break;
             double t = static_cast<double>(n / at_once) * k.stage[k.fit - 1];
             if (rest) t += k.stage[(rest - 1) / kComputeUnits];
             t *= static_cast<double>((stages + s - 1) / s);
             if (s > 1) t += 5.0 + static_cast<double>(rows) * static_cast<double>(cols) * 8.0 * s / 4e6;
             if (t < least) least = t, best = {k.tile, s};
         }
+    }
     return best;
 }
 
 inline int64_t am_partial_bytes(int64_t rows, int64_t cols, int32_t splits)
 {
     return splits > 1 ? (rows * cols * splits * 4 + 255) & ~int64_t{255} : 0;
+}
+
+// The plan for operands as they lie: whole are those that are fetched straight to LDS.
+inline AmPlan am_plan(const AmOperand &a, bool major_a, const AmOperand &b, bool major_b, int64_t inner, int el, int times, bool may_split)
+{
+    const bool whole = am_direct(a, major_a, static_cast<int32_t>(inner), el) && am_direct(b, major_b, static_cast<int32_t>(inner), el);
+    return am_plan(a.extent, b.extent, inner * times, may_split, whole);
+}
+
+// Bytes that the parts of a split product take, however its operands lie.
+inline int64_t am_most_partial_bytes(int64_t rows, int64_t cols, int64_t inner)
+{
+    const int64_t u = am_partial_bytes(rows, cols, am_plan(rows, cols, inner, true, false).splits);
+    const int64_t v = am_partial_bytes(rows, cols, am_plan(rows, cols, inner, true, true).splits);
+    return u > v ? u : v;
 }
 
 }  // namespace wfd

@@ -34,6 +34,41 @@ def test_launches_fit(tmp_path):
         assert b > 1 << 22 or len(runs) == 2
 
 
+def test_the_plan_goes_by_where_operands_lie(tmp_path):
+    # A plan for operands on 16 bytes is for those alone: not for a stride, or a first element, beside them.  4,096 x 1,024 of
+    # 2,048 is a product whose plans differ.
+    line = """{ const AmOperand a{(const char *)%dll, %dll, 4096}, b{(const char *)%dll, %dll, 1024};
+    const AmPlan p = am_plan(a, false, b, %s, %d, 2, 1, true); printf("%%d %%d ", p.tile, p.splits); }
+    """
+    cases = [(0, 4096, 0, 4096, "false", 2048), (16, 4112, 64, 8192, "false", 2048), (0, 4096, 0, 2048, "true", 2048),
+             (0, 4098, 0, 4096, "false", 2048), (0, 4096, 0, 2050, "true", 2048), (8, 4096, 0, 4096, "false", 2048),
+             (0, 4096, 2, 2048, "true", 2048), (0, 4096, 0, 4096, "false", 2044), (0, 1 << 23, 0, 4096, "false", 2048)]
+    plain = """{ const AmPlan p = am_plan(4096, 1024, 2048, true, %s); printf("%%d %%d ", p.tile, p.splits); }
+    """
+    got = run(tmp_path, "".join(line % c for c in cases) + plain % "true" + plain % "false"
+              + 'printf("%lld", (long long)am_most_partial_bytes(4096, 1024, 2048));')
+    plans = list(zip(got[:-1:2], got[1:-1:2]))
+    whole, other = plans[-2:]
+    assert whole != other
+    assert plans[:3] == [whole] * 3 and plans[3:-2] == [other] * 6
+    assert int(got[-1]) >= max(4 * 4096 * 1024 * int(s) if int(s) > 1 else 0 for _, s in (whole, other))
+
+
+def test_the_workspace_does_not_depend_on_where_operands_lie():
+    pytest.importorskip("torch")
+    import ctypes as C
+    from paper_1808_00687_amd import acoustic as am
+    sizes = set()
+    for at, pad in ((0, 0), (2, 0), (0, 1), (8, 3)):
+        a = am._LinearBackwardArgs()
+        for f, rows, cols in (("dy", 4096, 1024), ("x", 4096, 1024), ("w", 1024, 1024), ("dx", 4096, 1024), ("dw", 1024, 1024)):
+            setattr(a, f, am._Matrix(4096 + at, rows, cols, cols + pad, am.WFST_BF16, 0))
+        n = C.c_int64()
+        assert am._lib.wfst_am_linear_backward_workspace(bytes(a), C.byref(n)) == 0
+        sizes.add(n.value)
+    assert len(sizes) == 1
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("m,n", [(1, (1 << 28) + 33), ((1 << 30) - 5, 1)])
 def test_as_many_rows_or_columns_as_are_taken(m, n):
