@@ -501,7 +501,8 @@ int wfst_set_debug_opts(const wfst_debug_opts *opts);
  * captured into a HIP graph.  All matrices, vectors and workspaces are device
  * memory of the current device and must stay valid until the stream has
  * passed the call.  Outputs must not overlap inputs or one another, except
- * where a call says so.  Results do not depend on timing: no sum is taken in
+ * where a call says so.  (Column slices of one buffer do not overlap; matrices
+ * whose rows interleave in another way, with different strides, are refused.)  Results do not depend on timing: no sum is taken in
  * an order that can change from run to run.
  *
  * Sums, statistics and everything between the inputs and an output are held

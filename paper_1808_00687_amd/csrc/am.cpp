@@ -12,8 +12,20 @@ using namespace wfd;
 namespace {
 
 struct Range {
-    uintptr_t lo, hi;   // bytes [lo, hi); empty where there is nothing
+    uintptr_t lo, hi;        // bytes [lo, hi); empty where there is nothing
+    uintptr_t stride = 0;    // of a matrix of several rows: bytes [lo + i stride, lo + i stride + width) of them
+    uintptr_t width = 0;
 };
+
+// No byte of one is a byte of the other.  Matrices with the same stride are compared by
+// their columns (slices of one buffer), others by their whole spans.
+bool disjoint(const Range &a, const Range &b)
+{
+    if (!(a.lo < b.hi && b.lo < a.hi)) return true;
+    if (!a.stride || a.stride != b.stride) return false;
+    const uintptr_t off = b.lo >= a.lo ? (b.lo - a.lo) % a.stride : (a.stride - (a.lo - b.lo) % a.stride) % a.stride;
+    return off >= a.width && off + b.width <= a.stride;
+}
 
 // A call's checks: the first one that fails sets the message.
 struct Checks {
@@ -65,15 +77,16 @@ struct Checks {
     }
     bool apart(Range a, Range b, const char *what)
     {
-        return !(a.lo < b.hi && b.lo < a.hi) || fail(what);
+        return disjoint(a, b) || fail(what);
     }
 };
 
 Range range_of(const wfst_matrix &m)
 {
     if (!m.data || m.rows < 1) return {0, 0};
-    const uintptr_t p = reinterpret_cast<uintptr_t>(m.data);
-    return {p, p + static_cast<uintptr_t>(((m.rows - 1) * m.row_stride + m.cols) * am_type_bytes(m.type))};
+    const uintptr_t p = reinterpret_cast<uintptr_t>(m.data), size = static_cast<uintptr_t>(am_type_bytes(m.type));
+    const uintptr_t stride = static_cast<uintptr_t>(m.row_stride) * size, width = static_cast<uintptr_t>(m.cols) * size;
+    return {p, p + static_cast<uintptr_t>(m.rows - 1) * stride + width, m.rows > 1 ? stride : 0, width};
 }
 
 Range range_of(const void *p, int64_t bytes)

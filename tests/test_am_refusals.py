@@ -32,3 +32,12 @@ def test_products_of_more_elements_than_any_memory(am):  # noqa: F811
         assert refused(am, "linear", residual__data=None, pre__data=None, **change)
         from paper_1808_00687_amd import wfstdec
         assert "2^40" in wfstdec.wfst_last_error()
+
+
+def test_slices_that_share_a_column(am):  # noqa: F811
+    # x [4 x 16], w, residual, pre and y [4 x 8], rows 64 values apart in one buffer of 4-byte values
+    at = 0x10000000
+    for y, pre in ((0, 7), (7, 0), (0, -7), (60, 0), (0, 60), (0, 64 + 7), (0, 64 - 7), (0, 3 * 64 + 1)):
+        assert refused(am, "linear", y__data=at + 4 * y + 4096, y__row_stride=64, pre__data=at + 4 * pre + 4096, pre__row_stride=64)
+    # another stride: by the whole spans
+    assert refused(am, "linear", y__data=at + 4096, y__row_stride=64, pre__data=at + 4096 + 32, pre__row_stride=128)
