@@ -147,12 +147,14 @@ class _On:
 def _here(f):
     """f, which works on the current device and stream, with a ``stream``
     argument and on the device of its first argument."""
+    operand = f.__code__.co_varnames[0]
+
     def call(*args, stream=None, **kw):
-        first = args[0] if args else next(iter(kw.values()), None)
+        first = args[0] if args else kw.get(operand)
         if stream is None and (not isinstance(first, torch.Tensor) or not first.is_cuda
                                or first.get_device() == torch._C._cuda_getDevice()):
             return f(*args, **kw)
-        with _On(_device(first, "the first operand"), stream):
+        with _On(_device(first, operand), stream):
             return f(*args, **kw)
 
     call.__name__, call.__qualname__, call.__doc__ = f.__name__, f.__qualname__, f.__doc__
