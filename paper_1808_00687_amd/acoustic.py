@@ -121,6 +121,12 @@ def _vector(t: Optional[torch.Tensor], name: str, n: int, device: int, dtype=tor
     return t.data_ptr()
 
 
+def _entries(t: torch.Tensor, rows: int, k: int, device: int) -> int:
+    if tuple(t.shape) != (rows, k):
+        raise ValueError("top_index must be [%d x %d], as top_logit" % (rows, k))
+    return _vector(t, "top_index", rows * k, device, torch.int32)
+
+
 def _device(t: torch.Tensor, name: str) -> int:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a torch tensor on a GPU" % name)
@@ -301,7 +307,7 @@ def wfst_am_distill(logits: torch.Tensor, top_index: torch.Tensor, top_logit: to
         dlogits = torch.empty_like(logits, memory_format=_DENSE)
     _call("wfst_am_distill", _PACK["distill"].pack(
         *mx, *mt, *(_NONE if dlogits is None else _matrix(dlogits, "dlogits", d)),
-        _vector(top_index, "top_index", mt[1] * mt[2], d, torch.int32), _vector(weight, "weight", mx[1], d),
+        _entries(top_index, mt[1], mt[2], d), _vector(weight, "weight", mx[1], d),
         loss.data_ptr(), lse.data_ptr(), temperature, 0), _raw_stream(d))
     return loss, lse, dlogits
 
@@ -319,7 +325,7 @@ def wfst_am_distill_backward(logits: torch.Tensor, top_index: torch.Tensor, top_
         dlogits = torch.empty_like(logits, memory_format=_DENSE)
     _call("wfst_am_distill_backward", _PACK["distill"].pack(
         *mx, *mt, *_matrix(dlogits, "dlogits", d),
-        _vector(top_index, "top_index", mt[1] * mt[2], d, torch.int32), _vector(weight, "weight", mx[1], d),
+        _entries(top_index, mt[1], mt[2], d), _vector(weight, "weight", mx[1], d),
         0, _vector(lse, "lse", mx[1], d), temperature, 0), _raw_stream(d))
     return dlogits
 

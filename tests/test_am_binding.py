@@ -55,3 +55,28 @@ def test_a_stream_with_operands_by_name(am):
         am.wfst_am_linear(activation="relu", x=x, w=x, stream=0)
     with pytest.raises(TypeError, match="logits must be a torch tensor on a GPU"):
         am.wfst_am_loglikes(scale=2.0, logits=x, stream=0)
+
+
+@pytest.fixture
+def on_cpu(am, monkeypatch):
+    """Calls go up to the library's, with tensors on the CPU; what it would be called with."""
+    calls = []
+    monkeypatch.setattr(am, "_device", lambda t, name: t.get_device())
+    monkeypatch.setattr(am, "_raw_stream", lambda d: 0)
+    monkeypatch.setattr(am, "_call", lambda name, packed, stream: calls.append(name))
+    return calls
+
+
+def test_entries_have_their_logits_shape(am, on_cpu):
+    x, top, idx = torch.zeros(6, 20), torch.zeros(6, 3), torch.zeros(6, 3, dtype=torch.int32)
+    lse = torch.zeros(6)
+    both = (lambda i: am.wfst_am_distill.__wrapped__(x, i, top), lambda i: am.wfst_am_distill_backward.__wrapped__(x, i, top, lse))
+    for call in both:
+        call(idx)
+        for other in (idx.t().contiguous(), idx.flatten(), idx.reshape(3, 6), idx.reshape(2, 9), idx[:, :2].contiguous()):
+            with pytest.raises(ValueError, match="top_index must be .6 x 3."):
+                call(other)
+        for other in (idx.long(), torch.zeros(6, 4, dtype=torch.int32)[:, :3]):
+            with pytest.raises(ValueError, match="top_index"):
+                call(other)
+    assert on_cpu == ["wfst_am_distill", "wfst_am_distill_backward"]
