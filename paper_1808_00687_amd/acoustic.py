@@ -12,6 +12,11 @@ stream or a raw handle) or else torch's current stream, and take their results
 from torch's allocator on that stream (none where ``out`` is given), so they
 can be captured into a graph.  Arguments that the library
 refuses raise WfstError (WFST_EINVAL) with its message.
+
+Autograd does not follow these calls: an operand that requires a gradient is
+refused while gradients are recorded (inside a torch.autograd.Function, under
+no_grad and in inference mode they are not), and the gradients are the
+``*_backward`` calls'.  A tensor that a call writes counts as changed in place.
 """
 from __future__ import annotations
 
@@ -20,6 +25,7 @@ import struct
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.graph import increment_version
 
 from .wfstdec import WFST_OK, WfstError, _lib, wfst_last_error
 
@@ -90,6 +96,8 @@ for _n in ("linear_backward", "norm_backward"):
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _DENSE = torch.contiguous_format
+_NO_GRAPH = ("%s requires a gradient, which autograd does not get through this call: detach it, or call under "
+             "torch.no_grad(); gradients are the *_backward calls'")
 
 
 def _matrix(t: torch.Tensor, name: str, device: int, keep: Optional[list] = None) -> tuple:
@@ -98,6 +106,8 @@ def _matrix(t: torch.Tensor, name: str, device: int, keep: Optional[list] = None
     code = _TYPES.get(t.dtype)
     if code is None:
         raise TypeError("%s: type %s is not taken" % (name, t.dtype))
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(_NO_GRAPH % name)
     if t.dim() != 2 or t.get_device() != device:
         raise ValueError("%s must be a matrix on the operands' GPU" % name)
     rows, cols = t.shape
@@ -116,6 +126,8 @@ def _matrix(t: torch.Tensor, name: str, device: int, keep: Optional[list] = None
 def _vector(t: Optional[torch.Tensor], name: str, n: int, device: int, dtype=torch.float32) -> int:
     if t is None:
         return 0
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(_NO_GRAPH % name)
     if t.dtype != dtype or t.get_device() != device or t.numel() != n or not t.is_contiguous():
         raise ValueError("%s must be %d dense %s values on the operands' GPU" % (name, n, str(dtype)[6:]))
     return t.data_ptr()
@@ -200,7 +212,8 @@ def wfst_am_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor
     before the activation, for the gradient; ``residual`` may be ``out``."""
     d, keep = _device(x, "x"), []
     mx, mw = _matrix(x, "x", d, keep), _matrix(w, "w", d, keep)
-    if out is None:
+    given = out is not None
+    if not given:
         dt = out_dtype or (residual.dtype if residual is not None else
                            torch.bfloat16 if x.dtype == torch.float8_e4m3fn else x.dtype)
         out = x.new_empty((mx[1], mw[1]), dtype=dt)
@@ -211,6 +224,10 @@ def wfst_am_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor
         *(_NONE if pre is None else _matrix(pre, "pre", d)), *_matrix(out, "out", d),
         _vector(x_scale, "x_scale", mx[1], d), _vector(w_scale, "w_scale", mw[1], d),
         _vector(bias, "bias", mw[1], d), _activation(activation), 0), _raw_stream(d))
+    if pre is not None:
+        increment_version(pre)
+    if given:
+        increment_version(out)
     return out
 
 
@@ -257,6 +274,7 @@ def wfst_am_norm(x: torch.Tensor, gain: Optional[torch.Tensor] = None, *, residu
     d, keep = _device(x, "x"), []
     mx = _matrix(x, "x", d, keep)
     mr = _NONE if residual is None else _matrix(residual, "residual", d, keep)
+    given = [t for t in (out, sum_out) if t is not None]
     if out is None:
         out = torch.empty_like(x, dtype=out_dtype or x.dtype, memory_format=_DENSE)
     elif out_dtype is not None and out_dtype != out.dtype:
@@ -267,6 +285,8 @@ def wfst_am_norm(x: torch.Tensor, gain: Optional[torch.Tensor] = None, *, residu
     _call("wfst_am_norm", _PACK["norm"].pack(
         *mx, *mr, *(_NONE if sum_out is None else _matrix(sum_out, "sum_out", d)), *_matrix(out, "out", d),
         _vector(gain, "gain", mx[2], d), 0 if scale is None else scale.data_ptr(), eps, 0), _raw_stream(d))
+    if given:
+        increment_version(given)
     return out, scale, sum_out
 
 
@@ -303,12 +323,15 @@ def wfst_am_distill(logits: torch.Tensor, top_index: torch.Tensor, top_logit: to
     mx, mt = _matrix(logits, "logits", d, keep), _matrix(top_logit, "top_logit", d, keep)
     loss = logits.new_empty(mx[1], dtype=torch.float32)
     lse = torch.empty_like(loss)
-    if dlogits is None and gradient:
+    given = dlogits is not None
+    if not given and gradient:
         dlogits = torch.empty_like(logits, memory_format=_DENSE)
     _call("wfst_am_distill", _PACK["distill"].pack(
         *mx, *mt, *(_NONE if dlogits is None else _matrix(dlogits, "dlogits", d)),
         _entries(top_index, mt[1], mt[2], d), _vector(weight, "weight", mx[1], d),
         loss.data_ptr(), lse.data_ptr(), temperature, 0), _raw_stream(d))
+    if given:
+        increment_version(dlogits)
     return loss, lse, dlogits
 
 
@@ -321,12 +344,15 @@ def wfst_am_distill_backward(logits: torch.Tensor, top_index: torch.Tensor, top_
     call's weight."""
     d, keep = _device(logits, "logits"), []
     mx, mt = _matrix(logits, "logits", d, keep), _matrix(top_logit, "top_logit", d, keep)
-    if dlogits is None:
+    given = dlogits is not None
+    if not given:
         dlogits = torch.empty_like(logits, memory_format=_DENSE)
     _call("wfst_am_distill_backward", _PACK["distill"].pack(
         *mx, *mt, *_matrix(dlogits, "dlogits", d),
         _entries(top_index, mt[1], mt[2], d), _vector(weight, "weight", mx[1], d),
         0, _vector(lse, "lse", mx[1], d), temperature, 0), _raw_stream(d))
+    if given:
+        increment_version(dlogits)
     return dlogits
 
 
@@ -337,8 +363,11 @@ def wfst_am_loglikes(logits: torch.Tensor, log_prior: Optional[torch.Tensor] = N
     wfst_decode (wfst_am_loglikes)."""
     d, keep = _device(logits, "logits"), []
     mx = _matrix(logits, "logits", d, keep)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty_like(logits, dtype=torch.float32, memory_format=_DENSE)
     _call("wfst_am_loglikes", _PACK["loglikes"].pack(
         *mx, *_matrix(out, "out", d), _vector(log_prior, "log_prior", mx[2], d), scale, 0), _raw_stream(d))
+    if given:
+        increment_version(out)
     return out

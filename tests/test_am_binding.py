@@ -80,3 +80,63 @@ def test_entries_have_their_logits_shape(am, on_cpu):
             with pytest.raises(ValueError, match="top_index"):
                 call(other)
     assert on_cpu == ["wfst_am_distill", "wfst_am_distill_backward"]
+
+
+def calls_of(am):
+    """Every operator with tensors on the CPU: {name: (call, operands, results' places)}."""
+    f = lambda *shape: torch.zeros(*shape)  # noqa: E731
+    h = lambda *shape: torch.zeros(*shape, dtype=torch.bfloat16)  # noqa: E731
+    idx = torch.zeros(4, 3, dtype=torch.int32)
+    linear = dict(x=h(4, 8), w=h(6, 8), bias=f(6), residual=h(4, 6))
+    norm = dict(x=h(4, 8), gain=f(8), residual=h(4, 8))
+    distill = dict(logits=f(4, 9), top_logit=f(4, 3), weight=f(4))
+    return {
+        "linear": (lambda **kw: am.wfst_am_linear.__wrapped__(**kw), linear, dict(out=h(4, 6), pre=h(4, 6))),
+        "norm": (lambda **kw: am.wfst_am_norm.__wrapped__(**kw), norm, dict(out=h(4, 8), sum_out=h(4, 8))),
+        "norm_backward": (lambda **kw: am.wfst_am_norm_backward.__wrapped__(gain_gradient=False, **kw),
+                          dict(dy=h(4, 8), s=h(4, 8), gain=f(8), dsum=h(4, 8)), {}),
+        "linear_backward": (lambda **kw: am.wfst_am_linear_backward.__wrapped__(activation="silu", bias_gradient=False, **kw),
+                            dict(dy=h(4, 6), x=h(4, 8), w=h(6, 8), pre=h(4, 6)), {}),
+        "distill": (lambda **kw: am.wfst_am_distill.__wrapped__(top_index=idx, **kw), distill, dict(dlogits=f(4, 9))),
+        "distill_backward": (lambda **kw: am.wfst_am_distill_backward.__wrapped__(top_index=idx, **kw),
+                             dict(distill, lse=f(4)), dict(dlogits=f(4, 9))),
+        "loglikes": (lambda **kw: am.wfst_am_loglikes.__wrapped__(**kw), dict(logits=f(4, 9), log_prior=f(9)), dict(out=f(4, 9))),
+    }
+
+
+NAMES = ["linear", "linear_backward", "norm", "norm_backward", "distill", "distill_backward", "loglikes"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_operands_that_require_a_gradient(am, on_cpu, name, monkeypatch):
+    monkeypatch.setattr(am, "_bytes_for", lambda *_: 0)
+    call, operands, places = calls_of(am)[name]
+    call(**operands, **places)
+    for k in list(operands) + list(places):
+        changed = {n: t.detach().requires_grad_() if n == k else t for n, t in {**operands, **places}.items()}
+        with pytest.raises(ValueError, match="%s requires a gradient" % k):
+            call(**changed)
+        with torch.no_grad():
+            call(**changed)
+        with torch.inference_mode():
+            call(**changed)
+
+
+@pytest.mark.parametrize("name", [n for n in NAMES if not n.endswith("m_backward") and n != "linear_backward"])
+def test_results_count_as_written(am, on_cpu, name):
+    call, operands, places = calls_of(am)[name]
+    at = {k: t._version for k, t in places.items()}
+    call(**operands, **places)
+    for k, t in places.items():
+        assert t._version > at[k], k
+    for k, t in operands.items():
+        assert t._version == 0, k
+    # a graph that kept a result's old value notices
+    k, t = next(iter(places.items()))
+    leaf = torch.ones_like(t).requires_grad_()
+    loss = (leaf * t).sum()
+    call(**operands, **places)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():
+        call(**operands, **{k: torch.zeros_like(t) for k, t in places.items()})
