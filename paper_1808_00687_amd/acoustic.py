@@ -8,9 +8,11 @@ is two-dimensional; its rows may lie any distance apart (an input whose
 columns are not adjacent, or whose rows overlap, is copied first; an output
 like that is refused).  Vectors (bias, gain, scales, weights) are float32.
 The calls only enqueue, on the ``stream`` that each takes by name (a torch
-stream or a raw handle) or else torch's current stream, and take their results
-from torch's allocator on that stream (none where ``out`` is given), so they
-can be captured into a graph.  Arguments that the library
+stream or a raw handle) or else torch's current stream, so they can be captured
+into a graph.  Results that a call takes no place for, or is given none for, and
+the gradients' workspaces come from torch's allocator on that stream: an 8-bit
+norm's scales, a loss and its lse, and all that wfst_am_linear_backward and
+wfst_am_norm_backward return always do.  (The C calls allocate nothing.)  Arguments that the library
 refuses raise WfstError (WFST_EINVAL) with its message.
 
 Autograd does not follow these calls: an operand that requires a gradient is
