@@ -27,7 +27,6 @@ import struct
 from typing import Optional, Tuple
 
 import torch
-from torch.autograd.graph import increment_version
 
 from .wfstdec import WFST_OK, WfstError, _lib, wfst_last_error
 
@@ -97,6 +96,7 @@ for _n in ("linear_backward", "norm_backward"):
 
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_written = torch._C._increment_version   # of a sequence of tensors (torch.autograd.graph's wrapper takes as long again)
 _DENSE = torch.contiguous_format
 _NO_GRAPH = ("%s requires a gradient, which autograd does not get through this call: detach it, or call under "
              "torch.no_grad(); gradients are the *_backward calls'")
@@ -227,9 +227,9 @@ def wfst_am_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor
         _vector(x_scale, "x_scale", mx[1], d), _vector(w_scale, "w_scale", mw[1], d),
         _vector(bias, "bias", mw[1], d), _activation(activation), 0), _raw_stream(d))
     if pre is not None:
-        increment_version(pre)
+        _written((pre,))
     if given:
-        increment_version(out)
+        _written((out,))
     return out
 
 
@@ -288,7 +288,7 @@ def wfst_am_norm(x: torch.Tensor, gain: Optional[torch.Tensor] = None, *, residu
         *mx, *mr, *(_NONE if sum_out is None else _matrix(sum_out, "sum_out", d)), *_matrix(out, "out", d),
         _vector(gain, "gain", mx[2], d), 0 if scale is None else scale.data_ptr(), eps, 0), _raw_stream(d))
     if given:
-        increment_version(given)
+        _written(given)
     return out, scale, sum_out
 
 
@@ -333,7 +333,7 @@ def wfst_am_distill(logits: torch.Tensor, top_index: torch.Tensor, top_logit: to
         _entries(top_index, mt[1], mt[2], d), _vector(weight, "weight", mx[1], d),
         loss.data_ptr(), lse.data_ptr(), temperature, 0), _raw_stream(d))
     if given:
-        increment_version(dlogits)
+        _written((dlogits,))
     return loss, lse, dlogits
 
 
@@ -354,7 +354,7 @@ def wfst_am_distill_backward(logits: torch.Tensor, top_index: torch.Tensor, top_
         _entries(top_index, mt[1], mt[2], d), _vector(weight, "weight", mx[1], d),
         0, _vector(lse, "lse", mx[1], d), temperature, 0), _raw_stream(d))
     if given:
-        increment_version(dlogits)
+        _written((dlogits,))
     return dlogits
 
 
@@ -371,5 +371,5 @@ def wfst_am_loglikes(logits: torch.Tensor, log_prior: Optional[torch.Tensor] = N
     _call("wfst_am_loglikes", _PACK["loglikes"].pack(
         *mx, *_matrix(out, "out", d), _vector(log_prior, "log_prior", mx[2], d), scale, 0), _raw_stream(d))
     if given:
-        increment_version(out)
+        _written((out,))
     return out
