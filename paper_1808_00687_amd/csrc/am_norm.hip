@@ -257,6 +257,10 @@ __global__ __launch_bounds__(1024) void column_join_kernel(const float *partial,
     out[c] = t;
 }
 
+// Workgroups at most.  Forward, (53274, 1024) to 8 bits: 2, 4, 8, 16, 32 and 64 a CU take 74,
+// 80, 75, 70, 68 and 66 us, (53274, 96) 45, 35, 31, 27, 27 and 29.  Backward, whose workgroups'
+// sums are joined, (16384, 2048): 2, 3, 4, 6 and 8 take 57, 52, 49, 52 and 60, (53274, 256) 53,
+// 42, 38, 35 and 38, (16000, 5000) with 3 133 and with 4 170.
 constexpr int64_t kForwardBlocks = 256 * 16;
 constexpr int64_t kBackwardBlocks = 256 * 3;
 
@@ -277,13 +281,13 @@ void launch_norm(const wfst_am_norm_args &a, hipStream_t st)
     if constexpr (kChunk<T> > 4)
         if (a.y.type == WFST_F32) {
             // (53274, 1024) bf16 to f32: 60 us, with chunks of 8 71; with the residual 101 and 107
-            am_row_shape<4>(a.x.cols, [&](auto shape) {
+            am_row_shape_norm<4>(a.x.cols, [&](auto shape) {
                 using S = decltype(shape);
                 norm_kernel<T, S, false><<<am_row_blocks<S>(a.x.rows, kForwardBlocks), S::kThreads, 0, st>>>(a);
             });
             return;
         }
-    am_row_shape<kChunk<T>>(a.x.cols, [&](auto shape) {
+    am_row_shape_norm<kChunk<T>>(a.x.cols, [&](auto shape) {
         using S = decltype(shape);
         const unsigned g = am_row_blocks<S>(a.x.rows, kForwardBlocks);
         if (a.y.type == WFST_F8E4M3) norm_kernel<T, S, true><<<g, S::kThreads, 0, st>>>(a);

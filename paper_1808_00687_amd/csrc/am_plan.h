@@ -54,6 +54,10 @@ struct AmPlan {
 // to LDS) go through registers, in tiles and at times of their own: forward of (4096,
 // 1024, 1024) with rows 2 bytes off 21 us in tiles of 128 and 29 of 64, gradient of x
 // of (3000, 1024, 2048) 40 and 30, of w 56 and 35.
+// The times are of 16-bit operands and decide for 8 bits too: of 14 products the best
+// tile is missed by more than 10% in (4096, 1024, 2048) e4m3, 27 us in 256, 23 in 128,
+// (3000, 1024, 2048), 25 and 22, and (53274, 512, 640), 56 and 46; of 14 in bf16 in two,
+// (3000, 1024, 2048), 28.5 and 23, and (4096, 1024, 2048), 29 and 25.
 inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split, bool whole)
 {
     struct Kind {

@@ -40,7 +40,15 @@ struct RowShape {
     }
 };
 
-// Calls go(shape) with the shape for rows of D columns.
+// Calls go(shape) with the shape for rows of D columns.  Its bounds, in us for 8e7
+// bf16 values (norm to 8 bits with a residual / loss with gradient / log-likelihoods):
+//   1,024 columns: a wave 73 / 85 / 60, 256 threads 87 / 180 / 110
+//   2,048: a wave 106 / 109 / 94, 256 threads 112 / 147 / 92
+//   4,096: 256 threads 110 / 95 / 93, 1,024 threads 137 / 277 / 156
+//   6,000: 256 threads in three chunks 117 / 86 / 94, in four 130 / 142 / 96
+//   8,192: 256 threads 108 / 106 / 94, 1,024 threads 112 / 160 / 95
+//   16,384: 1,024 threads in two chunks 137 / 101 / 94, in four 300 / 110 / 122
+//   20,000: held in four chunks 369 / 97 / 115, read again in each pass 178 / 130 / 136
 template <int C, typename F>
 void am_row_shape(int64_t D, F go)
 {
@@ -56,14 +64,26 @@ void am_row_shape(int64_t D, F go)
     else go(RowShape<1024, 0, C>{});
 }
 
-// The same for an operator that holds several matrices and sums besides:
-// rows of 1,024 to 2,048 go to 256 threads, a chunk each.
+// The same for the norm's gradients, which hold three matrices and sums besides: a
+// chunk a thread (2,048 columns 124 us, a wave 140; 8,192 136, 256 threads 145) but where
+// many threads would have none (5,000 bf16 223, 256 threads 131, float32 255 and 273).  Between 1,024 and 1,536
+// columns it depends on the type: 1,500 bf16 58, a wave 48, float32 78 and 84.
 template <int C, typename F>
 void am_row_shape_lean(int64_t D, F go)
 {
     constexpr int k = 8 / C;
     if (D > 1024 && D <= 2048) go(RowShape<256, 1 * k, C>{});
-    else if (D > 4096 && D <= 8192) go(RowShape<1024, 1 * k, C>{});
+    else if (D > 6144 && D <= 8192) go(RowShape<1024, 1 * k, C>{});
+    else am_row_shape<C>(D, go);
+}
+
+// And for the norm forward, whose rows with their residuals' take twice the registers:
+// held up to 16,384 columns ((4000, 20000) bf16 with the residual 206 us, read again 158,
+// without 100 and 80, float32 390 and 136; (2441, 32768) 148 and 161, 79 and 72).
+template <int C, typename F>
+void am_row_shape_norm(int64_t D, F go)
+{
+    if (D > 16384) go(RowShape<1024, 0, C>{});
     else am_row_shape<C>(D, go);
 }
 

@@ -79,6 +79,10 @@ __device__ __forceinline__ float tempered(float x, float inv_t)
 // log sum exp of x / temperature; -inf for a row of -inf
 __device__ __forceinline__ float lse_of(const RowStat &s, float inv_t) { return tempered(s.top, inv_t) + logf(s.sum); }
 
+// Workgroups at most.  Loss and gradient of (16384, 6000): 2, 3, 4, 5, 6 and 8 a CU take 151,
+// 117, 99, 127, 116 and 101 us; log-likelihoods of (53274, 6000): 2, 4, 8 and 16 359, 376, 376
+// and 370, of (4000, 20000) 113, 117, 122 and 138.  Short rows would rather have more (loss and
+// gradient of (53274, 80): 4 71, 16 59).
 constexpr int64_t kSoftmaxBlocks = 256 * 4;
 
 }  // namespace wfd
