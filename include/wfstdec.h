@@ -578,8 +578,8 @@ int wfst_am_linear(const wfst_am_linear_args *args, void *hip_stream);
  * The matrix cores multiply 16-bit operands.  The products read the dz of a
  * silu or gelu as the sum of two 16-bit values, within 2^-16 (WFST_BF16) or
  * 2^-22 (WFST_F16, or 2^-35 if that is more) of it; round_dz = 1 makes it one,
- * rounded to nearest (dx and dw 1.4 times as far from the exact ones, a little over
- * half the time).  Other dz are dy, or 0, and exact.  dbias sums the float32 dz.
+ * rounded to nearest (16-bit dx and dw 1.4 times as far from the exact ones, in a
+ * little over half the time).  Other dz are dy, or 0, and exact.  dbias sums the float32 dz.
  * M = 0 gives zero dw, dbias.
  * Sizes as for wfst_am_linear.
  * Errors: WFST_EINVAL (also a workspace that is too small), WFST_EDEVICE.
@@ -616,7 +616,8 @@ int wfst_am_linear_backward(const wfst_am_linear_backward_args *args, void *hip_
  *   y_scale  [M] float32, needed with WFST_F8E4M3, NULL otherwise
  *   gain     [D] float32 or NULL (ones);  eps > 0, finite
  *
- * Errors: WFST_EINVAL, WFST_EDEVICE.
+ * The squares are summed in float32: a row's s^2 may add up to 3e38 (a root
+ * mean square of 1.8e19 / sqrt(D)).  Errors: WFST_EINVAL, WFST_EDEVICE.
  */
 typedef struct wfst_am_norm_args {
     wfst_matrix x, residual, sum, y;

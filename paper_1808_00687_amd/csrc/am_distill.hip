@@ -7,9 +7,9 @@
 // in LDS, to the thread that holds its unit, so that every gradient is written
 // once, whole.
 //
-// (16384, 6000) bf16, 20 entries, loss and gradient: 106 us, 395 MB, 3.7 TB/s; what
+// (16384, 6000) bf16, 20 entries, loss and gradient: 105 us, 395 MB, 3.8 TB/s; what
 // is over a copy's 77 us is the chain of a row: the entries, two reductions over a
-// wave, the barrier.  The exponentials are kept between the statistics and the
+// wave, the barrier (waves wait 64% of their time).  The exponentials are kept between the statistics and the
 // gradient (recomputed, the row's arithmetic alone would take half as long again).
 #include "am_softmax.h"
 

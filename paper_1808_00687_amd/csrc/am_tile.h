@@ -8,7 +8,7 @@
 // ones are fetched while the matrix cores work on the present one.  The fetch goes
 // straight from memory to LDS (16 bytes a lane, no registers); operands that are
 // not aligned to 16 bytes go through registers ((16384, 1001, 2048) forward, both
-// gradients: 121, 111, 127 us; with 1024 aligned columns 75, 60, 93).
+// gradients: 120, 109, 114 us; with 1024 aligned columns 70, 59, 89).
 //
 // 8-bit operands are widened to bf16 as they are read from LDS (each value
 // exactly).  The 8-bit matrix instructions would be twice as fast, but drop the
@@ -32,14 +32,17 @@
 //
 // Measured, bf16: (16384, 4096, 1024) k-contiguous 107 us, 1,280 TFLOP/s (the
 // library's product 94 us); (16384, 4096, 1024) with b k-major 120; k = 16384
-// into 4096 x 1024, both k-major, 144 and 24 for joining 4 parts.  The matrix cores are
-// busy 57 to 65% of the time; no LDS bank conflicts in any layout; the rest is the
-// waves' meeting once a stage and, for a short k, the start and the epilogue of a
-// tile ((16384, 1024, 4096): 152 us).  256 x 256 tiles with 4 waves of twice the
+// into 4096 x 1024, both k-major, 139 and 17 for joining 4 parts; with a in two parts
+// 240 and 318.  The matrix cores are busy 53% of the time (k-contiguous a) and 37% (both
+// k-major, 1.3 GB of reads behind the L2s for two parts).  No LDS bank conflicts but in
+// k-contiguous stages of 64 bytes, where they take 6 to 11% of a CU's cycles (7 in 8
+// bits, 11 in unaligned rows).  The rest is the waves' meeting once a stage and, for a
+// short k, the start and the epilogue of a tile ((16384, 1024, 4096): 142 to 159 us).  256 x 256 tiles with 4 waves of twice the
 // registers made the compiler move sums about; 256 x 128 ones in two workgroups a
 // CU read half as much again from L2 (143 us instead of 107), but pay for 8 bits,
 // where operands are half as large and the epilogue of one overlaps the
-// other's products ((53274, 1024, 4096) e4m3 with gelu: 494 us, 905 TFLOP/s).
+// other's products ((53274, 1024, 4096) e4m3 with gelu: 493 to 514 us by the card, 870 to
+// 905 TFLOP/s; matrix cores busy 38%).
 #pragma once
 
 #include <type_traits>
