@@ -37,12 +37,12 @@
 // k-major, 1.3 GB of reads behind the L2s for two parts).  No LDS bank conflicts but in
 // k-contiguous stages of 64 bytes, where they take 6 to 11% of a CU's cycles (7 in 8
 // bits, 11 in unaligned rows).  The rest is the waves' meeting once a stage and, for a
-// short k, the start and the epilogue of a tile ((16384, 1024, 4096): 142 to 159 us).  256 x 256 tiles with 4 waves of twice the
-// registers made the compiler move sums about; 256 x 128 ones in two workgroups a
-// CU read half as much again from L2 (143 us instead of 107), but pay for 8 bits,
-// where operands are half as large and the epilogue of one overlaps the
-// other's products ((53274, 1024, 4096) e4m3 with gelu: 493 to 514 us by the card, 870 to
-// 905 TFLOP/s; matrix cores busy 38%).
+// short k, the start and the epilogue of a tile ((16384, 1024, 4096): 142 to 159 us).
+// 256 x 256 tiles with 4 waves of twice the registers made the compiler move sums about;
+// 256 x 128 ones in two workgroups a CU read half as much again from L2 (143 us instead
+// of 107), but pay for 8 bits, where operands are half as large and the epilogue of one
+// overlaps the other's products ((53274, 1024, 4096) e4m3 with gelu: 493 to 514 us by the
+// card, 870 to 905 TFLOP/s; matrix cores busy 38%).
 #pragma once
 
 #include <type_traits>
