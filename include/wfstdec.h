@@ -658,6 +658,70 @@ int wfst_am_norm_backward_workspace(const wfst_am_norm_backward_args *args, int6
 int wfst_am_norm_backward(const wfst_am_norm_backward_args *args, void *hip_stream);
 
 /*
+ * wfst_am_layer_norm -- layer norm of each row, with the residual's addition
+ * before it and an output in 8 bits after it:
+ *   s = x + residual;  v = (s - mean(s)) / sqrt(var(s) + eps) * gain + bias
+ *   y = v, or with y of type WFST_F8E4M3 the row's values by its scale, as in
+ *   wfst_am_norm
+ * var(s) = mean((s - mean(s))^2).
+ *
+ *   x        [M x D], WFST_F32, WFST_F16 or WFST_BF16; M >= 0, D >= 1
+ *   residual [M x D] optional, of x's type
+ *   sum      [M x D] optional output: s, of x's type; may be x or residual
+ *            itself (same data and stride).  The norm is taken of the
+ *            unrounded s
+ *   y        [M x D] output, any type
+ *   y_scale  [M] float32, needed with WFST_F8E4M3, NULL otherwise
+ *   gain     [D] float32 or NULL (ones);  bias [D] float32 or NULL (zeros)
+ *   eps      > 0, finite
+ *
+ * Differences are taken from the row's mean before they are squared, so a row
+ * far from zero loses nothing but what s itself has lost.  A row's values and
+ * the squares of its differences are summed in float32: neither sum may pass
+ * 3e38.  Errors: WFST_EINVAL, WFST_EDEVICE.
+ */
+typedef struct wfst_am_layer_norm_args {
+    wfst_matrix x, residual, sum, y;
+    const float *gain, *bias;
+    float *y_scale;
+    float eps;
+    int32_t reserved;
+} wfst_am_layer_norm_args;
+
+int wfst_am_layer_norm(const wfst_am_layer_norm_args *args, void *hip_stream);
+
+/*
+ * wfst_am_layer_norm_backward -- gradients of v (wfst_am_layer_norm) with
+ * respect to s, gain and bias; with u = dy * gain, r = 1 / sqrt(var(s) + eps)
+ * and h = (s - mean(s)) r:
+ *   dx = r (u - mean(u) - h mean(u h)) + dsum
+ *   dgain[d] = sum_m dy[m][d] h[m][d];  dbias[d] = sum_m dy[m][d]
+ *
+ *   dy, s    [M x D] of one type, WFST_F32, WFST_F16 or WFST_BF16
+ *   dsum     [M x D] optional, of that type: the gradient that reaches s past
+ *            the norm (the residual stream's)
+ *   dx       [M x D] optional output of that type: the gradient of x and of
+ *            residual; may be dy or dsum itself (same data and stride)
+ *   dgain, dbias  [D] float32, each an optional output (zeros for M = 0)
+ *   workspace  at least wfst_am_layer_norm_backward_workspace bytes, 256-byte
+ *            aligned
+ *
+ * Errors: WFST_EINVAL, WFST_EDEVICE.
+ */
+typedef struct wfst_am_layer_norm_backward_args {
+    wfst_matrix dy, s, dsum, dx;
+    const float *gain;
+    float *dgain, *dbias;
+    void *workspace;
+    int64_t workspace_bytes;
+    float eps;
+    int32_t reserved;
+} wfst_am_layer_norm_backward_args;
+
+int wfst_am_layer_norm_backward_workspace(const wfst_am_layer_norm_backward_args *args, int64_t *bytes);
+int wfst_am_layer_norm_backward(const wfst_am_layer_norm_backward_args *args, void *hip_stream);
+
+/*
  * wfst_am_distill -- loss of a student's logits against a teacher's top
  * logits, and its gradient.  Per row m, over the used entries j of the
  * teacher's k (an index inside [0, L) and a logit above -inf; a unit that

@@ -11,8 +11,8 @@ The calls only enqueue, on the ``stream`` that each takes by name (a torch
 stream or a raw handle) or else torch's current stream, so they can be captured
 into a graph.  Results that a call takes no place for, or is given none for, and
 the gradients' workspaces come from torch's allocator on that stream: an 8-bit
-norm's scales, a loss and its lse, and all that wfst_am_linear_backward and
-wfst_am_norm_backward return always do.  (The C calls allocate nothing.)  Arguments that the library
+norm's scales, a loss and its lse, and all that wfst_am_linear_backward,
+wfst_am_norm_backward and wfst_am_layer_norm_backward return always do.  (The C calls allocate nothing.)  Arguments that the library
 refuses raise WfstError (WFST_EINVAL) with its message.
 
 Autograd does not follow these calls: an operand that requires a gradient is
@@ -66,6 +66,17 @@ class _NormBackwardArgs(C.Structure):
                 ("eps", C.c_float), ("reserved", C.c_int32)]
 
 
+class _LayerNormArgs(C.Structure):
+    _fields_ = [("x", _Matrix), ("residual", _Matrix), ("sum", _Matrix), ("y", _Matrix), ("gain", C.c_void_p),
+                ("bias", C.c_void_p), ("y_scale", C.c_void_p), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class _LayerNormBackwardArgs(C.Structure):
+    _fields_ = [("dy", _Matrix), ("s", _Matrix), ("dsum", _Matrix), ("dx", _Matrix), ("gain", C.c_void_p),
+                ("dgain", C.c_void_p), ("dbias", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_int64), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
 class _DistillArgs(C.Structure):
     _fields_ = [("logits", _Matrix), ("top_logit", _Matrix), ("dlogits", _Matrix), ("top_index", C.c_void_p),
                 ("weight", C.c_void_p), ("loss", C.c_void_p), ("lse", C.c_void_p), ("temperature", C.c_float),
@@ -82,14 +93,16 @@ class _LoglikesArgs(C.Structure):
 _M = "Pqqqii"
 _PACK = {"linear": struct.Struct(_M * 5 + "PPPii"), "linear_backward": struct.Struct(_M * 6 + "PPqii"),
          "norm": struct.Struct(_M * 4 + "PPfi"), "norm_backward": struct.Struct(_M * 4 + "PPPqfi"),
+         "layer_norm": struct.Struct(_M * 4 + "PPPfi"), "layer_norm_backward": struct.Struct(_M * 4 + "PPPPqfi"),
          "distill": struct.Struct(_M * 3 + "PPPPfi"), "loglikes": struct.Struct(_M * 2 + "Pfi")}
 _NONE = (0, 0, 0, 0, 0, 0)
 
-for _n in ("linear", "linear_backward", "norm", "norm_backward", "distill", "distill_backward", "loglikes"):
+for _n in ("linear", "linear_backward", "norm", "norm_backward", "layer_norm", "layer_norm_backward", "distill",
+           "distill_backward", "loglikes"):
     _f = getattr(_lib, "wfst_am_" + _n)
     _f.argtypes = [C.c_char_p, C.c_void_p]
     _f.restype = C.c_int
-for _n in ("linear_backward", "norm_backward"):
+for _n in ("linear_backward", "norm_backward", "layer_norm_backward"):
     _f = getattr(_lib, "wfst_am_%s_workspace" % _n)
     _f.argtypes = [C.c_char_p, C.POINTER(C.c_int64)]
     _f.restype = C.c_int
@@ -310,6 +323,59 @@ def wfst_am_norm_backward(dy: torch.Tensor, s: torch.Tensor, gain: Optional[torc
     work = s.new_empty(need, dtype=torch.uint8) if need else None
     _call("wfst_am_norm_backward", pack(*head, work.data_ptr() if need else 0, need, eps, 0), _raw_stream(d))
     return dx, dg
+
+
+@_here
+def wfst_am_layer_norm(x: torch.Tensor, gain: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+                       residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                       out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                       sum_out: Optional[torch.Tensor] = None
+                       ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(y, y_scale, sum): the layer norm of x + residual, times ``gain`` plus
+    ``bias`` (wfst_am_layer_norm).  With ``out_dtype`` torch.float8_e4m3fn,
+    y_scale [M] is what the rows of y stand for; else None.  ``sum`` is
+    x + residual (None without a residual), in ``sum_out`` where given, which
+    may be x or residual."""
+    d, keep = _device(x, "x"), []
+    mx = _matrix(x, "x", d, keep)
+    mr = _NONE if residual is None else _matrix(residual, "residual", d, keep)
+    given = [t for t in (out, sum_out) if t is not None]
+    if out is None:
+        out = torch.empty_like(x, dtype=out_dtype or x.dtype, memory_format=_DENSE)
+    elif out_dtype is not None and out_dtype != out.dtype:
+        raise ValueError("out_dtype differs from out's")
+    if sum_out is None and residual is not None:
+        sum_out = torch.empty_like(x, memory_format=_DENSE)
+    scale = x.new_empty(mx[1], dtype=torch.float32) if out.dtype == torch.float8_e4m3fn else None
+    _call("wfst_am_layer_norm", _PACK["layer_norm"].pack(
+        *mx, *mr, *(_NONE if sum_out is None else _matrix(sum_out, "sum_out", d)), *_matrix(out, "out", d),
+        _vector(gain, "gain", mx[2], d), _vector(bias, "bias", mx[2], d), 0 if scale is None else scale.data_ptr(),
+        eps, 0), _raw_stream(d))
+    if given:
+        _written(given)
+    return out, scale, sum_out
+
+
+@_here
+def wfst_am_layer_norm_backward(dy: torch.Tensor, s: torch.Tensor, gain: Optional[torch.Tensor] = None, *,
+                                dsum: Optional[torch.Tensor] = None, eps: float = 1e-5, gain_gradient: bool = True,
+                                bias_gradient: bool = True
+                                ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(dx, dgain, dbias) of wfst_am_layer_norm at its sum ``s`` (x itself
+    without a residual); dx is the gradient of x and of residual.  ``dsum``:
+    the gradient that reaches the sum past the norm."""
+    d, keep = _device(dy, "dy"), []
+    mdy, ms = _matrix(dy, "dy", d, keep), _matrix(s, "s", d, keep)
+    dx = torch.empty_like(s, memory_format=_DENSE)
+    dg = s.new_empty(ms[2], dtype=torch.float32) if gain_gradient else None
+    db = s.new_empty(ms[2], dtype=torch.float32) if bias_gradient else None
+    head = (*mdy, *ms, *(_NONE if dsum is None else _matrix(dsum, "dsum", d, keep)), *_matrix(dx, "dx", d),
+            _vector(gain, "gain", ms[2], d), 0 if dg is None else dg.data_ptr(), 0 if db is None else db.data_ptr())
+    pack = _PACK["layer_norm_backward"].pack
+    need = _bytes_for("wfst_am_layer_norm_backward_workspace", pack(*head, 0, 0, eps, 0))
+    work = s.new_empty(need, dtype=torch.uint8) if need else None
+    _call("wfst_am_layer_norm_backward", pack(*head, work.data_ptr() if need else 0, need, eps, 0), _raw_stream(d))
+    return dx, dg, db
 
 
 @_here

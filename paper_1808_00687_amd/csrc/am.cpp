@@ -233,6 +233,54 @@ bool check(Checks &c, const wfst_am_norm_backward_args &a)
                           (!a.dsum.data || apart_or_same(c, a.dx, a.dsum, kOverlap)));
 }
 
+bool check(Checks &c, const wfst_am_layer_norm_args &a)
+{
+    const int64_t M = a.x.rows, D = a.x.cols;
+    const bool f8 = a.y.type == WFST_F8E4M3;
+    if (!c.dims(M, D) || !c.need(good_eps(a.eps), "eps must be positive and finite")) return false;
+    if (!c.matrix(a.x, "x", M, D, kFloats)) return false;
+    if (a.residual.data && !c.matrix(a.residual, "residual", M, D, 1u << a.x.type)) return false;
+    if (a.sum.data && !c.matrix(a.sum, "sum", M, D, 1u << a.x.type)) return false;
+    if (!c.matrix(a.y, "y", M, D, kFloats | 1u << WFST_F8E4M3)) return false;
+    if (!c.need(f8 || !a.y_scale, "y_scale is for an 8-bit y")) return false;
+    if (!c.vector(a.y_scale, "y_scale", f8 && M > 0) || !c.vector(a.gain, "gain", false) || !c.vector(a.bias, "bias", false))
+        return false;
+    const Range y = range_of(a.y), sum = range_of(a.sum), scale = range_of(a.y_scale, 4 * M);
+    const Range in[] = {range_of(a.x), range_of(a.residual), range_of(a.gain, 4 * D), range_of(a.bias, 4 * D)};
+    for (const Range &r : in)
+        if (!c.apart(y, r, kOverlap) || !c.apart(scale, r, kOverlap)) return false;
+    if (!c.apart(y, sum, kOverlap) || !c.apart(y, scale, kOverlap) || !c.apart(sum, scale, kOverlap) ||
+        !c.apart(sum, in[2], kOverlap) || !c.apart(sum, in[3], kOverlap))
+        return false;
+    return !a.sum.data || (apart_or_same(c, a.sum, a.x, kOverlap) &&
+                           (!a.residual.data || apart_or_same(c, a.sum, a.residual, kOverlap)));
+}
+
+bool check_sizes(Checks &c, const wfst_am_layer_norm_backward_args &a) { return c.dims(a.s.rows, a.s.cols); }
+
+bool check(Checks &c, const wfst_am_layer_norm_backward_args &a)
+{
+    const int64_t M = a.s.rows, D = a.s.cols;
+    if (!check_sizes(c, a) || !c.need(good_eps(a.eps), "eps must be positive and finite")) return false;
+    if (!c.matrix(a.s, "s", M, D, kFloats) || !c.matrix(a.dy, "dy", M, D, 1u << a.s.type)) return false;
+    if (a.dsum.data && !c.matrix(a.dsum, "dsum", M, D, 1u << a.s.type)) return false;
+    if (a.dx.data && !c.matrix(a.dx, "dx", M, D, 1u << a.s.type)) return false;
+    if (!c.vector(a.gain, "gain", false) || !c.vector(a.dgain, "dgain", false) || !c.vector(a.dbias, "dbias", false)) return false;
+    const int64_t need = am_layer_norm_backward_bytes(a);
+    if (!c.need(need == 0 || (a.workspace && a.workspace_bytes >= need), "the workspace is too small")) return false;
+    if (!c.need(reinterpret_cast<uintptr_t>(a.workspace) % 256 == 0, "the workspace is not aligned")) return false;
+    const Range in[] = {range_of(a.gain, 4 * D), range_of(a.s), range_of(a.dy), range_of(a.dsum)};
+    const Range out[] = {range_of(a.dx), range_of(a.dgain, 4 * D), range_of(a.dbias, 4 * D), range_of(a.workspace, need)};
+    for (int i = 0; i < 4; i++) {
+        for (int j = 0; j < (i ? 4 : 2); j++)
+            if (!c.apart(out[i], in[j], kOverlap)) return false;
+        for (int j = 0; j < i; j++)
+            if (!c.apart(out[i], out[j], kOverlap)) return false;
+    }
+    return !a.dx.data || (apart_or_same(c, a.dx, a.dy, kOverlap) &&
+                          (!a.dsum.data || apart_or_same(c, a.dx, a.dsum, kOverlap)));
+}
+
 bool check(Checks &c, const wfst_am_distill_args &a, bool backward)
 {
     const int64_t M = a.logits.rows, L = a.logits.cols, k = a.top_logit.cols;
@@ -329,6 +377,34 @@ extern "C" int wfst_am_norm_backward(const wfst_am_norm_backward_args *args, voi
     Checks c{"wfst_am_norm_backward"};
     if (!check(c, *args)) return WFST_EINVAL;
     return launched(am_launch_norm_backward(*args, stream_of(hip_stream)), c.who);
+}
+
+extern "C" int wfst_am_layer_norm(const wfst_am_layer_norm_args *args, void *hip_stream)
+{
+    clear_error();
+    if (!args) return no_args("wfst_am_layer_norm");
+    Checks c{"wfst_am_layer_norm"};
+    if (!check(c, *args)) return WFST_EINVAL;
+    return args->x.rows ? launched(am_launch_layer_norm(*args, stream_of(hip_stream)), c.who) : WFST_OK;
+}
+
+extern "C" int wfst_am_layer_norm_backward_workspace(const wfst_am_layer_norm_backward_args *args, int64_t *bytes)
+{
+    clear_error();
+    if (!args || !bytes) return no_args("wfst_am_layer_norm_backward_workspace");
+    Checks c{"wfst_am_layer_norm_backward_workspace"};
+    if (!check_sizes(c, *args)) return WFST_EINVAL;
+    *bytes = am_layer_norm_backward_bytes(*args);
+    return WFST_OK;
+}
+
+extern "C" int wfst_am_layer_norm_backward(const wfst_am_layer_norm_backward_args *args, void *hip_stream)
+{
+    clear_error();
+    if (!args) return no_args("wfst_am_layer_norm_backward");
+    Checks c{"wfst_am_layer_norm_backward"};
+    if (!check(c, *args)) return WFST_EINVAL;
+    return launched(am_launch_layer_norm_backward(*args, stream_of(hip_stream)), c.who);
 }
 
 extern "C" int wfst_am_distill(const wfst_am_distill_args *args, void *hip_stream)

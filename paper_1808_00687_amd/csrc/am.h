@@ -1,5 +1,5 @@
 // Acoustic-model operators: what the checks (am.cpp) and the kernels
-// (am_norm.hip, am_distill.hip, am_loglikes.hip, am_linear*.hip) share.
+// (am_norm.hip, am_layer_norm.hip, am_distill.hip, am_loglikes.hip, am_linear*.hip) share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -18,6 +18,9 @@ hipError_t am_launch_linear_backward(const wfst_am_linear_backward_args &a, hipS
 hipError_t am_launch_norm(const wfst_am_norm_args &a, hipStream_t stream);
 int64_t am_norm_backward_bytes(const wfst_am_norm_backward_args &a);
 hipError_t am_launch_norm_backward(const wfst_am_norm_backward_args &a, hipStream_t stream);       // M >= 0
+hipError_t am_launch_layer_norm(const wfst_am_layer_norm_args &a, hipStream_t stream);
+int64_t am_layer_norm_backward_bytes(const wfst_am_layer_norm_backward_args &a);
+hipError_t am_launch_layer_norm_backward(const wfst_am_layer_norm_backward_args &a, hipStream_t stream);   // M >= 0
 hipError_t am_launch_distill(const wfst_am_distill_args &a, bool backward, hipStream_t stream);
 hipError_t am_launch_loglikes(const wfst_am_loglikes_args &a, hipStream_t stream);
 

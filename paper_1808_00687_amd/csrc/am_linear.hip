@@ -103,7 +103,7 @@ void launch_backward(const wfst_am_linear_backward_args &a, hipStream_t st)
     if (a.dbias || dz) {
         const dim3 grid(static_cast<unsigned>((N + plan.across * 8 - 1) / (plan.across * 8)), static_cast<unsigned>(plan.strips));
         slope_kernel<T><<<grid, 256, 0, st>>>(a, dz, dz_low, sums, plan.across);
-        if (sums && plan.strips > 1) am_launch_column_join(sums, plan.strips, N, a.dbias, st);
+        if (sums && plan.strips > 1) am_launch_column_join(sums, plan.strips, N, a.dbias, nullptr, st);
     }
     const char *g = dz ? reinterpret_cast<const char *>(dz) : static_cast<const char *>(a.dy.data);
     const int64_t ld = (dz ? am_dz_stride(N) : a.dy.row_stride) * static_cast<int64_t>(sizeof(T));

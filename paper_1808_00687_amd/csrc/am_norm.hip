@@ -15,22 +15,6 @@
 namespace wfd {
 namespace {
 
-template <typename T>
-__device__ __forceinline__ const T *row(const wfst_matrix &m, int64_t r)
-{
-    return static_cast<const T *>(m.data) + r * m.row_stride;
-}
-
-template <typename T>
-__device__ __forceinline__ T *row_out(const wfst_matrix &m, int64_t r)
-{
-    return static_cast<T *>(m.data) + r * m.row_stride;
-}
-
-// chunks where a matrix has 32-bit elements are half as long (the result's type is looked at below)
-template <typename T>
-constexpr int kChunk = sizeof(T) == 4 ? 4 : 8;
-
 template <typename T, typename S, bool k8Bits>
 __global__ __launch_bounds__(S::kThreads) void norm_kernel(wfst_am_norm_args a)
 {
@@ -74,8 +58,7 @@ __global__ __launch_bounds__(S::kThreads) void norm_kernel(wfst_am_norm_args a)
             for (int e = 0; e < S::kC; e++) ss = fmaf(s[e], s[e], ss);
         });
         const float rho = 1.0f / sqrtf(row_sum<S>(ss, scratch, turn) / static_cast<float>(D) + a.eps);
-        float scale = 1.0f, inv = 1.0f;
-        bool whole = false;   // is a quotient formed by a division?
+        E4m3Quotient by;
         if constexpr (k8Bits) {
             uint32_t top = 0;
             S::each(D, t, [&](int v, int64_t c, int64_t left) {
@@ -90,14 +73,8 @@ __global__ __launch_bounds__(S::kThreads) void norm_kernel(wfst_am_norm_args a)
                     top = e < left && b > top ? b : top;
                 }
             });
-            scale = __uint_as_float(row_max_u32<S>(top, scratch, turn)) / kE4m3Max;
-            scale = scale < 1.17549435e-38f ? 1.17549435e-38f : scale;   // a NaN stays one
-            // A product with the rounded reciprocal, corrected once, is the rounded quotient
-            // (Markstein 1990) unless the divisor's bits are all ones or something leaves the
-            // range; 72.8 us for (53274, 1024) bf16, 74.5 with divisions.
-            inv = 1.0f / scale;
-            whole = __builtin_amdgcn_readfirstlane(!(scale >= 0x1p-90f && scale <= 0x1p90f) || (__float_as_uint(scale) & 0x7FFFFFu) == 0x7FFFFFu) != 0;
-            if (t == 0) a.y_scale[m] = scale;
+            by.set(row_max_u32<S>(top, scratch, turn));
+            if (t == 0) a.y_scale[m] = by.scale;
         }
         S::each(D, t, [&](int v, int64_t c, int64_t left) {
             float s[S::kC];
@@ -107,15 +84,7 @@ __global__ __launch_bounds__(S::kThreads) void norm_kernel(wfst_am_norm_args a)
             for (int e = 0; e < S::kC; e++) s[e] *= rho;
             times_gain(v, c, left, s);
             if constexpr (k8Bits) {
-                if (whole)
-#pragma unroll
-                    for (int e = 0; e < S::kC; e++) s[e] /= scale;
-                else
-#pragma unroll
-                    for (int e = 0; e < S::kC; e++) {
-                        const float q = s[e] * inv;   // alone it would move ties of e4m3
-                        s[e] = fmaf(fmaf(-q, scale, s[e]), inv, q);
-                    }
+                by.divide(s);
                 store_floats(row_out<f8>(a.y, m) + c, left, s);
             } else if (a.y.type == WFST_BF16) {
                 store_floats(row_out<bf16>(a.y, m) + c, left, s);
@@ -233,12 +202,14 @@ __global__ __launch_bounds__(256) void norm_dgain_kernel(wfst_am_norm_backward_a
     a.dgain[d] = t;
 }
 
-// 32 columns a workgroup, 32 threads a column, 4 strips of a thread on their way at a time
-__global__ __launch_bounds__(1024) void column_join_kernel(const float *partial, int64_t strips, int64_t n, float *out)
+// 32 columns a workgroup, 32 threads a column, 4 strips of a thread on their way at a
+// time; blockIdx.y: which of two sums (the second one's strips behind the first one's)
+__global__ __launch_bounds__(1024) void column_join_kernel(const float *partial, int64_t strips, int64_t n, float *out, float *out2)
 {
     __shared__ float part[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + x;
+    if (blockIdx.y) partial += strips * n, out = out2;
     float t = 0.0f;
     if (c < n) {
         int64_t s = y;
@@ -305,7 +276,7 @@ void launch_norm_backward(const wfst_am_norm_backward_args &a, hipStream_t st)
         const unsigned g = M ? am_row_blocks<S>(M, kBackwardBlocks) : 0;
         if constexpr (S::kNv > 0) {
             if (M) norm_backward_kernel<T, S><<<g, S::kThreads, 0, st>>>(a, a.dgain ? work : nullptr, nullptr);
-            if (a.dgain) am_launch_column_join(work, g, D, a.dgain, st);
+            if (a.dgain) am_launch_column_join(work, g, D, a.dgain, nullptr, st);
         } else {
             // the gain's gradient before dx may overwrite dy
             wfst_am_norm_backward_args b = a;
@@ -321,9 +292,9 @@ void launch_norm_backward(const wfst_am_norm_backward_args &a, hipStream_t st)
 
 }  // namespace
 
-void am_launch_column_join(const float *partial, int64_t strips, int64_t n, float *out, hipStream_t st)
+void am_launch_column_join(const float *partial, int64_t strips, int64_t n, float *out, float *out2, hipStream_t st)
 {
-    column_join_kernel<<<static_cast<unsigned>((n + 31) / 32), 1024, 0, st>>>(partial, strips, n, out);
+    column_join_kernel<<<dim3(static_cast<unsigned>((n + 31) / 32), out2 ? 2 : 1), 1024, 0, st>>>(partial, strips, n, out, out2);
 }
 
 hipError_t am_launch_norm(const wfst_am_norm_args &a, hipStream_t st)

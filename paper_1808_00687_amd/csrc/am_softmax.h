@@ -5,12 +5,6 @@
 
 namespace wfd {
 
-template <typename T>
-__device__ __forceinline__ const T *row(const wfst_matrix &m, int64_t r)
-{
-    return static_cast<const T *>(m.data) + r * m.row_stride;
-}
-
 constexpr float kLog2e = 1.44269504f;
 constexpr float kFloatMax = 3.40282347e38f;
 
