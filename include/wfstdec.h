@@ -767,6 +767,46 @@ int wfst_am_distill(const wfst_am_distill_args *args, void *hip_stream);
 int wfst_am_distill_backward(const wfst_am_distill_args *args, void *hip_stream);
 
 /*
+ * wfst_am_clip -- the norm of several tensors together (a model's gradients),
+ * and the tensors times what keeps it within a limit:
+ *   norm = sqrt(sum of all values' squares)
+ *   out_i = g_i * (norm > max_norm ? max_norm / norm : 1)
+ *
+ *   grads    [count] matrices, a host array that is read during the call; each
+ *            WFST_F32, WFST_F16 or WFST_BF16, of any size (rows >= 0, cols >= 1)
+ *   outs     [count] matrices as the grads (types and shapes), or NULL: each
+ *            grad itself.  An output may be its own grad (same data, stride),
+ *            but may not overlap another one or an output, so without outs no
+ *            tensor is given twice
+ *   count    0 to WFST_AM_MAX_TENSORS
+ *   max_norm > 0; INFINITY clips nothing (the norm alone)
+ *   norm     [1] float32 output: the norm before the clipping; an infinity where
+ *            it is larger than float32 values are
+ *   workspace  at least wfst_am_clip_workspace bytes, 256-byte aligned
+ *
+ * Squares are summed and the factor is held in 64 bits.  Where nothing is to be
+ * clipped a grad in place is not written.  With a NaN among the values the norm
+ * is one and nothing is clipped; an infinity makes the norm infinite and, unless
+ * max_norm is, the factor 0: infinities become NaN, the others 0.
+ * Errors: WFST_EINVAL (also a workspace that is too small), WFST_ENOMEM,
+ * WFST_EDEVICE.
+ */
+#define WFST_AM_MAX_TENSORS 65536
+
+typedef struct wfst_am_clip_args {
+    const wfst_matrix *grads, *outs;
+    int64_t count;
+    double max_norm;
+    float *norm;
+    void *workspace;
+    int64_t workspace_bytes;
+} wfst_am_clip_args;
+
+/* The workspace that args needs; it depends on count. */
+int wfst_am_clip_workspace(const wfst_am_clip_args *args, int64_t *bytes);
+int wfst_am_clip(const wfst_am_clip_args *args, void *hip_stream);
+
+/*
  * wfst_am_loglikes -- logits to the rows that wfst_decode reads:
  *   ll[m][l] = scale (logits[m][l] - log sum_l' exp(logits[m][l']) - log_prior[l])
  * A unit whose logit or log prior is -inf (never seen in training) has ll

@@ -12,7 +12,7 @@ stream or a raw handle) or else torch's current stream, so they can be captured
 into a graph.  Results that a call takes no place for, or is given none for, and
 the gradients' workspaces come from torch's allocator on that stream: an 8-bit
 norm's scales, a loss and its lse, and all that wfst_am_linear_backward,
-wfst_am_norm_backward and wfst_am_layer_norm_backward return always do.  (The C calls allocate nothing.)  Arguments that the library
+wfst_am_norm_backward and wfst_am_layer_norm_backward return, and wfst_am_clip's norm, always do.  (The C calls allocate nothing.)  Arguments that the library
 refuses raise WfstError (WFST_EINVAL) with its message.
 
 Autograd does not follow these calls: an operand that requires a gradient is
@@ -24,7 +24,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -83,6 +83,11 @@ class _DistillArgs(C.Structure):
                 ("reserved", C.c_int32)]
 
 
+class _ClipArgs(C.Structure):
+    _fields_ = [("grads", C.c_void_p), ("outs", C.c_void_p), ("count", C.c_int64), ("max_norm", C.c_double),
+                ("norm", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 class _LoglikesArgs(C.Structure):
     _fields_ = [("logits", _Matrix), ("ll", _Matrix), ("log_prior", C.c_void_p), ("scale", C.c_float),
                 ("reserved", C.c_int32)]
@@ -94,15 +99,16 @@ _M = "Pqqqii"
 _PACK = {"linear": struct.Struct(_M * 5 + "PPPii"), "linear_backward": struct.Struct(_M * 6 + "PPqii"),
          "norm": struct.Struct(_M * 4 + "PPfi"), "norm_backward": struct.Struct(_M * 4 + "PPPqfi"),
          "layer_norm": struct.Struct(_M * 4 + "PPPfi"), "layer_norm_backward": struct.Struct(_M * 4 + "PPPPqfi"),
-         "distill": struct.Struct(_M * 3 + "PPPPfi"), "loglikes": struct.Struct(_M * 2 + "Pfi")}
+         "distill": struct.Struct(_M * 3 + "PPPPfi"), "clip": struct.Struct("PPqdPPq"),
+         "loglikes": struct.Struct(_M * 2 + "Pfi")}
 _NONE = (0, 0, 0, 0, 0, 0)
 
 for _n in ("linear", "linear_backward", "norm", "norm_backward", "layer_norm", "layer_norm_backward", "distill",
-           "distill_backward", "loglikes"):
+           "distill_backward", "clip", "loglikes"):
     _f = getattr(_lib, "wfst_am_" + _n)
     _f.argtypes = [C.c_char_p, C.c_void_p]
     _f.restype = C.c_int
-for _n in ("linear_backward", "norm_backward", "layer_norm_backward"):
+for _n in ("linear_backward", "norm_backward", "layer_norm_backward", "clip"):
     _f = getattr(_lib, "wfst_am_%s_workspace" % _n)
     _f.argtypes = [C.c_char_p, C.POINTER(C.c_int64)]
     _f.restype = C.c_int
@@ -179,11 +185,13 @@ class _On:
 
 def _here(f):
     """f, which works on the current device and stream, with a ``stream``
-    argument and on the device of its first argument."""
+    argument and on the device of its first argument (or of that one's first tensor)."""
     operand = f.__code__.co_varnames[0]
 
     def call(*args, stream=None, **kw):
         first = args[0] if args else kw.get(operand)
+        if isinstance(first, (list, tuple)) and first:
+            first = first[0]
         if stream is None and (not isinstance(first, torch.Tensor) or not first.is_cuda
                                or first.get_device() == torch._C._cuda_getDevice()):
             return f(*args, **kw)
@@ -422,6 +430,60 @@ def wfst_am_distill_backward(logits: torch.Tensor, top_index: torch.Tensor, top_
     if given:
         _written((dlogits,))
     return dlogits
+
+
+def _tensors(ts, name: str, device: int, keep: Optional[list] = None) -> list:
+    """Tensors of any shape as wfst_matrix fields, one after the other.  A dense one is rows of its last
+    dimension; one that is not has to be a matrix."""
+    flat = []
+    recorded = torch.is_grad_enabled()
+    for t in ts:
+        code = _TYPES.get(t.dtype)
+        if code is None:
+            raise TypeError("%s: type %s is not taken" % (name, t.dtype))
+        if recorded and t.requires_grad:
+            raise ValueError(_NO_GRAPH % name)
+        if t.get_device() != device:
+            raise ValueError("%s must be on one GPU" % name)
+        n = t.numel()
+        if n and not t.is_contiguous():
+            if t.dim() == 2 or keep is None:
+                flat.extend(_matrix(t, name, device, keep))
+                continue
+            t = t.contiguous()
+            keep.append(t)
+        cols = t.shape[-1] if t.dim() and n else 1
+        flat.extend((t.data_ptr(), n // cols, cols, cols, code, 0))
+    return flat
+
+
+@_here
+def wfst_am_clip(grads: Sequence[torch.Tensor], max_norm: float, *, out: Optional[Sequence[torch.Tensor]] = None
+                 ) -> Tuple[Sequence[torch.Tensor], torch.Tensor]:
+    """(out, norm): the tensors times what keeps the norm of all of them within
+    ``max_norm`` (infinity: as they are), in ``out`` (tensors of the same types
+    and shapes) or else in place; ``norm`` [1] is that before the clipping
+    (wfst_am_clip).  Tensors that are not dense have to be matrices; a
+    parameter's gradient may be of any shape."""
+    if not isinstance(grads, (list, tuple)) or not grads:
+        raise TypeError("grads must be a list of one tensor or more")
+    d, n, keep = _device(grads[0], "grads"), len(grads), []
+    if out is not None and (len(out) != n or any(o.shape != g.shape for o, g in zip(out, grads))):
+        raise ValueError("out must have the shapes of grads")
+    to = grads if out is None else out
+    fields = struct.Struct(_M * n)
+    written = fields.pack(*_tensors(to, "grads" if out is None else "out", d))
+    read = written if out is None else fields.pack(*_tensors(grads, "grads", d, keep))
+    first = grads[0]
+    norm = first.new_empty(1, dtype=torch.float32)
+    at = C.cast(C.c_char_p(read), C.c_void_p).value
+    head = (at, 0 if out is None else C.cast(C.c_char_p(written), C.c_void_p).value, n, max_norm, norm.data_ptr())
+    pack = _PACK["clip"].pack
+    need = _bytes_for("wfst_am_clip_workspace", pack(*head, 0, 0))
+    work = first.new_empty(need, dtype=torch.uint8)
+    _call("wfst_am_clip", pack(*head, work.data_ptr(), need), _raw_stream(d))
+    _written(tuple(to))
+    return to, norm
 
 
 @_here

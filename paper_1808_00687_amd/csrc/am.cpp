@@ -1,8 +1,11 @@
 // Entry points of the acoustic-model operators: the argument checks (before
 // any device call), then one launcher each.
+#include <algorithm>
 #include <cmath>
 #include <cstddef>
 #include <cstdint>
+#include <exception>
+#include <vector>
 
 #include "am.h"
 #include "internal.h"
@@ -305,6 +308,59 @@ bool check(Checks &c, const wfst_am_distill_args &a, bool backward)
     return !a.dlogits.data || apart_or_same(c, a.dlogits, a.logits, kOverlap);
 }
 
+bool check_sizes(Checks &c, const wfst_am_clip_args &a)
+{
+    return c.need(a.count >= 0 && a.count <= WFST_AM_MAX_TENSORS, "the tensors must be 0 to 65536");
+}
+
+// Outputs lie apart from one another and from all other grads.  Spans are gone
+// through in the order of their first bytes; those that the present one may overlap
+// are kept, so tensors with places of their own cost a sort.
+bool check_places(Checks &c, const wfst_am_clip_args &a, Range norm, Range workspace)
+{
+    struct Span {
+        Range r;
+        int64_t i;     // tensor; -1: the norm or the workspace
+        bool written;
+    };
+    std::vector<Span> spans, outs, ins;   // all; those written and those read that reach as far as the present one
+    spans.reserve(static_cast<size_t>(a.count) * 2 + 2);
+    for (int64_t i = 0; i < a.count; i++) {
+        spans.push_back({range_of(a.outs ? a.outs[i] : a.grads[i]), i, true});
+        if (a.outs && !same_place(a.outs[i], a.grads[i])) spans.push_back({range_of(a.grads[i]), i, false});
+    }
+    spans.push_back({norm, -1, true});
+    spans.push_back({workspace, -1, true});
+    std::sort(spans.begin(), spans.end(), [](const Span &x, const Span &y) { return x.r.lo < y.r.lo; });
+    for (const Span &s : spans) {
+        if (s.r.lo == s.r.hi) continue;
+        for (std::vector<Span> *v : {&outs, &ins}) std::erase_if(*v, [&](const Span &o) { return o.r.hi <= s.r.lo; });
+        for (const Span &o : outs)
+            if (!c.apart(s.r, o.r, kOverlap)) return false;
+        if (s.written)
+            for (const Span &o : ins)
+                if (!c.apart(s.r, o.r, kOverlap)) return false;
+        (s.written ? outs : ins).push_back(s);
+    }
+    return true;
+}
+
+bool check(Checks &c, const wfst_am_clip_args &a)
+{
+    if (!check_sizes(c, a)) return false;
+    if (!c.need(a.max_norm > 0.0, "max_norm must be positive")) return false;
+    if (!c.need(a.grads || a.count == 0, "grads is NULL") || !c.vector(a.norm, "norm", true)) return false;
+    for (int64_t i = 0; i < a.count; i++) {
+        const wfst_matrix &g = a.grads[i];
+        if (!c.dims(g.rows, g.cols) || !c.matrix(g, "a grad", g.rows, g.cols, kFloats)) return false;
+        if (a.outs && !c.matrix(a.outs[i], "an output", g.rows, g.cols, 1u << g.type)) return false;
+    }
+    const int64_t need = am_clip_bytes(a);
+    if (!c.need(a.workspace && a.workspace_bytes >= need, "the workspace is too small")) return false;
+    if (!c.need(reinterpret_cast<uintptr_t>(a.workspace) % 256 == 0, "the workspace is not aligned")) return false;
+    return check_places(c, a, range_of(a.norm, 4), range_of(a.workspace, need));
+}
+
 bool check(Checks &c, const wfst_am_loglikes_args &a)
 {
     const int64_t M = a.logits.rows, L = a.logits.cols;
@@ -423,6 +479,30 @@ extern "C" int wfst_am_distill_backward(const wfst_am_distill_args *args, void *
     Checks c{"wfst_am_distill_backward"};
     if (!check(c, *args, true)) return WFST_EINVAL;
     return args->logits.rows ? launched(am_launch_distill(*args, true, stream_of(hip_stream)), c.who) : WFST_OK;
+}
+
+extern "C" int wfst_am_clip_workspace(const wfst_am_clip_args *args, int64_t *bytes)
+{
+    clear_error();
+    if (!args || !bytes) return no_args("wfst_am_clip_workspace");
+    Checks c{"wfst_am_clip_workspace"};
+    if (!check_sizes(c, *args)) return WFST_EINVAL;
+    *bytes = am_clip_bytes(*args);
+    return WFST_OK;
+}
+
+extern "C" int wfst_am_clip(const wfst_am_clip_args *args, void *hip_stream)
+{
+    clear_error();
+    if (!args) return no_args("wfst_am_clip");
+    Checks c{"wfst_am_clip"};
+    try {
+        if (!check(c, *args)) return WFST_EINVAL;
+    } catch (const std::exception &) {   // no memory for the list of places
+        set_error("%s: out of host memory", c.who);
+        return WFST_ENOMEM;
+    }
+    return launched(am_launch_clip(*args, stream_of(hip_stream)), c.who);
 }
 
 extern "C" int wfst_am_loglikes(const wfst_am_loglikes_args *args, void *hip_stream)

@@ -1,5 +1,6 @@
 // Acoustic-model operators: what the checks (am.cpp) and the kernels
-// (am_norm.hip, am_layer_norm.hip, am_distill.hip, am_loglikes.hip, am_linear*.hip) share.
+// (am_norm.hip, am_layer_norm.hip, am_distill.hip, am_clip.hip,
+// am_loglikes.hip, am_linear*.hip) share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -22,6 +23,8 @@ hipError_t am_launch_layer_norm(const wfst_am_layer_norm_args &a, hipStream_t st
 int64_t am_layer_norm_backward_bytes(const wfst_am_layer_norm_backward_args &a);
 hipError_t am_launch_layer_norm_backward(const wfst_am_layer_norm_backward_args &a, hipStream_t stream);   // M >= 0
 hipError_t am_launch_distill(const wfst_am_distill_args &a, bool backward, hipStream_t stream);
+int64_t am_clip_bytes(const wfst_am_clip_args &a);
+hipError_t am_launch_clip(const wfst_am_clip_args &a, hipStream_t stream);   // count >= 0
 hipError_t am_launch_loglikes(const wfst_am_loglikes_args &a, hipStream_t stream);
 
 inline int64_t am_type_bytes(int32_t type)

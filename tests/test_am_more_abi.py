@@ -12,7 +12,8 @@ from test_am_abi import A, ROOT, am, matrix, put  # noqa: F401
 torch = pytest.importorskip("torch")
 
 STRUCTS = {"wfst_am_layer_norm_args": ("layer_norm", "_LayerNormArgs"),
-           "wfst_am_layer_norm_backward_args": ("layer_norm_backward", "_LayerNormBackwardArgs")}
+           "wfst_am_layer_norm_backward_args": ("layer_norm_backward", "_LayerNormBackwardArgs"),
+           "wfst_am_clip_args": ("clip", "_ClipArgs")}
 
 
 def test_structs_match_the_header(am, tmp_path):  # noqa: F811
@@ -60,7 +61,17 @@ def layer_norm_backward(am):  # noqa: F811
     return a
 
 
-MAKE = {f.__name__: f for f in (layer_norm, layer_norm_backward)}
+def clip(am):  # noqa: F811
+    """Two grads in places of their own, outputs in others.  The matrices live as long as the arguments."""
+    a = am._ClipArgs()
+    a.kept = ((am._Matrix * 2)(matrix(am, 0, 4, 16, 2), matrix(am, 1, 1, 9, 0)),
+              (am._Matrix * 2)(matrix(am, 2, 4, 16, 2), matrix(am, 3, 1, 9, 0)))
+    a.grads, a.outs = (C.cast(k, C.c_void_p) for k in a.kept)
+    a.count, a.max_norm, a.norm, a.workspace, a.workspace_bytes = 2, 1.0, A[5], A[6], 1 << 20
+    return a
+
+
+MAKE = {f.__name__: f for f in (layer_norm, layer_norm_backward, clip)}
 
 REFUSED = [
     ("layer_norm", {"x.type": 3}), ("layer_norm", {"x.cols": 0}), ("layer_norm", {"x.rows": -1}),
@@ -92,6 +103,60 @@ def test_refusals(am, name, change):  # noqa: F811
         put(a, path, v)
     assert getattr(am._lib, "wfst_am_" + name)(bytes(a), None) == wfstdec.WFST_EINVAL
     assert wfstdec.wfst_last_error().startswith("wfst_am_" + name)
+
+
+CLIP_REFUSED = [
+    ({"count": -1}, {}), ({"count": 65537}, {}), ({"max_norm": 0.0}, {}), ({"max_norm": -1.0}, {}),
+    ({"max_norm": math.nan}, {}), ({"norm": None}, {}), ({"norm": A[5] + 2}, {}), ({"norm": A[2] + 4}, {}),
+    ({"norm": A[1] + 4}, {}), ({"norm": A[6] + 64}, {}), ({"workspace": None}, {}), ({"workspace_bytes": 100}, {}),
+    ({"workspace": A[6] + 8}, {}), ({"workspace": A[0]}, {}), ({"workspace": A[3]}, {}), ({"grads": None}, {}),
+    ({}, {"grads.0.type": 3}), ({}, {"grads.0.rows": -1}), ({}, {"grads.1.cols": 0}), ({}, {"grads.1.data": None}),
+    ({}, {"grads.0.row_stride": 15}), ({}, {"grads.0.data": A[0] + 1}), ({}, {"outs.0.type": 1}),
+    ({}, {"outs.0.cols": 15}), ({}, {"outs.1.rows": 2}), ({}, {"outs.1.data": A[3] + 2}),
+    # an output over another one, over another's grad, beside its own grad's place, in its place with other rows
+    ({}, {"outs.1.data": A[2] + 60}), ({}, {"outs.1.data": A[0]}), ({}, {"outs.0.data": A[0] + 2}),
+    ({}, {"outs.0.data": A[0], "outs.0.row_stride": 17}), ({"outs": None}, {"grads.1.data": A[0]}),
+]
+
+
+@pytest.mark.parametrize("change,inner", CLIP_REFUSED)
+def test_clip_refusals(am, change, inner):  # noqa: F811
+    from paper_1808_00687_amd import wfstdec
+    a = clip(am)
+    for path, v in change.items():
+        put(a, path, v)
+    for path, v in inner.items():
+        which, i, field = path.split(".")
+        setattr(a.kept[which == "outs"][int(i)], field, v)
+    assert am._lib.wfst_am_clip(bytes(a), None) == wfstdec.WFST_EINVAL
+    assert wfstdec.wfst_last_error().startswith("wfst_am_clip")
+
+
+def test_clip_workspace(am):  # noqa: F811
+    from paper_1808_00687_amd import wfstdec
+    n = C.c_int64(-1)
+    q = am._lib.wfst_am_clip_workspace
+    sizes = []
+    for count in (0, 1, 71, 72, 1000, 65536):
+        a = am._ClipArgs()
+        a.count = count
+        assert q(bytes(a), C.byref(n)) == 0 and n.value > 0
+        sizes.append(n.value)
+    assert sizes == sorted(sizes)
+    a.count = 65537
+    assert q(bytes(a), C.byref(n)) == wfstdec.WFST_EINVAL
+    assert q(None, C.byref(n)) == wfstdec.WFST_EINVAL and q(bytes(a), None) == wfstdec.WFST_EINVAL
+
+
+def test_clip_binding_refuses(am):  # noqa: F811
+    x = torch.zeros(2, 8)
+    for grads in (x, [], iter([x]), None):
+        with pytest.raises(TypeError, match="list"):
+            am.wfst_am_clip(grads, 1.0)
+    with pytest.raises(TypeError, match="GPU"):
+        am.wfst_am_clip([x], 1.0)
+    with pytest.raises(TypeError, match="GPU"):
+        am.wfst_am_clip(grads=(x,), max_norm=1.0, stream=0)
 
 
 @pytest.mark.parametrize("name", list(MAKE))
