@@ -600,6 +600,69 @@ int wfst_am_linear_backward_workspace(const wfst_am_linear_backward_args *args, 
 int wfst_am_linear_backward(const wfst_am_linear_backward_args *args, void *hip_stream);
 
 /*
+ * wfst_am_gated -- one gated layer over M rows: two projections of the same
+ * rows, the first one's activation times the second one:
+ *   z[m][n] = sum_k x[m][k] w[n][k]  (* x_scale[m] * w_scale[n])  + bias[n],  n < 2 N
+ *   y[m][n] = act(z[m][n]) * z[m][N + n],  n < N
+ *
+ *   x        [M x K], w [2 N x K] (the gates' rows, then the values'), of one
+ *            type: WFST_F16, WFST_BF16 or WFST_F8E4M3; M >= 0, K >= 1, N >= 1;
+ *            M, K and 2 N at most 2^30, and no matrix of more than 2^40 elements
+ *   pre      [M x 2 N] optional output: z, of y's type (for the gradient)
+ *   y        [M x N] output, WFST_F32, WFST_F16 or WFST_BF16
+ *   x_scale  [M], w_scale [2 N] float32: as in wfst_am_linear
+ *   bias     [2 N] float32 or NULL
+ *   activation  any; WFST_ACT_NONE makes y the projections' product
+ *
+ * Errors: WFST_EINVAL, WFST_EDEVICE.
+ */
+typedef struct wfst_am_gated_args {
+    wfst_matrix x, w, pre, y;
+    const float *x_scale, *w_scale, *bias;
+    int32_t activation;
+    int32_t reserved;
+} wfst_am_gated_args;
+
+int wfst_am_gated(const wfst_am_gated_args *args, void *hip_stream);
+
+/*
+ * wfst_am_gated_backward -- gradients of wfst_am_gated (16-bit types); with
+ * pre = [gate value]:
+ *   dz = [dy * value * act'(gate), dy * act(gate)]
+ *   dx = dz w;  dw = dz^T x;  dbias[n] = sum_m dz[m][n]
+ *
+ *   dy       [M x N], pre [M x 2 N], x [M x K], w [2 N x K], all of one type,
+ *            WFST_F16 or WFST_BF16
+ *   dx [M x K], dw [2 N x K], dbias [2 N] float32: outputs, each optional; dx
+ *            and dw WFST_F32, WFST_F16 or WFST_BF16.  x is read for dw only and w
+ *            for dx only (data may be NULL otherwise)
+ *   workspace  at least wfst_am_gated_backward_workspace bytes, 256-byte aligned
+ *   round_dz  0 or 1
+ *
+ * The products read dz as the sum of two 16-bit values, within 2^-16 (WFST_BF16)
+ * or 2^-22 (WFST_F16, or 2^-35 if that is more) of it; round_dz = 1 makes it one,
+ * rounded to nearest (16-bit dx and dw 1.4 times as far from the exact ones, in a
+ * little over half the time).  In WFST_F16 a dz of magnitude 131,008 or more
+ * (65,504 with round_dz) is an infinity in the products; dbias sums the float32 dz.
+ * M = 0 gives zero dw, dbias.  Sizes as for wfst_am_gated.
+ * Errors: WFST_EINVAL (also a workspace that is too small), WFST_EDEVICE.
+ */
+typedef struct wfst_am_gated_backward_args {
+    wfst_matrix dy, pre, x, w, dx, dw;
+    float *dbias;
+    void *workspace;
+    int64_t workspace_bytes;
+    int32_t activation;
+    int32_t round_dz;
+} wfst_am_gated_backward_args;
+
+/* The workspace that args needs (its workspace fields and data pointers are
+   only tested for NULL); it depends on sizes, types, round_dz and which outputs
+   are asked for. */
+int wfst_am_gated_backward_workspace(const wfst_am_gated_backward_args *args, int64_t *bytes);
+int wfst_am_gated_backward(const wfst_am_gated_backward_args *args, void *hip_stream);
+
+/*
  * wfst_am_norm -- root-mean-square norm of each row, with the residual's
  * addition before it and an output in 8 bits after it:
  *   s = x + residual;  v = s / sqrt(mean(s^2) + eps) * gain

@@ -11,8 +11,9 @@ The calls only enqueue, on the ``stream`` that each takes by name (a torch
 stream or a raw handle) or else torch's current stream, so they can be captured
 into a graph.  Results that a call takes no place for, or is given none for, and
 the gradients' workspaces come from torch's allocator on that stream: an 8-bit
-norm's scales, a loss and its lse, and all that wfst_am_linear_backward,
-wfst_am_norm_backward and wfst_am_layer_norm_backward return, and wfst_am_clip's norm, always do.  (The C calls allocate nothing.)  Arguments that the library
+norm's scales, a loss and its lse, and all that
+wfst_am_linear_backward, wfst_am_gated_backward, wfst_am_norm_backward and
+wfst_am_layer_norm_backward return, and wfst_am_clip's norm, always do.  (The C calls allocate nothing.)  Arguments that the library
 refuses raise WfstError (WFST_EINVAL) with its message.
 
 Autograd does not follow these calls: an operand that requires a gradient is
@@ -53,6 +54,15 @@ class _LinearBackwardArgs(C.Structure):
     _fields_ = [("dy", _Matrix), ("pre", _Matrix), ("x", _Matrix), ("w", _Matrix), ("dx", _Matrix), ("dw", _Matrix),
                 ("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
                 ("activation", C.c_int32), ("round_dz", C.c_int32)]
+
+
+class _GatedArgs(C.Structure):
+    _fields_ = [("x", _Matrix), ("w", _Matrix), ("pre", _Matrix), ("y", _Matrix), ("x_scale", C.c_void_p),
+                ("w_scale", C.c_void_p), ("bias", C.c_void_p), ("activation", C.c_int32), ("reserved", C.c_int32)]
+
+
+class _GatedBackwardArgs(C.Structure):
+    _fields_ = list(_LinearBackwardArgs._fields_)
 
 
 class _NormArgs(C.Structure):
@@ -97,18 +107,19 @@ class _LoglikesArgs(C.Structure):
 # per call than a small kernel runs); the layouts are the structures' above.
 _M = "Pqqqii"
 _PACK = {"linear": struct.Struct(_M * 5 + "PPPii"), "linear_backward": struct.Struct(_M * 6 + "PPqii"),
+         "gated": struct.Struct(_M * 4 + "PPPii"), "gated_backward": struct.Struct(_M * 6 + "PPqii"),
          "norm": struct.Struct(_M * 4 + "PPfi"), "norm_backward": struct.Struct(_M * 4 + "PPPqfi"),
          "layer_norm": struct.Struct(_M * 4 + "PPPfi"), "layer_norm_backward": struct.Struct(_M * 4 + "PPPPqfi"),
          "distill": struct.Struct(_M * 3 + "PPPPfi"), "clip": struct.Struct("PPqdPPq"),
          "loglikes": struct.Struct(_M * 2 + "Pfi")}
 _NONE = (0, 0, 0, 0, 0, 0)
 
-for _n in ("linear", "linear_backward", "norm", "norm_backward", "layer_norm", "layer_norm_backward", "distill",
-           "distill_backward", "clip", "loglikes"):
+for _n in ("linear", "linear_backward", "gated", "gated_backward", "norm", "norm_backward", "layer_norm",
+           "layer_norm_backward", "distill", "distill_backward", "clip", "loglikes"):
     _f = getattr(_lib, "wfst_am_" + _n)
     _f.argtypes = [C.c_char_p, C.c_void_p]
     _f.restype = C.c_int
-for _n in ("linear_backward", "norm_backward", "layer_norm_backward", "clip"):
+for _n in ("linear_backward", "gated_backward", "norm_backward", "layer_norm_backward", "clip"):
     _f = getattr(_lib, "wfst_am_%s_workspace" % _n)
     _f.argtypes = [C.c_char_p, C.POINTER(C.c_int64)]
     _f.restype = C.c_int
@@ -281,6 +292,62 @@ def wfst_am_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Opti
     need = _bytes_for("wfst_am_linear_backward_workspace", pack(*head, 0, 0, act, rounded))
     work = dy.new_empty(need, dtype=torch.uint8) if need else None
     _call("wfst_am_linear_backward", pack(*head, work.data_ptr() if need else 0, need, act, rounded), _raw_stream(d))
+    return dx, dw, db
+
+
+@_here
+def wfst_am_gated(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
+                  activation: str = "silu", x_scale: Optional[torch.Tensor] = None,
+                  w_scale: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """act(gate) * value, both of z = x w^T [* x_scale w_scale] + bias: x [M x K],
+    w [2 N x K], the gates' rows and then the values' -> [M x N] (wfst_am_gated).
+    ``out_dtype``: that of ``out``, else x's (bfloat16 for 8-bit x).  ``pre``
+    [M x 2 N] receives z, for the gradient."""
+    d, keep = _device(x, "x"), []
+    mx, mw = _matrix(x, "x", d, keep), _matrix(w, "w", d, keep)
+    if mw[1] % 2:
+        raise ValueError("w must have a row for each gate and one for each value")
+    given = out is not None
+    if not given:
+        dt = out_dtype or (torch.bfloat16 if x.dtype == torch.float8_e4m3fn else x.dtype)
+        out = x.new_empty((mx[1], mw[1] // 2), dtype=dt)
+    elif out_dtype is not None and out_dtype != out.dtype:
+        raise ValueError("out_dtype differs from out's")
+    _call("wfst_am_gated", _PACK["gated"].pack(
+        *mx, *mw, *(_NONE if pre is None else _matrix(pre, "pre", d)), *_matrix(out, "out", d),
+        _vector(x_scale, "x_scale", mx[1], d), _vector(w_scale, "w_scale", mw[1], d),
+        _vector(bias, "bias", mw[1], d), _activation(activation), 0), _raw_stream(d))
+    if pre is not None:
+        _written((pre,))
+    if given:
+        _written((out,))
+    return out
+
+
+@_here
+def wfst_am_gated_backward(dy: torch.Tensor, pre: torch.Tensor, x: Optional[torch.Tensor], w: Optional[torch.Tensor], *,
+                           activation: str = "silu", bias_gradient: bool = True,
+                           weight_dtype: Optional[torch.dtype] = None, round_dz: bool = False
+                           ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(dx, dw, dbias) of wfst_am_gated with a 16-bit x, from its ``pre``.  ``w``
+    None leaves out dx, ``x`` None dw.  ``weight_dtype``: dw's type, dy's by
+    default.  ``round_dz``: dx and dw from a dz rounded to 16 bits, faster, where
+    two 16-bit values hold it otherwise."""
+    d, keep = _device(dy, "dy"), []
+    act, rounded = _activation(activation), int(bool(round_dz))
+    mdy, mpre = _matrix(dy, "dy", d, keep), _matrix(pre, "pre", d, keep)
+    mx = _NONE if x is None else _matrix(x, "x", d, keep)
+    mw = _NONE if w is None else _matrix(w, "w", d, keep)
+    dx = None if w is None else dy.new_empty((mdy[1], mw[2]))
+    dw = None if x is None else dy.new_empty((2 * mdy[2], mx[2]), dtype=weight_dtype or dy.dtype)
+    db = dy.new_empty(2 * mdy[2], dtype=torch.float32) if bias_gradient else None
+    head = (*mdy, *mpre, *mx, *mw, *(_NONE if dx is None else _matrix(dx, "dx", d)),
+            *(_NONE if dw is None else _matrix(dw, "dw", d)), 0 if db is None else db.data_ptr())
+    pack = _PACK["gated_backward"].pack
+    need = _bytes_for("wfst_am_gated_backward_workspace", pack(*head, 0, 0, act, rounded))
+    work = dy.new_empty(need, dtype=torch.uint8) if need else None
+    _call("wfst_am_gated_backward", pack(*head, work.data_ptr() if need else 0, need, act, rounded), _raw_stream(d))
     return dx, dw, db
 
 

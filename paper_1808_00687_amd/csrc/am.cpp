@@ -187,6 +187,66 @@ bool check(Checks &c, const wfst_am_linear_backward_args &a)
     return true;
 }
 
+bool check(Checks &c, const wfst_am_gated_args &a)
+{
+    const int64_t M = a.x.rows, K = a.x.cols, N = a.y.cols;
+    const bool f8 = a.x.type == WFST_F8E4M3;
+    if (!c.need(N >= 1 && N <= INT32_MAX, "y must have 1 to 2^31 - 1 columns")) return false;
+    if (!c.product_dims(M, K) || !c.product_dims(M, 2 * N) || !c.product_dims(2 * N, K)) return false;
+    if (!c.need(good_activation(a.activation), "unknown activation")) return false;
+    if (!c.matrix(a.x, "x", M, K, kHalves | 1u << WFST_F8E4M3)) return false;
+    if (!c.matrix(a.w, "w", 2 * N, K, 1u << a.x.type)) return false;
+    if (!c.matrix(a.y, "y", M, N, kFloats)) return false;
+    if (a.pre.data && !c.matrix(a.pre, "pre", M, 2 * N, 1u << a.y.type)) return false;
+    if (!c.need(f8 || (!a.x_scale && !a.w_scale), "scales are for 8-bit operands")) return false;
+    if (!c.vector(a.x_scale, "x_scale", f8 && M > 0) || !c.vector(a.w_scale, "w_scale", f8)) return false;
+    if (!c.vector(a.bias, "bias", false)) return false;
+    const Range in[] = {range_of(a.x), range_of(a.w), range_of(a.x_scale, 4 * M), range_of(a.w_scale, 8 * N),
+                        range_of(a.bias, 8 * N)};
+    const Range y = range_of(a.y), pre = range_of(a.pre);
+    for (const Range &r : in)
+        if (!c.apart(y, r, kOverlap) || !c.apart(pre, r, kOverlap)) return false;
+    return c.apart(y, pre, kOverlap);
+}
+
+// everything but the pointers: what the workspace depends on
+bool check_sizes(Checks &c, const wfst_am_gated_backward_args &a)
+{
+    const int64_t M = a.dy.rows, N = a.dy.cols;
+    if (!c.need(N >= 1 && N <= INT32_MAX, "dy must have 1 to 2^31 - 1 columns") || !c.product_dims(M, 2 * N)) return false;
+    if (!c.need(good_activation(a.activation), "unknown activation")) return false;
+    if (!c.need(a.round_dz == 0 || a.round_dz == 1, "round_dz must be 0 or 1")) return false;
+    if (!c.need(a.dy.type == WFST_F16 || a.dy.type == WFST_BF16, "dy has a type that is not taken here")) return false;
+    if (a.dx.data && (!c.product_dims(M, a.dx.cols) || !c.product_dims(2 * N, a.dx.cols))) return false;
+    return !a.dw.data || (c.product_dims(2 * N, a.dw.cols) && c.product_dims(M, a.dw.cols));
+}
+
+bool check(Checks &c, const wfst_am_gated_backward_args &a)
+{
+    if (!check_sizes(c, a)) return false;
+    const int64_t M = a.dy.rows, N = a.dy.cols;
+    const uint32_t type = 1u << a.dy.type;
+    if (!c.matrix(a.dy, "dy", M, N, type) || !c.matrix(a.pre, "pre", M, 2 * N, type)) return false;
+    if (a.dx.data && (!c.matrix(a.dx, "dx", M, a.dx.cols, kFloats) || !c.matrix(a.w, "w", 2 * N, a.dx.cols, type)))
+        return false;
+    if (a.dw.data && (!c.matrix(a.dw, "dw", 2 * N, a.dw.cols, kFloats) || !c.matrix(a.x, "x", M, a.dw.cols, type)))
+        return false;
+    if (!c.vector(a.dbias, "dbias", false)) return false;
+    const int64_t need = am_gated_backward_bytes(a);
+    if (!c.need(need == 0 || (a.workspace && a.workspace_bytes >= need), "the workspace is too small")) return false;
+    if (!c.need(reinterpret_cast<uintptr_t>(a.workspace) % 256 == 0, "the workspace is not aligned")) return false;
+    const Range none{0, 0};
+    const Range in[] = {range_of(a.dy), range_of(a.pre), a.dw.data ? range_of(a.x) : none, a.dx.data ? range_of(a.w) : none};
+    const Range out[] = {range_of(a.dx), range_of(a.dw), range_of(a.dbias, 8 * N), range_of(a.workspace, need)};
+    for (int i = 0; i < 4; i++) {
+        for (const Range &r : in)
+            if (!c.apart(out[i], r, kOverlap)) return false;
+        for (int j = 0; j < i; j++)
+            if (!c.apart(out[i], out[j], kOverlap)) return false;
+    }
+    return true;
+}
+
 bool good_eps(float eps) { return std::isfinite(eps) && eps > 0.0f; }
 
 bool check(Checks &c, const wfst_am_norm_args &a)
@@ -405,6 +465,34 @@ extern "C" int wfst_am_linear_backward(const wfst_am_linear_backward_args *args,
     Checks c{"wfst_am_linear_backward"};
     if (!check(c, *args)) return WFST_EINVAL;
     return launched(am_launch_linear_backward(*args, stream_of(hip_stream)), c.who);
+}
+
+extern "C" int wfst_am_gated(const wfst_am_gated_args *args, void *hip_stream)
+{
+    clear_error();
+    if (!args) return no_args("wfst_am_gated");
+    Checks c{"wfst_am_gated"};
+    if (!check(c, *args)) return WFST_EINVAL;
+    return args->x.rows ? launched(am_launch_gated(*args, stream_of(hip_stream)), c.who) : WFST_OK;
+}
+
+extern "C" int wfst_am_gated_backward_workspace(const wfst_am_gated_backward_args *args, int64_t *bytes)
+{
+    clear_error();
+    if (!args || !bytes) return no_args("wfst_am_gated_backward_workspace");
+    Checks c{"wfst_am_gated_backward_workspace"};
+    if (!check_sizes(c, *args)) return WFST_EINVAL;
+    *bytes = am_gated_backward_bytes(*args);
+    return WFST_OK;
+}
+
+extern "C" int wfst_am_gated_backward(const wfst_am_gated_backward_args *args, void *hip_stream)
+{
+    clear_error();
+    if (!args) return no_args("wfst_am_gated_backward");
+    Checks c{"wfst_am_gated_backward"};
+    if (!check(c, *args)) return WFST_EINVAL;
+    return launched(am_launch_gated_backward(*args, stream_of(hip_stream)), c.who);
 }
 
 extern "C" int wfst_am_norm(const wfst_am_norm_args *args, void *hip_stream)

@@ -1,6 +1,6 @@
 // Acoustic-model operators: what the checks (am.cpp) and the kernels
 // (am_norm.hip, am_layer_norm.hip, am_distill.hip, am_clip.hip,
-// am_loglikes.hip, am_linear*.hip) share.
+// am_loglikes.hip, am_linear*.hip, am_gated*.hip) share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -16,6 +16,9 @@ namespace wfd {
 hipError_t am_launch_linear(const wfst_am_linear_args &a, hipStream_t stream);
 int64_t am_linear_backward_bytes(const wfst_am_linear_backward_args &a);
 hipError_t am_launch_linear_backward(const wfst_am_linear_backward_args &a, hipStream_t stream);   // M >= 0
+hipError_t am_launch_gated(const wfst_am_gated_args &a, hipStream_t stream);
+int64_t am_gated_backward_bytes(const wfst_am_gated_backward_args &a);
+hipError_t am_launch_gated_backward(const wfst_am_gated_backward_args &a, hipStream_t stream);     // M >= 0
 hipError_t am_launch_norm(const wfst_am_norm_args &a, hipStream_t stream);
 int64_t am_norm_backward_bytes(const wfst_am_norm_backward_args &a);
 hipError_t am_launch_norm_backward(const wfst_am_norm_backward_args &a, hipStream_t stream);       // M >= 0

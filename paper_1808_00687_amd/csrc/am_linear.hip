@@ -5,19 +5,6 @@
 namespace wfd {
 namespace {
 
-// act'(z)
-__device__ __forceinline__ float slope(float z, int32_t kind)
-{
-    if (kind == WFST_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if (kind == WFST_ACT_SILU) {
-        const float s = __builtin_amdgcn_rcpf(1.0f + am_exp(-z));
-        return s * (1.0f + z * (1.0f - s));
-    }
-    float bell;
-    const float n = am_normal(z, bell);
-    return fmaf(z * 0.39894228f, bell, n);
-}
-
 // Sums the parts of a split product and finishes them.
 __global__ __launch_bounds__(256) void join_kernel(AmProduct p)
 {
@@ -59,20 +46,8 @@ __global__ __launch_bounds__(256) void slope_kernel(wfst_am_linear_backward_args
                 float z[8];
                 load_floats(static_cast<const T *>(a.pre.data) + m * a.pre.row_stride + n, N - n, z);
 #pragma unroll
-                for (int e = 0; e < 8; e++) g[e] *= slope(z[e], a.activation);
-                if (dz_low) {
-                    float high[8], low[8];
-#pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        high[e] = g[e] * (1.0f / AmParts<T>::kHigh);
-                        const float held = static_cast<float>(static_cast<T>(high[e])) * AmParts<T>::kHigh;
-                        low[e] = fabsf(held) < INFINITY ? (g[e] - held) * (1.0f / AmParts<T>::kLow) : 0.0f;
-                    }
-                    store_floats(dz + m * ld + n, N - n, high);
-                    store_floats(dz_low + m * ld + n, N - n, low);
-                } else if (dz) {
-                    store_floats(dz + m * ld + n, N - n, g);
-                }
+                for (int e = 0; e < 8; e++) g[e] *= am_slope(z[e], a.activation);
+                if (dz) am_store_dz(dz + m * ld + n, dz_low ? dz_low + m * ld + n : nullptr, N - n, g);
             }
 #pragma unroll
             for (int e = 0; e < 8; e++) sum[e] += g[e];
@@ -93,7 +68,7 @@ __global__ __launch_bounds__(256) void slope_kernel(wfst_am_linear_backward_args
 template <typename T>
 void launch_backward(const wfst_am_linear_backward_args &a, hipStream_t st)
 {
-    const int64_t M = a.dy.rows, N = a.dy.cols;
+    const int64_t N = a.dy.cols;
     const BackwardPlan plan = am_backward_plan(a);
     char *work = static_cast<char *>(a.workspace);
     T *dz = plan.dz_bytes ? reinterpret_cast<T *>(work) : nullptr;
@@ -107,29 +82,8 @@ void launch_backward(const wfst_am_linear_backward_args &a, hipStream_t st)
     }
     const char *g = dz ? reinterpret_cast<const char *>(dz) : static_cast<const char *>(a.dy.data);
     const int64_t ld = (dz ? am_dz_stride(N) : a.dy.row_stride) * static_cast<int64_t>(sizeof(T));
-    float *partial = reinterpret_cast<float *>(work);   // the column sums are joined by then
-    if (a.dx.data && M > 0) {
-        AmProduct p{};
-        p.a = {g, ld, static_cast<int32_t>(M)};
-        p.a_low = reinterpret_cast<const char *>(dz_low);
-        p.b = {static_cast<const char *>(a.w.data), a.w.row_stride * 2, static_cast<int32_t>(a.dx.cols)};
-        p.inner = static_cast<int32_t>(N);
-        p.splits = plan.dx.splits;
-        p.partial = partial;
-        p.out = a.dx;
-        am_product_dx<T>(p, plan.dx.tile, st);
-    }
-    if (a.dw.data) {
-        AmProduct p{};
-        p.a = {g, ld, static_cast<int32_t>(N)};
-        p.a_low = reinterpret_cast<const char *>(dz_low);
-        p.b = {static_cast<const char *>(a.x.data), a.x.row_stride * 2, static_cast<int32_t>(a.dw.cols)};
-        p.inner = static_cast<int32_t>(M);
-        p.splits = plan.dw.splits;
-        p.partial = partial;   // the other product's parts are joined by now
-        p.out = a.dw;
-        am_product_dw<T>(p, plan.dw.tile, st);
-    }
+    // the column sums are joined before the products' parts take their place
+    am_launch_gradient_products<T>(a, plan, g, reinterpret_cast<const char *>(dz_low), ld, reinterpret_cast<float *>(work), st);
 }
 
 }  // namespace

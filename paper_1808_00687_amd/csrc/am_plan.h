@@ -24,6 +24,15 @@ inline bool am_direct(const AmOperand &o, bool major, int32_t inner, int el)
     return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && row % 16 == 0 && am_near(o);
 }
 
+// A gated layer's weights: b.extent rows of gates, then as many of values.  A tile has
+// rows of both, whose offsets stay in 31 bits.
+inline bool am_gated_near(const AmOperand &b) { return am_near(b) && b.extent * b.ld < (int64_t{1} << 30); }
+
+inline bool am_gated_direct(const AmOperand &a, const AmOperand &b, int32_t inner, int el)
+{
+    return am_direct(a, false, inner, el) && am_direct(b, false, inner, el) && am_gated_near(b);
+}
+
 inline int64_t am_tiles(int64_t rows, int64_t cols, int64_t m, int64_t n) { return ((rows + m - 1) / m) * ((cols + n - 1) / n); }
 
 // go(first, count) for consecutive runs of `blocks` workgroups, each run a launch: one

@@ -36,22 +36,28 @@ __device__ __forceinline__ i32x4 am_thin_load(const AmOperand &o, int64_t row, i
     return i32x4{static_cast<int>(w[0]), static_cast<int>(w[1]), static_cast<int>(w[2]), static_cast<int>(w[3])};
 }
 
-template <typename E, int TI, int TJ>
+// kGated: the first half of the TJ fragments are gates, the second half the same
+// results' values, p.b.extent rows behind them.
+template <typename E, int TI, int TJ, bool kGated>
 __global__ __launch_bounds__(kThinWaves * 64, 2) void am_thin_kernel(AmProduct p)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int kWide = 16 / static_cast<int>(sizeof(E)), kStep = 4 * kWide;   // values of k in a fragment's row
     constexpr int kUnroll = TI + TJ <= 2 ? 8 : TI + TJ <= 3 ? 4 : 2;           // steps under way
-    constexpr int kCols = TJ * 16, kRows = TI * 16, kValues = kRows * kCols;
+    constexpr int kCols = TJ * 16, kRows = TI * 16, kResults = kGated ? kCols / 2 : kCols, kValues = kRows * kResults;
     constexpr int kOwn = kValues <= kThinWaves * 64 ? 1 : kValues / (kThinWaves * 64);   // results a thread finishes
     __shared__ float part[kThinWaves][kRows][kCols + 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, s = lane & 15;
-    const int64_t tiles_j = (static_cast<int64_t>(p.b.extent) + kCols - 1) / kCols;
-    const int64_t block = p.first + blockIdx.x, i0 = block / tiles_j * kRows, j0 = block % tiles_j * kCols;
+    const int64_t tiles_j = (static_cast<int64_t>(p.b.extent) + kResults - 1) / kResults;
+    const int64_t block = p.first + blockIdx.x, i0 = block / tiles_j * kRows, j0 = block % tiles_j * kResults;
 
     int64_t row_a[TI], row_b[TJ];   // past the end: the last row again, whose results are not stored
     am_each<TI>([&](auto f) { row_a[f] = i0 + f * 16 + s < p.a.extent ? i0 + f * 16 + s : p.a.extent - 1; });
-    am_each<TJ>([&](auto f) { row_b[f] = j0 + f * 16 + s < p.b.extent ? j0 + f * 16 + s : p.b.extent - 1; });
+    am_each<TJ>([&](auto f) {
+        constexpr bool kValue = kGated && f >= TJ / 2;
+        const int64_t j = j0 + (kValue ? f - TJ / 2 : f) * 16 + s;
+        row_b[f] = (j < p.b.extent ? j : p.b.extent - 1) + (kValue ? p.b.extent : 0);
+    });
     const int32_t steps = (p.inner + kStep - 1) / kStep;
     const int32_t s_first = static_cast<int32_t>(static_cast<int64_t>(steps) * wave / kThinWaves);
     const int32_t s_last = static_cast<int32_t>(static_cast<int64_t>(steps) * (wave + 1) / kThinWaves);
@@ -92,28 +98,39 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void am_thin_kernel(AmProduct p
         am_each<TJ>([&](auto h) { *reinterpret_cast<f32x4 *>(&part[wave][f * 16 + s][h * 16 + g * 4]) = acc[f][h]; });
     });
     __syncthreads();
-    const int at = threadIdx.x * kOwn, ri = at / kCols, rj = at % kCols;
+    const int at = threadIdx.x * kOwn, ri = at / kResults, rj = at % kResults;
     const int64_t i = i0 + ri, j = j0 + rj;
     if (at >= kValues || i >= p.a.extent || j >= p.b.extent) return;
-    float v[kOwn], b_scale[kOwn], bias[kOwn];
+    const auto sum = [&](int c) {
+        float t = part[0][ri][c];
+#pragma unroll
+        for (int w = 1; w < kThinWaves; w++) t += part[w][ri][c];
+        return t;
+    };
+    float b_scale[kOwn], bias[kOwn];
     am_columns(p, j, b_scale, bias);
+    if constexpr (kGated) {
+        float v[2 * kOwn], v_scale[kOwn], v_bias[kOwn];
+        am_columns(p, j, v_scale, v_bias, p.b.extent);
 #pragma unroll
-    for (int e = 0; e < kOwn; e++) {
-        v[e] = part[0][ri][rj + e];
+        for (int e = 0; e < kOwn; e++) v[e] = sum(rj + e), v[kOwn + e] = sum(kResults + rj + e);
+        am_finish_gated<kOwn>(p, i, j, v, b_scale, bias, v_scale, v_bias);
+    } else {
+        float v[kOwn];
 #pragma unroll
-        for (int w = 1; w < kThinWaves; w++) v[e] += part[w][ri][rj + e];
+        for (int e = 0; e < kOwn; e++) v[e] = sum(rj + e);
+        am_finish(p, i, j, v, b_scale, bias);
     }
-    am_finish(p, i, j, v, b_scale, bias);
 #endif
 }
 
-template <typename E, int TI, int TJ>
+template <typename E, int TI, int TJ, bool kGated = false>
 void am_launch_thin(const AmProduct &p, hipStream_t st)
 {
-    am_in_launches(am_tiles(p.a.extent, p.b.extent, TI * 16, TJ * 16), [&](uint32_t first, uint32_t blocks) {
+    am_in_launches(am_tiles(p.a.extent, p.b.extent, TI * 16, kGated ? TJ * 8 : TJ * 16), [&](uint32_t first, uint32_t blocks) {
         AmProduct part = p;
         part.first = first;
-        am_thin_kernel<E, TI, TJ><<<blocks, kThinWaves * 64, 0, st>>>(part);
+        am_thin_kernel<E, TI, TJ, kGated><<<blocks, kThinWaves * 64, 0, st>>>(part);
     });
 }
 
@@ -132,6 +149,19 @@ void am_thin(const AmProduct &p, hipStream_t st)
     else if (r22 <= r21 && r22 <= r11) am_launch_thin<E, 2, 2>(p, st);
     else if (r21 <= r11) am_launch_thin<E, 2, 1>(p, st);
     else am_launch_thin<E, 1, 1>(p, st);
+}
+
+// The same for gated layers, with a fragment of gates and one of values a workgroup.
+template <typename E>
+void am_gated_thin(const AmProduct &p, hipStream_t st)
+{
+    const auto rows = [&](int ti) {
+        return (am_tiles(p.a.extent, p.b.extent, ti * 16, 16) + kComputeUnits - 1) / kComputeUnits * (ti + 2);
+    };
+    const int64_t r1 = rows(1), r2 = rows(2), r4 = rows(4);
+    if (r4 <= r2 && r4 <= r1) am_launch_thin<E, 4, 2, true>(p, st);
+    else if (r2 <= r1) am_launch_thin<E, 2, 2, true>(p, st);
+    else am_launch_thin<E, 1, 2, true>(p, st);
 }
 
 }  // namespace wfd

@@ -30,6 +30,12 @@
 // results are 4 consecutive j of one i.  Where b is k-contiguous the rows of b
 // are dealt to the fragments so that a lane holds 4 * TJ consecutive j.
 //
+// Gated layers have two rows of b for each result, a gate's and a value's, b.extent
+// rows apart.  A tile takes half as many of either: the first half of the rows that
+// make up a lane's run are gates, the second half the same results' values, so
+// both meet in one lane's registers and nothing but the products' addresses and
+// the epilogue differs.
+//
 // Measured, bf16: (16384, 4096, 1024) k-contiguous 107 us, 1,280 TFLOP/s (the
 // library's product 94 us); (16384, 4096, 1024) with b k-major 120; k = 16384
 // into 4096 x 1024, both k-major, 139 and 17 for joining 4 parts; with a in two parts
@@ -80,6 +86,7 @@ struct AmProduct {
     float *partial;            // [splits][a.extent][b.extent]
     const float *a_scale, *b_scale, *bias;
     wfst_matrix residual, pre, out;
+    wfst_matrix value_pre;     // gated: the values' half of pre (pre is the gates')
     int32_t activation;
     uint32_t first;            // tile of the launch's first workgroup
 };
@@ -214,12 +221,38 @@ __device__ __forceinline__ void am_finish(const AmProduct &p, int64_t i, int64_t
     am_store(p.out, i, j, v, full);
 }
 
+// The epilogue of N results of a gated row i from j on (j < cols): v holds their gates, then their values.
 template <int N>
-__device__ __forceinline__ void am_columns(const AmProduct &p, int64_t j, float (&b_scale)[N], float (&bias)[N])
+__device__ __forceinline__ void am_finish_gated(const AmProduct &p, int64_t i, int64_t j, const float (&v)[2 * N],
+                                                const float (&g_scale)[N], const float (&g_bias)[N],
+                                                const float (&v_scale)[N], const float (&v_bias)[N])
+{
+    const bool full = j + N <= p.b.extent;
+    float gate[N], value[N];
+    const float s = p.a_scale ? p.a_scale[i] : 1.0f;
+#pragma unroll
+    for (int e = 0; e < N; e++) {
+        gate[e] = v[e], value[e] = v[N + e];
+        if (p.a_scale) gate[e] *= s * g_scale[e], value[e] *= s * v_scale[e];
+        if (p.bias) gate[e] += g_bias[e], value[e] += v_bias[e];
+    }
+    if (p.pre.data) {
+        am_store(p.pre, i, j, gate, full);
+        am_store(p.value_pre, i, j, value, full);
+    }
+    am_activate(gate, p.activation);
+#pragma unroll
+    for (int e = 0; e < N; e++) gate[e] *= value[e];
+    am_store(p.out, i, j, gate, full);
+}
+
+// of columns from j + `skip` on (skip: the values' columns of a gated layer)
+template <int N>
+__device__ __forceinline__ void am_columns(const AmProduct &p, int64_t j, float (&b_scale)[N], float (&bias)[N], int64_t skip = 0)
 {
 #pragma unroll
     for (int e = 0; e < N; e++) {
-        const int64_t c = j + e < p.b.extent ? j + e : p.b.extent - 1;
+        const int64_t c = (j + e < p.b.extent ? j + e : p.b.extent - 1) + skip;
         b_scale[e] = p.b_scale ? p.b_scale[c] : 1.0f;
         bias[e] = p.bias ? p.bias[c] : 0.0f;
     }
@@ -275,8 +308,9 @@ constexpr int am_log2(int x) { return x <= 1 ? 0 : 1 + am_log2(x / 2); }
 // One operand's part of the tile kernel: R rows (i or j) of SB bytes a stage,
 // kMajor its storage, kDeal > 1: rows dealt to fragments so that a lane gets
 // kDeal runs of 4 rows; kFar: rows so far apart that offsets inside a tile pass
-// 31 bits.
-template <typename E, int R, int SB, int kWaves, bool kMajor, int kDeal, bool kFar>
+// 31 bits; kGated: of every 4 * kDeal rows the first half are gates and the second
+// half their values, which lie o.extent rows behind them.
+template <typename E, int R, int SB, int kWaves, bool kMajor, int kDeal, bool kFar, bool kGated = false>
 struct AmSide {
     static constexpr int kEl = sizeof(E);
     static constexpr int kWide = 16 / kEl;                       // values of a chunk
@@ -285,6 +319,15 @@ struct AmSide {
     static constexpr int kPerWave = kBytes / 1024 / kWaves;      // fetches of 1 KiB a wave
     static constexpr int kHalves = SB / 64;                      // fragments along k
     static_assert(kBytes % (1024 * kWaves) == 0 && (kEl == 2 || !kMajor) && (kHalves == 1 || kHalves == 2), "");
+    static_assert(!kGated || (!kMajor && kDeal > 1), "");
+
+    // the operand's row that a tile's row is, counted from the tile's first; is it a value's?
+    __device__ static __forceinline__ int source(int row)
+    {
+        if constexpr (kGated) return row / (4 * kDeal) * (2 * kDeal) + row % (2 * kDeal);
+        else return row;
+    }
+    __device__ static __forceinline__ bool is_value(int row) { return kGated && row % (4 * kDeal) >= 2 * kDeal; }
 
     // chunk permutation of a stored row
     __device__ static __forceinline__ int permute(int row)
@@ -314,8 +357,11 @@ struct AmSide {
     __device__ __forceinline__ void init(const AmOperand &o, int wave, int lane)
     {
 #pragma unroll
-        for (int q = 0; q < kPerWave; q++)
-            voff[q] = row_of(q, wave, lane) * static_cast<int32_t>(o.ld) + chunk_of(q, wave, lane) * 16;
+        for (int q = 0; q < kPerWave; q++) {
+            const int row = row_of(q, wave, lane);
+            voff[q] = source(row) * static_cast<int32_t>(o.ld) + chunk_of(q, wave, lane) * 16;
+            if (is_value(row)) voff[q] += o.extent * static_cast<int32_t>(o.ld);
+        }
     }
 
     // Before the fetch of a last, partial stage with `tail` bytes of k: chunks
@@ -340,7 +386,7 @@ struct AmSide {
             size = (static_cast<int64_t>(inner) - 1) * o.ld + static_cast<int64_t>(o.extent) * kEl;
         } else {
             skip = first * o.ld + static_cast<int64_t>(k0) * kEl;
-            size = (static_cast<int64_t>(o.extent) - 1) * o.ld + static_cast<int64_t>(inner) * kEl;
+            size = (static_cast<int64_t>(o.extent) * (kGated ? 2 : 1) - 1) * o.ld + static_cast<int64_t>(inner) * kEl;
         }
         const int64_t left = there ? size - skip : 0;
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(o.data) + skip, 0,
@@ -366,8 +412,10 @@ struct AmSide {
         const int32_t last = kMajor ? inner - k0 - 1 : o.extent - static_cast<int32_t>(first) - 1;
 #pragma unroll
         for (int q = 0; q < kPerWave; q++) {
-            int32_t row = row_of(q, wave, lane), at = from + chunk_of(q, wave, lane) * kWide;
+            const int32_t in_tile = row_of(q, wave, lane);
+            int32_t row = source(in_tile), at = from + chunk_of(q, wave, lane) * kWide;
             row = row < last ? row : last;
+            if (is_value(in_tile)) row += o.extent;
             const AM_GLOBAL char *p = base + static_cast<Offset>(row) * static_cast<Offset>(o.ld);
             if (length >= kWide) {
                 at = at < length - kWide ? at : length - kWide;
@@ -462,7 +510,7 @@ struct AmShape {
 
 // kTwice: a is in two parts.  The whole of k is gone through twice into the same
 // sums: the low parts, a change of scale, the high parts.
-template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kFar, bool kTwice>
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kFar, bool kTwice, bool kGated>
 __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(AmProduct p)
 {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub alone
@@ -470,7 +518,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
     constexpr int kWaves = S::WM * WN, TI = BM / S::WM / 16, TJ = BN / WN / 16, kK = SB / static_cast<int>(sizeof(E));
     constexpr int kDeal = kMajorB ? 1 : TJ;
     using SideA = AmSide<E, BM, SB, kWaves, kMajorA, 1, kFar>;
-    using SideB = AmSide<E, BN, SB, kWaves, kMajorB, kDeal, kFar>;
+    using SideB = AmSide<E, BN, SB, kWaves, kMajorB, kDeal, kFar, kGated>;
+    constexpr int kResults = kGated ? BN / 2 : BN;   // columns of a tile
     // one object a stage, so the compiler knows that a fetch into one does not touch the others
     __shared__ __attribute__((aligned(1024))) char a0[SideA::kBytes], a1[SideA::kBytes];
     __shared__ __attribute__((aligned(1024))) char a2[kBuffers > 2 ? SideA::kBytes : 1], a3[kBuffers > 3 ? SideA::kBytes : 1];
@@ -491,8 +540,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
 
     const int lane_ = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t ti, tj;
-    am_tile_of(p.first + blockIdx.x, (p.a.extent + BM - 1) / BM, (p.b.extent + BN - 1) / BN, ti, tj);
-    const int64_t i0 = static_cast<int64_t>(ti) * BM, j0 = static_cast<int64_t>(tj) * BN;
+    am_tile_of(p.first + blockIdx.x, (p.a.extent + BM - 1) / BM, (p.b.extent + kResults - 1) / kResults, ti, tj);
+    const int64_t i0 = static_cast<int64_t>(ti) * BM, j0 = static_cast<int64_t>(tj) * kResults;
     const int wi = wave / WN * (BM / S::WM), wj = wave % WN * (BN / WN);
 
     const int32_t stages = (p.inner + kK - 1) / kK;
@@ -691,6 +740,25 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
                 am_set<e>(acc[f][3], w[1]);
             });
         });
+    if constexpr (kGated) {
+        constexpr int kOwn = kRun / 2;
+        const int64_t j = j0 + wj / 2 + (lane_ >> 4) * kOwn;
+        if (j >= p.b.extent) return;
+        float g_scale[kOwn], g_bias[kOwn], v_scale[kOwn], v_bias[kOwn];
+        am_columns(p, j, g_scale, g_bias);
+        am_columns(p, j, v_scale, v_bias, p.b.extent);
+        am_each<TI>([&](auto f) {
+            const int64_t i = i0 + wi + f * 16 + (lane_ & 15);
+            if (i >= p.a.extent) return;
+            float v[kRun];
+            am_each<TJ>([&](auto d) {
+                const f32x4 a = acc[f][d];
+                v[d * 4] = a[0], v[d * 4 + 1] = a[1], v[d * 4 + 2] = a[2], v[d * 4 + 3] = a[3];
+            });
+            am_finish_gated<kOwn>(p, i, j, v, g_scale, g_bias, v_scale, v_bias);
+        });
+        return;
+    }
     const int64_t j = j0 + wj + (lane_ >> 4) * kRun;
     if (j >= p.b.extent) return;
     float b_scale[kRun], bias[kRun];
@@ -717,13 +785,13 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
 // sums the parts of a split product and finishes them (am_linear.hip)
 void am_launch_join(const AmProduct &p, hipStream_t st);
 
-template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kTwice, bool kFar = false>
+template <typename E, bool kMajorA, bool kMajorB, bool kDirect, typename S, bool kTwice, bool kFar = false, bool kGated = false>
 void am_launch_tiles(const AmProduct &p, hipStream_t st)
 {
-    am_in_launches(am_tiles(p.a.extent, p.b.extent, S::BM, S::BN), [&](uint32_t first, uint32_t blocks) {
+    am_in_launches(am_tiles(p.a.extent, p.b.extent, S::BM, kGated ? S::BN / 2 : S::BN), [&](uint32_t first, uint32_t blocks) {
         AmProduct part = p;
         part.first = first;
-        am_tile_kernel<E, kMajorA, kMajorB, kDirect, S, kFar, kTwice><<<dim3(blocks, p.splits), S::kThreads, 0, st>>>(part);
+        am_tile_kernel<E, kMajorA, kMajorB, kDirect, S, kFar, kTwice, kGated><<<dim3(blocks, p.splits), S::kThreads, 0, st>>>(part);
     });
     if (p.splits > 1) am_launch_join(p, st);
 }
@@ -756,6 +824,25 @@ void am_product(const AmProduct &p, int32_t tile, hipStream_t st)
         am_launch_tiles<E, kMajorA, kMajorB, false, AmMediumStaged, kTwice>(p, st);
     } else {
         am_launch_tiles<E, kMajorA, kMajorB, false, std::conditional_t<kMajorB, AmSmallMajorStaged, AmSmallStaged>, kTwice>(p, st);
+    }
+}
+
+// y = act(a gates^T) * (a values^T), all k-contiguous: p.b the gates, the values p.b.extent rows behind them
+template <typename E>
+void am_gated_product(const AmProduct &p, int32_t tile, hipStream_t st)
+{
+    if (am_gated_direct(p.a, p.b, p.inner, sizeof(E))) {
+        if (tile == 256) am_launch_tiles<E, false, false, true, std::conditional_t<sizeof(E) == 1, AmLarge8, AmLarge>, false, false, true>(p, st);
+        else if (tile == 128 && am_tiles(p.a.extent, 2 * int64_t{p.b.extent}, 128, 128) <= kComputeUnits)
+            am_launch_tiles<E, false, false, true, AmMediumDeep, false, false, true>(p, st);
+        else if (tile == 128) am_launch_tiles<E, false, false, true, AmMedium, false, false, true>(p, st);
+        else am_launch_tiles<E, false, false, true, AmSmall, false, false, true>(p, st);
+    } else if (!am_near(p.a) || !am_gated_near(p.b)) {
+        am_launch_tiles<E, false, false, false, AmSmallStaged, false, true, true>(p, st);
+    } else if (tile >= 128) {
+        am_launch_tiles<E, false, false, false, AmMediumStaged, false, false, true>(p, st);
+    } else {
+        am_launch_tiles<E, false, false, false, AmSmallStaged, false, false, true>(p, st);
     }
 }
 

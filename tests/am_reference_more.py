@@ -72,3 +72,35 @@ def layer_norm_backward(dy, s, gain, dsum, eps):
     dg, db = (dy * mo.h).sum(0), dy.sum(0)
     e_dg = R.sum_bound(m, (dy * mo.h).abs().sum(0)) + (dy.abs() * mo.err).sum(0) * 1.01
     return dx, dg, db, err, e_dg, R.sum_bound(m, dy.abs().sum(0))
+
+
+def gated(x, w, bias, kind, x_scale=None, w_scale=None):
+    """(y, z, bound on z's error, bound on y's, both before a rounding).  The activation is good to 8 u of its
+    value and its argument, and its slope is at most ACT_LIPSCHITZ."""
+    _, z, err = R.linear(x, w, bias, "none", None, x_scale, w_scale)
+    n = z.shape[1] // 2
+    a, v = R.act(z[:, :n], kind), z[:, n:]
+    e_a = R.ACT_LIPSCHITZ * err[:, :n] + 8 * U32 * (a.abs() + z[:, :n].abs())
+    y = a * v
+    return y, z, err, e_a * v.abs() + a.abs() * err[:, n:] + e_a * err[:, n:] + U32 * y.abs()
+
+
+def gated_dz(dy, pre, kind):
+    """(dz, bound on its error): products' roundings, and a slope and an activation good to 16 u (1 + |gate|)."""
+    dy, pre = d(dy), d(pre)
+    n = dy.shape[1]
+    gate, value = pre[:, :n], pre[:, n:]
+    dz = torch.cat([dy * value * R.slope(gate, kind), dy * R.act(gate, kind)], 1)
+    loose = 16 * U32 * (1 + gate.abs()) * dy.abs()
+    return dz, torch.cat([loose * value.abs(), loose], 1)
+
+
+# what two 16-bit values leave of dz: relative, absolute
+LEFT = {torch.bfloat16: (2.0 ** -16, 0.0), torch.float16: (2.0 ** -22, 2.0 ** -35)}
+
+
+def product(a, b, slack, rel, least, tiny):
+    """(a b, bound) where a is held to `slack`, and to rel of it or least besides, as independent errors."""
+    want = a @ b
+    err = R.sum_bound(2 * a.shape[1], a.abs() @ b.abs()) + (slack + least) @ b.abs()
+    return want, err + R.LAMBDA * rel * torch.sqrt((a * a) @ (b * b)) + tiny * b.abs().sum(0)

@@ -13,6 +13,8 @@ torch = pytest.importorskip("torch")
 
 STRUCTS = {"wfst_am_layer_norm_args": ("layer_norm", "_LayerNormArgs"),
            "wfst_am_layer_norm_backward_args": ("layer_norm_backward", "_LayerNormBackwardArgs"),
+           "wfst_am_gated_args": ("gated", "_GatedArgs"),
+           "wfst_am_gated_backward_args": ("gated_backward", "_GatedBackwardArgs"),
            "wfst_am_clip_args": ("clip", "_ClipArgs")}
 
 
@@ -71,7 +73,22 @@ def clip(am):  # noqa: F811
     return a
 
 
-MAKE = {f.__name__: f for f in (layer_norm, layer_norm_backward, clip)}
+def gated(am):  # noqa: F811
+    a = am._GatedArgs()
+    a.x, a.w, a.pre, a.y = matrix(am, 0, 4, 16, 2), matrix(am, 1, 16, 16, 2), matrix(am, 2, 4, 16, 0), matrix(am, 3, 4, 8, 0)
+    a.bias, a.activation = A[4], 2
+    return a
+
+
+def gated_backward(am):  # noqa: F811
+    a = am._GatedBackwardArgs()
+    a.dy, a.pre, a.x, a.w = (matrix(am, 0, 4, 8, 1), matrix(am, 1, 4, 16, 1), matrix(am, 2, 4, 16, 1), matrix(am, 3, 16, 16, 1))
+    a.dx, a.dw, a.dbias = matrix(am, 4, 4, 16, 1), matrix(am, 5, 16, 16, 0), A[6]
+    a.workspace, a.workspace_bytes, a.activation = A[7], 1 << 20, 2
+    return a
+
+
+MAKE = {f.__name__: f for f in (layer_norm, layer_norm_backward, clip, gated, gated_backward)}
 
 REFUSED = [
     ("layer_norm", {"x.type": 3}), ("layer_norm", {"x.cols": 0}), ("layer_norm", {"x.rows": -1}),
@@ -92,6 +109,23 @@ REFUSED = [
     ("layer_norm_backward", {"dbias": A[5]}), ("layer_norm_backward", {"dbias": A[2]}),
     ("layer_norm_backward", {"dx.data": A[0] + 2}), ("layer_norm_backward", {"dbias": A[6] + 1}),
     ("layer_norm_backward", {"dgain": A[7]}),
+    ("gated", {"x.data": None}), ("gated", {"w.data": None}), ("gated", {"y.data": None}), ("gated", {"x.type": 0, "w.type": 0}),
+    ("gated", {"w.type": 1}), ("gated", {"y.type": 3}), ("gated", {"w.rows": 15}), ("gated", {"w.rows": 17}),
+    ("gated", {"w.cols": 15}), ("gated", {"y.cols": 9}), ("gated", {"y.cols": 0}), ("gated", {"y.cols": -8}), ("gated", {"y.rows": 5}),
+    ("gated", {"pre.cols": 8}), ("gated", {"pre.type": 2}), ("gated", {"pre.data": A[3]}), ("gated", {"pre.data": A[0]}),
+    ("gated", {"y.data": A[1]}), ("gated", {"y.data": A[2] + 32}), ("gated", {"y.data": A[4] + 32}),
+    ("gated", {"pre.data": A[4] + 60}), ("gated", {"activation": 4}), ("gated", {"activation": -1}), ("gated", {"x.rows": -1}),
+    ("gated", {"x_scale": A[5]}), ("gated", {"x.type": 3, "w.type": 3}), ("gated", {"x.type": 3, "w.type": 3, "x_scale": A[5]}),
+    ("gated", {"bias": A[4] + 2}), ("gated", {"y.cols": 1 << 30, "y.row_stride": 1 << 30}), ("gated", {"x.row_stride": 15}),
+    ("gated_backward", {"dy.type": 0}), ("gated_backward", {"dy.cols": 0}), ("gated_backward", {"dy.cols": 7}),
+    ("gated_backward", {"pre.data": None}), ("gated_backward", {"pre.cols": 8}), ("gated_backward", {"pre.type": 2}),
+    ("gated_backward", {"x.rows": 3}), ("gated_backward", {"w.rows": 8}), ("gated_backward", {"w.data": None}),
+    ("gated_backward", {"x.type": 2}), ("gated_backward", {"dx.type": 3}), ("gated_backward", {"dw.rows": 8}),
+    ("gated_backward", {"dw.cols": 0}), ("gated_backward", {"activation": 9}), ("gated_backward", {"round_dz": 2}),
+    ("gated_backward", {"round_dz": -1}), ("gated_backward", {"workspace": None}), ("gated_backward", {"workspace_bytes": 8}),
+    ("gated_backward", {"workspace": A[7] + 4}), ("gated_backward", {"workspace": A[1]}), ("gated_backward", {"dx.data": A[1]}),
+    ("gated_backward", {"dw.data": A[4]}), ("gated_backward", {"dbias": A[3] + 4}), ("gated_backward", {"dbias": A[6] + 1}),
+    ("gated_backward", {"dw.data": A[6] + 32}),
 ]
 
 
@@ -165,7 +199,7 @@ def test_refuses_no_arguments(am, name):  # noqa: F811
     assert getattr(am._lib, "wfst_am_" + name)(None, None) == wfstdec.WFST_EINVAL
 
 
-FORWARD = ["layer_norm"]
+FORWARD = ["layer_norm", "gated"]
 
 
 @pytest.mark.parametrize("name", FORWARD)
@@ -193,6 +227,7 @@ def test_workspace_queries(am, name):  # noqa: F811
 
 def test_binding_refuses_host_tensors(am):  # noqa: F811
     x = torch.zeros(2, 8)
-    for call in (lambda: am.wfst_am_layer_norm(x), lambda: am.wfst_am_layer_norm_backward(x, x)):
+    for call in (lambda: am.wfst_am_layer_norm(x), lambda: am.wfst_am_layer_norm_backward(x, x),
+                 lambda: am.wfst_am_gated(x, x), lambda: am.wfst_am_gated_backward(x, x, x, x)):
         with pytest.raises(TypeError):
             call()
