@@ -107,16 +107,15 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void am_thin_kernel(AmProduct p
         for (int w = 1; w < kThinWaves; w++) t += part[w][ri][c];
         return t;
     };
-    float b_scale[kOwn], bias[kOwn];
-    am_columns(p, j, b_scale, bias);
     if constexpr (kGated) {
-        float v[2 * kOwn], v_scale[kOwn], v_bias[kOwn];
-        am_columns(p, j, v_scale, v_bias, p.b.extent);
+        float v[2 * kOwn], b_scale[2 * kOwn], bias[2 * kOwn];
+        am_columns_gated(p, j, b_scale, bias);
 #pragma unroll
         for (int e = 0; e < kOwn; e++) v[e] = sum(rj + e), v[kOwn + e] = sum(kResults + rj + e);
-        am_finish_gated<kOwn>(p, i, j, v, b_scale, bias, v_scale, v_bias);
+        am_finish_gated<kOwn>(p, i, j, v, b_scale, bias);
     } else {
-        float v[kOwn];
+        float v[kOwn], b_scale[kOwn], bias[kOwn];
+        am_columns(p, j, b_scale, bias);
 #pragma unroll
         for (int e = 0; e < kOwn; e++) v[e] = sum(rj + e);
         am_finish(p, i, j, v, b_scale, bias);

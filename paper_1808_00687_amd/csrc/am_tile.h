@@ -221,21 +221,23 @@ __device__ __forceinline__ void am_finish(const AmProduct &p, int64_t i, int64_t
     am_store(p.out, i, j, v, full);
 }
 
-// The epilogue of N results of a gated row i from j on (j < cols): v holds their gates, then their values.
+// The epilogue of N results of a gated row i from j on (j < cols): v, scales and biases hold their gates', then their values'.
 template <int N>
-__device__ __forceinline__ void am_finish_gated(const AmProduct &p, int64_t i, int64_t j, const float (&v)[2 * N],
-                                                const float (&g_scale)[N], const float (&g_bias)[N],
-                                                const float (&v_scale)[N], const float (&v_bias)[N])
+__device__ __forceinline__ void am_finish_gated(const AmProduct &p, int64_t i, int64_t j, float (&v)[2 * N],
+                                                const float (&b_scale)[2 * N], const float (&bias)[2 * N])
 {
     const bool full = j + N <= p.b.extent;
-    float gate[N], value[N];
-    const float s = p.a_scale ? p.a_scale[i] : 1.0f;
+    if (p.a_scale) {
+        const float s = p.a_scale[i];
 #pragma unroll
-    for (int e = 0; e < N; e++) {
-        gate[e] = v[e], value[e] = v[N + e];
-        if (p.a_scale) gate[e] *= s * g_scale[e], value[e] *= s * v_scale[e];
-        if (p.bias) gate[e] += g_bias[e], value[e] += v_bias[e];
+        for (int e = 0; e < 2 * N; e++) v[e] *= s * b_scale[e];
     }
+    if (p.bias)
+#pragma unroll
+        for (int e = 0; e < 2 * N; e++) v[e] += bias[e];
+    float gate[N], value[N];
+#pragma unroll
+    for (int e = 0; e < N; e++) gate[e] = v[e], value[e] = v[N + e];
     if (p.pre.data) {
         am_store(p.pre, i, j, gate, full);
         am_store(p.value_pre, i, j, value, full);
@@ -246,13 +248,24 @@ __device__ __forceinline__ void am_finish_gated(const AmProduct &p, int64_t i, i
     am_store(p.out, i, j, gate, full);
 }
 
-// of columns from j + `skip` on (skip: the values' columns of a gated layer)
 template <int N>
-__device__ __forceinline__ void am_columns(const AmProduct &p, int64_t j, float (&b_scale)[N], float (&bias)[N], int64_t skip = 0)
+__device__ __forceinline__ void am_columns(const AmProduct &p, int64_t j, float (&b_scale)[N], float (&bias)[N])
 {
 #pragma unroll
     for (int e = 0; e < N; e++) {
-        const int64_t c = (j + e < p.b.extent ? j + e : p.b.extent - 1) + skip;
+        const int64_t c = j + e < p.b.extent ? j + e : p.b.extent - 1;
+        b_scale[e] = p.b_scale ? p.b_scale[c] : 1.0f;
+        bias[e] = p.bias ? p.bias[c] : 0.0f;
+    }
+}
+
+// of gates and values of columns from j on
+template <int N>
+__device__ __forceinline__ void am_columns_gated(const AmProduct &p, int64_t j, float (&b_scale)[N], float (&bias)[N])
+{
+#pragma unroll
+    for (int e = 0; e < N; e++) {
+        const int64_t at = j + e % (N / 2), c = (at < p.b.extent ? at : p.b.extent - 1) + (e < N / 2 ? 0 : p.b.extent);
         b_scale[e] = p.b_scale ? p.b_scale[c] : 1.0f;
         bias[e] = p.bias ? p.bias[c] : 0.0f;
     }
@@ -620,6 +633,19 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
                 do {
                     (go(std::integral_constant<int, n>{}), ...);
                 } while (s < s_last);
+            } else if constexpr (kGated) {
+                // The stages past the end are jumped over inside the loop: with an exit at
+                // each stage the sums of this epilogue were moved about and spilled (1,708 us
+                // where this form takes 325).  The copy of the count keeps the compiler
+                // from making exits of the jumps.
+                const auto unless_past = [&](auto m) {
+                    int32_t left = s_last - s;
+                    __asm__ volatile("" : "+s"(left));
+                    if (m == 0 || left > 0) go(m);
+                };
+                do {
+                    (unless_past(std::integral_constant<int, n>{}), ...);
+                } while (s < s_last);
             } else {
                 while ((go(std::integral_constant<int, n>{}) && ...)) {
                 }
@@ -744,9 +770,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
         constexpr int kOwn = kRun / 2;
         const int64_t j = j0 + wj / 2 + (lane_ >> 4) * kOwn;
         if (j >= p.b.extent) return;
-        float g_scale[kOwn], g_bias[kOwn], v_scale[kOwn], v_bias[kOwn];
-        am_columns(p, j, g_scale, g_bias);
-        am_columns(p, j, v_scale, v_bias, p.b.extent);
+        float b_scale[kRun], bias[kRun];
+        am_columns_gated(p, j, b_scale, bias);
         am_each<TI>([&](auto f) {
             const int64_t i = i0 + wi + f * 16 + (lane_ & 15);
             if (i >= p.a.extent) return;
@@ -755,7 +780,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
                 const f32x4 a = acc[f][d];
                 v[d * 4] = a[0], v[d * 4 + 1] = a[1], v[d * 4 + 2] = a[2], v[d * 4 + 3] = a[3];
             });
-            am_finish_gated<kOwn>(p, i, j, v, g_scale, g_bias, v_scale, v_bias);
+            am_finish_gated<kOwn>(p, i, j, v, b_scale, bias);
         });
         return;
     }
