@@ -1,10 +1,12 @@
 // The norm of many tensors together, and their clipping by it.
 //
 // Two passes: squares are summed, then values are multiplied by the factor that
-// the sum gives.  Both are bound by memory.  The tensors are cut into chunks of
-// 16 KB, numbered through; a workgroup takes a run of consecutive ones, so it
-// looks its first tensor up once and then only steps on.  The second pass goes
-// through each run backwards: what the first one read last may still be in a cache.
+// the sum gives.  Both are bound by memory.  The tensors are cut into chunks,
+// numbered through; a workgroup takes every blocks-th one and has the next one's
+// loads on their way while it works on the present one.  The second pass goes
+// through them backwards: what the first one read last may still be in a cache; its
+// stores are not kept there.  125 tensors of 1.6 GB: 928 us, 4.9 GB in all, 5.3 TB/s (956
+// forwards, 982 with stores that are kept, 1,213 without the loads ahead).
 //
 // The sum is held in 64 bits (a square of a float32 may be no float32, and a
 // billion of them would lose bits): a workgroup's goes to the workspace, and every
@@ -30,9 +32,13 @@ struct Tensor {
     int32_t type;
 };
 
-constexpr int kThreads = 256, kParts = 4;
-constexpr int64_t kChunkBytes = kThreads * kParts * 16;
+constexpr int kThreads = 256;
 constexpr int64_t kMostBlocks = 256 * 8;
+// Parts of 4 KB in a chunk.  The large model above takes 1,913, 1,228, 1,105, 976, 928 us with 1, 2,
+// 4, 6, 8 (12 and 16: 1,002 and 931); a small one of 15 tensors has too few chunks then, 7 us with 1 or 2
+// and 10 with 4.  Large chunks from where they are as many as the workgroups.
+constexpr int kFewParts = 2, kManyParts = 8;
+constexpr int64_t chunk_bytes(int parts) { return int64_t{kThreads} * 16 * parts; }
 constexpr int kInArgs = 71;   // what fits into 4 KB of arguments with the rest
 
 struct Table {
@@ -54,12 +60,27 @@ struct FewArgs {
 };
 static_assert(sizeof(FewArgs) <= 4096, "");
 
-// 16 bytes of values from value i of t on (i < count); values past the end are 0
+// 16 bytes of values from value i of t on; values past the end are 0
 template <typename T>
 struct Piece {
     static constexpr int C = 16 / static_cast<int>(sizeof(T));
     float v[C];
 
+    using V = T __attribute__((ext_vector_type(C)));
+
+    __device__ __forceinline__ void take(uint32_t __attribute__((ext_vector_type(4))) raw)
+    {
+        const V t = __builtin_bit_cast(V, raw);
+#pragma unroll
+        for (int e = 0; e < C; e++) v[e] = to_f32(t[e]);
+    }
+    __device__ __forceinline__ uint32_t __attribute__((ext_vector_type(4))) give() const
+    {
+        V t;
+#pragma unroll
+        for (int e = 0; e < C; e++) t[e] = static_cast<T>(v[e]);
+        return __builtin_bit_cast(uint32_t __attribute__((ext_vector_type(4))), t);
+    }
     // f(index of a value here, place of it) for the values of a piece that does not lie in one run
     template <typename F>
     __device__ __forceinline__ static void each(const Tensor &t, int64_t i, int64_t stride, F f)
@@ -103,31 +124,72 @@ struct Piece {
     }
 };
 
-// use(the tensor as its type, first value) for the workgroup's chunks
-template <bool kBackwards, typename F>
-__device__ __forceinline__ void each_chunk(const Tensor *table, const Job &j, F use)
-{
-    const int64_t from = j.chunks * blockIdx.x / j.blocks, to = j.chunks * (blockIdx.x + 1) / j.blocks;
-    if (from >= to) return;
-    int lo = 0, hi = j.tensors;   // the last tensor whose first chunk is not behind the first one wanted
-    const int64_t start = kBackwards ? to - 1 : from;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (table[mid].first <= start) lo = mid;
-        else hi = mid;
-    }
-    for (int64_t n = 0; n < to - from; n++) {
-        const int64_t c = kBackwards ? to - 1 - n : from + n;
-        if (kBackwards) {
-            if (c < table[lo].first) lo--;
-        } else if (lo + 1 < j.tensors && c >= table[lo + 1].first) {
-            lo++;
+using Raw = uint32_t __attribute__((ext_vector_type(4), aligned(1)));   // 16 bytes at any address
+
+// A chunk of a tensor, 16 bytes a thread and part.
+template <int kParts>
+struct Place {
+    static constexpr int64_t kBytes = chunk_bytes(kParts);
+    int at;           // tensor; -1: none
+    int64_t inside;   // chunk of the tensor
+    int64_t run;      // bytes from this thread's first part to the end of a tensor that lies in one run, else 0
+
+    __device__ __forceinline__ void find(const Tensor *table, const Job &j, int64_t c)
+    {
+        at = -1, inside = 0, run = 0;
+        if (c < 0 || c >= j.chunks) return;
+        int lo = 0, hi = j.tensors;   // the last tensor whose first chunk is not behind c
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (table[mid].first <= c) lo = mid;
+            else hi = mid;
         }
         const Tensor &t = table[lo];
-        if (t.type == WFST_F32) use(t, float{}, (c - t.first) * (kChunkBytes / 4));
-        else if (t.type == WFST_F16) use(t, f16{}, (c - t.first) * (kChunkBytes / 2));
-        else use(t, bf16{}, (c - t.first) * (kChunkBytes / 2));
+        at = lo, inside = c - t.first;
+        if (!t.cols) run = t.count * (t.type == WFST_F32 ? 4 : 2) - byte();
     }
+    __device__ __forceinline__ int64_t byte() const { return inside * kBytes + static_cast<int64_t>(threadIdx.x) * 16; }
+    // does part q lie inside the run?
+    __device__ __forceinline__ bool in_run(int q) const { return run >= (q * kThreads + 1) * 16; }
+    __device__ __forceinline__ void load(const Tensor *table, Raw (&r)[kParts]) const
+    {
+        if (at < 0) return;
+        const AM_GLOBAL char *p = (const AM_GLOBAL char *)table[at].data + byte();
+#pragma unroll
+        for (int q = 0; q < kParts; q++)
+            if (in_run(q)) r[q] = *(const AM_GLOBAL Raw *)(p + q * kThreads * 16);
+    }
+};
+
+// use(place, 16 bytes of each part that lies in a run) for the workgroup's chunks, every
+// j.blocks-th one; the next one's are on their way meanwhile
+template <int kParts, bool kBackwards, typename F>
+__device__ __forceinline__ void each_chunk(const Tensor *table, const Job &j, F use)
+{
+    const int64_t step = kBackwards ? -static_cast<int64_t>(j.blocks) : j.blocks;
+    int64_t c = kBackwards ? j.chunks - 1 - blockIdx.x : blockIdx.x;
+    Place<kParts> place, next;
+    Raw r[kParts], ahead[kParts];
+    place.find(table, j, c);
+    place.load(table, r);
+    while (place.at >= 0) {
+        c += step;
+        next.find(table, j, c);
+        next.load(table, ahead);
+        use(place, r);
+        place = next;
+#pragma unroll
+        for (int q = 0; q < kParts; q++) r[q] = ahead[q];
+    }
+}
+
+// go(type, bytes of it) with a value of the tensor's type
+template <typename F>
+__device__ __forceinline__ void as_type(const Tensor &t, F go)
+{
+    if (t.type == WFST_F32) go(float{});
+    else if (t.type == WFST_F16) go(f16{});
+    else go(bf16{});
 }
 
 __device__ __forceinline__ double block_sum(double v, double (&part)[kThreads / 64])
@@ -142,33 +204,33 @@ __device__ __forceinline__ double block_sum(double v, double (&part)[kThreads / 
     return v;
 }
 
+template <int kParts>
 __device__ __forceinline__ void square_sums(const Tensor *table, const Job &j)
 {
     __shared__ double part[kThreads / 64];
     double sum = 0.0;
-    each_chunk<false>(table, j, [&](const Tensor &t, auto type, int64_t first) {
-        using P = Piece<decltype(type)>;
-        P p[kParts];
+    each_chunk<kParts, false>(table, j, [&](const Place<kParts> &place, const Raw (&r)[kParts]) {
+        const Tensor &t = table[place.at];
+        as_type(t, [&](auto type) {
+            using P = Piece<decltype(type)>;
 #pragma unroll
-        for (int q = 0; q < kParts; q++) {
-            const int64_t i = first + (q * kThreads + static_cast<int>(threadIdx.x)) * P::C;
-            if (i < t.count) p[q].load(t, i);
-            else
+            for (int q = 0; q < kParts; q++) {
+                P p;
+                if (place.in_run(q)) p.take(r[q]);
+                else p.load(t, place.byte() / static_cast<int64_t>(sizeof(type)) + q * kThreads * P::C);
 #pragma unroll
-                for (int e = 0; e < P::C; e++) p[q].v[e] = 0.0f;
-        }
-#pragma unroll
-        for (int q = 0; q < kParts; q++)
-#pragma unroll
-            for (int e = 0; e < P::C; e++) {
-                const double d = p[q].v[e];
-                sum = fma(d, d, sum);
+                for (int e = 0; e < P::C; e++) {
+                    const double d = p.v[e];
+                    sum = fma(d, d, sum);
+                }
             }
+        });
     });
     sum = block_sum(sum, part);
     if (threadIdx.x == 0) j.partial[blockIdx.x] = sum;
 }
 
+template <int kParts>
 __device__ __forceinline__ void scale_values(const Tensor *table, const Job &j)
 {
     __shared__ double part[kThreads / 64];
@@ -178,38 +240,54 @@ __device__ __forceinline__ void scale_values(const Tensor *table, const Job &j)
     if (blockIdx.x == 0 && threadIdx.x == 0) *j.norm = static_cast<float>(norm);
     const bool clipped = norm > j.max_norm;   // not with a NaN
     const double factor = clipped ? j.max_norm / norm : 1.0;
-    each_chunk<true>(table, j, [&](const Tensor &t, auto type, int64_t first) {
+    each_chunk<kParts, true>(table, j, [&](const Place<kParts> &place, const Raw (&r)[kParts]) {
+        const Tensor &t = table[place.at];
         if (!clipped && t.out == t.data) return;
-        using P = Piece<decltype(type)>;
-        P p[kParts];
+        as_type(t, [&](auto type) {
+            using P = Piece<decltype(type)>;
 #pragma unroll
-        for (int q = 0; q < kParts; q++) {
-            const int64_t i = first + (q * kThreads + static_cast<int>(threadIdx.x)) * P::C;
-            if (i < t.count) p[q].load(t, i);
-        }
+            for (int q = 0; q < kParts; q++) {
+                P p;
+                const int64_t i = place.byte() / static_cast<int64_t>(sizeof(type)) + q * kThreads * P::C;
+                if (place.in_run(q)) p.take(r[q]);
+                else p.load(t, i);
 #pragma unroll
-        for (int q = 0; q < kParts; q++) {
-            const int64_t i = first + (q * kThreads + static_cast<int>(threadIdx.x)) * P::C;
-            if (i >= t.count) continue;
-#pragma unroll
-            for (int e = 0; e < P::C; e++) p[q].v[e] = static_cast<float>(p[q].v[e] * factor);
-            p[q].store(t, i);
-        }
+                for (int e = 0; e < P::C; e++) p.v[e] = static_cast<float>(p.v[e] * factor);
+                if (place.in_run(q)) __builtin_nontemporal_store(p.give(), (AM_GLOBAL Raw *)((AM_GLOBAL char *)t.out + place.byte() + q * kThreads * 16));
+                else p.store(t, i);
+            }
+        });
     });
 }
 
-__global__ __launch_bounds__(kThreads) void square_few_kernel(FewArgs a) { square_sums(a.few.t, a.job); }
-__global__ __launch_bounds__(kThreads) void scale_few_kernel(FewArgs a) { scale_values(a.few.t, a.job); }
-__global__ __launch_bounds__(kThreads) void square_kernel(Job j) { square_sums(j.table, j); }
-__global__ __launch_bounds__(kThreads) void scale_kernel(Job j) { scale_values(j.table, j); }
+template <int kParts>
+__global__ __launch_bounds__(kThreads) void square_few_kernel(FewArgs a)
+{
+    square_sums<kParts>(a.few.t, a.job);
+}
+template <int kParts>
+__global__ __launch_bounds__(kThreads) void scale_few_kernel(FewArgs a)
+{
+    scale_values<kParts>(a.few.t, a.job);
+}
+template <int kParts>
+__global__ __launch_bounds__(kThreads) void square_kernel(Job j)
+{
+    square_sums<kParts>(j.table, j);
+}
+template <int kParts>
+__global__ __launch_bounds__(kThreads) void scale_kernel(Job j)
+{
+    scale_values<kParts>(j.table, j);
+}
 
 __global__ __launch_bounds__(128) void table_kernel(Table some, Tensor *to, int32_t n)
 {
     if (static_cast<int>(threadIdx.x) < n) to[threadIdx.x] = some.t[threadIdx.x];
 }
 
-// the i-th tensor's description, first chunk aside; its chunks
-Tensor describe(const wfst_am_clip_args &a, int64_t i, int64_t &chunks)
+// the i-th tensor's description, first chunk aside
+Tensor describe(const wfst_am_clip_args &a, int64_t i)
 {
     const wfst_matrix &g = a.grads[i], &o = a.outs ? a.outs[i] : g;
     Tensor t{};
@@ -220,9 +298,13 @@ Tensor describe(const wfst_am_clip_args &a, int64_t i, int64_t &chunks)
     t.type = g.type;
     const bool dense = g.rows <= 1 || (g.row_stride == g.cols && o.row_stride == g.cols);
     t.cols = dense ? 0 : static_cast<int32_t>(g.cols);
-    const int64_t each = kChunkBytes / am_type_bytes(g.type);
-    chunks = (t.count + each - 1) / each;
     return t;
+}
+
+int64_t chunks_of(const wfst_matrix &g, int parts)
+{
+    const int64_t each = chunk_bytes(parts) / am_type_bytes(g.type);
+    return (g.rows * g.cols + each - 1) / each;
 }
 
 int64_t table_bytes(int64_t tensors)
@@ -230,11 +312,8 @@ int64_t table_bytes(int64_t tensors)
     return tensors > kInArgs ? (tensors * static_cast<int64_t>(sizeof(Tensor)) + 255) & ~int64_t{255} : 0;
 }
 
-}  // namespace
-
-int64_t am_clip_bytes(const wfst_am_clip_args &a) { return table_bytes(a.count) + kMostBlocks * 8; }
-
-hipError_t am_launch_clip(const wfst_am_clip_args &a, hipStream_t st)
+template <int kParts>
+void launch(const wfst_am_clip_args &a, hipStream_t st)
 {
     Job j{};
     j.partial = reinterpret_cast<double *>(static_cast<char *>(a.workspace) + table_bytes(a.count));
@@ -246,12 +325,11 @@ hipError_t am_launch_clip(const wfst_am_clip_args &a, hipStream_t st)
     Table &some = args.few;
     int32_t n = 0;   // in `some`; tensors without values are left out
     for (int64_t i = 0; i < a.count; i++) {
-        int64_t chunks;
-        Tensor t = describe(a, i, chunks);
+        const int64_t chunks = chunks_of(a.grads[i], kParts);
         if (!chunks) continue;
-        t.first = j.chunks;
+        some.t[n] = describe(a, i);
+        some.t[n++].first = j.chunks;
         j.chunks += chunks;
-        some.t[n++] = t;
         if (!few && n == kInArgs) {
             table_kernel<<<1, 128, 0, st>>>(some, table + j.tensors, n);
             j.tensors += n;
@@ -263,12 +341,24 @@ hipError_t am_launch_clip(const wfst_am_clip_args &a, hipStream_t st)
     j.blocks = static_cast<int32_t>(std::clamp<int64_t>(j.chunks, 1, kMostBlocks));
     args.job = j;
     if (few) {
-        square_few_kernel<<<j.blocks, kThreads, 0, st>>>(args);
-        scale_few_kernel<<<j.blocks, kThreads, 0, st>>>(args);
+        square_few_kernel<kParts><<<j.blocks, kThreads, 0, st>>>(args);
+        scale_few_kernel<kParts><<<j.blocks, kThreads, 0, st>>>(args);
     } else {
-        square_kernel<<<j.blocks, kThreads, 0, st>>>(j);
-        scale_kernel<<<j.blocks, kThreads, 0, st>>>(j);
+        square_kernel<kParts><<<j.blocks, kThreads, 0, st>>>(j);
+        scale_kernel<kParts><<<j.blocks, kThreads, 0, st>>>(j);
     }
+}
+
+}  // namespace
+
+int64_t am_clip_bytes(const wfst_am_clip_args &a) { return table_bytes(a.count) + kMostBlocks * 8; }
+
+hipError_t am_launch_clip(const wfst_am_clip_args &a, hipStream_t st)
+{
+    int64_t chunks = 0;
+    for (int64_t i = 0; i < a.count; i++) chunks += chunks_of(a.grads[i], kManyParts);
+    if (chunks >= kMostBlocks) launch<kManyParts>(a, st);
+    else launch<kFewParts>(a, st);
     return hipGetLastError();
 }
 
