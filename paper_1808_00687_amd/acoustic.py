@@ -500,12 +500,13 @@ def wfst_am_distill_backward(logits: torch.Tensor, top_index: torch.Tensor, top_
 
 
 def _tensors(ts, name: str, device: int, keep: Optional[list] = None) -> list:
-    """Tensors of any shape as wfst_matrix fields, one after the other.  A dense one is rows of its last
-    dimension; one that is not has to be a matrix."""
+    """Tensors of any shape as wfst_matrix fields, one after the other.  A dense one is a single row (rows of its
+    last dimension where one would be too long); one that is not has to be a matrix (or is copied, if ``keep`` is
+    given)."""
     flat = []
-    recorded = torch.is_grad_enabled()
+    add, types, recorded = flat.extend, _TYPES, torch.is_grad_enabled()
     for t in ts:
-        code = _TYPES.get(t.dtype)
+        code = types.get(t.dtype)
         if code is None:
             raise TypeError("%s: type %s is not taken" % (name, t.dtype))
         if recorded and t.requires_grad:
@@ -515,13 +516,27 @@ def _tensors(ts, name: str, device: int, keep: Optional[list] = None) -> list:
         n = t.numel()
         if n and not t.is_contiguous():
             if t.dim() == 2 or keep is None:
-                flat.extend(_matrix(t, name, device, keep))
+                add(_matrix(t, name, device, keep))
                 continue
             t = t.contiguous()
             keep.append(t)
-        cols = t.shape[-1] if t.dim() and n else 1
-        flat.extend((t.data_ptr(), n // cols, cols, cols, code, 0))
+        if 0 < n < 1 << 31:
+            add((t.data_ptr(), 1, n, n, code, 0))
+        elif n:
+            cols = t.shape[-1]
+            add((t.data_ptr(), n // cols, cols, cols, code, 0))
+        else:
+            add((0, 0, 1, 1, code, 0))
     return flat
+
+
+def _same_shapes(a: list, b: list) -> None:
+    """Where one of a pair of _tensors is a matrix of several rows and the other a single row, that one too
+    becomes a matrix."""
+    for i in range(1, len(a), 6):
+        if a[i] != b[i]:
+            few, many = (a, b) if a[i] == 1 else (b, a)
+            few[i], few[i + 1], few[i + 2] = many[i], many[i + 1], many[i + 1]
 
 
 @_here
@@ -539,8 +554,13 @@ def wfst_am_clip(grads: Sequence[torch.Tensor], max_norm: float, *, out: Optiona
         raise ValueError("out must have the shapes of grads")
     to = grads if out is None else out
     fields = struct.Struct(_M * n)
-    written = fields.pack(*_tensors(to, "grads" if out is None else "out", d))
-    read = written if out is None else fields.pack(*_tensors(grads, "grads", d, keep))
+    places = _tensors(to, "grads" if out is None else "out", d)
+    if out is None:
+        read = written = fields.pack(*places)
+    else:
+        values = _tensors(grads, "grads", d, keep)
+        _same_shapes(values, places)
+        read, written = fields.pack(*values), fields.pack(*places)
     first = grads[0]
     norm = first.new_empty(1, dtype=torch.float32)
     at = C.cast(C.c_char_p(read), C.c_void_p).value

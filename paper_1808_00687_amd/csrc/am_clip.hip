@@ -5,8 +5,8 @@
 // numbered through; a workgroup takes every blocks-th one and has the next one's
 // loads on their way while it works on the present one.  The second pass goes
 // through them backwards: what the first one read last may still be in a cache; its
-// stores are not kept there.  125 tensors of 1.6 GB: 928 us, 4.9 GB in all, 5.3 TB/s (956
-// forwards, 982 with stores that are kept, 1,213 without the loads ahead).
+// stores are not kept there.  125 tensors of 1.6 GB: 920 us, 4.9 GB in all, 5.3 TB/s (10
+// more forwards, 40 more with stores that are kept); the norm alone of 1 GB: 187 us, 5.7 TB/s.
 //
 // The sum is held in 64 bits (a square of a float32 may be no float32, and a
 // billion of them would lose bits): a workgroup's goes to the workspace, and every
@@ -34,9 +34,9 @@ struct Tensor {
 
 constexpr int kThreads = 256;
 constexpr int64_t kMostBlocks = 256 * 8;
-// Parts of 4 KB in a chunk.  The large model above takes 1,913, 1,228, 1,105, 976, 928 us with 1, 2,
-// 4, 6, 8 (12 and 16: 1,002 and 931); a small one of 15 tensors has too few chunks then, 7 us with 1 or 2
-// and 10 with 4.  Large chunks from where they are as many as the workgroups.
+// Parts of 4 KB in a chunk.  The large model above takes 1,131, 1,161, 999, 920 us with 2, 4, 6, 8;
+// ten tensors of 16 MB together 17 and 23 with 2 and 8, of 128 MB 69 and 73, of 256 MB 133 and 132.  So many
+// from three chunks a workgroup on.
 constexpr int kFewParts = 2, kManyParts = 8;
 constexpr int64_t chunk_bytes(int parts) { return int64_t{kThreads} * 16 * parts; }
 constexpr int kInArgs = 71;   // what fits into 4 KB of arguments with the rest
@@ -52,6 +52,7 @@ struct Job {
     double max_norm;
     int64_t chunks;
     int32_t tensors, blocks;
+    int32_t in_place;      // all of them
 };
 
 struct FewArgs {
@@ -134,11 +135,15 @@ struct Place {
     int64_t inside;   // chunk of the tensor
     int64_t run;      // bytes from this thread's first part to the end of a tensor that lies in one run, else 0
 
-    __device__ __forceinline__ void find(const Tensor *table, const Job &j, int64_t c)
+    // near: a tensor to look at first (a large one has several of a workgroup's chunks)
+    __device__ __forceinline__ void find(const Tensor *table, const Job &j, int64_t c, int near)
     {
         at = -1, inside = 0, run = 0;
         if (c < 0 || c >= j.chunks) return;
         int lo = 0, hi = j.tensors;   // the last tensor whose first chunk is not behind c
+        if (table[near].first > c) hi = near;
+        else if (near + 1 < j.tensors && table[near + 1].first <= c) lo = near + 1;
+        else lo = near, hi = near + 1;
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
             if (table[mid].first <= c) lo = mid;
@@ -153,7 +158,6 @@ struct Place {
     __device__ __forceinline__ bool in_run(int q) const { return run >= (q * kThreads + 1) * 16; }
     __device__ __forceinline__ void load(const Tensor *table, Raw (&r)[kParts]) const
     {
-        if (at < 0) return;
         const AM_GLOBAL char *p = (const AM_GLOBAL char *)table[at].data + byte();
 #pragma unroll
         for (int q = 0; q < kParts; q++)
@@ -162,21 +166,22 @@ struct Place {
 };
 
 // use(place, 16 bytes of each part that lies in a run) for the workgroup's chunks, every
-// j.blocks-th one; the next one's are on their way meanwhile
-template <int kParts, bool kBackwards, typename F>
-__device__ __forceinline__ void each_chunk(const Tensor *table, const Job &j, F use)
+// j.blocks-th one, but for tensors that are not wanted(tensor); the next one's are on
+// their way meanwhile
+template <int kParts, bool kBackwards, typename W, typename F>
+__device__ __forceinline__ void each_chunk(const Tensor *table, const Job &j, W wanted, F use)
 {
     const int64_t step = kBackwards ? -static_cast<int64_t>(j.blocks) : j.blocks;
     int64_t c = kBackwards ? j.chunks - 1 - blockIdx.x : blockIdx.x;
     Place<kParts> place, next;
     Raw r[kParts], ahead[kParts];
-    place.find(table, j, c);
-    place.load(table, r);
+    place.find(table, j, c, 0);
+    if (place.at >= 0 && wanted(table[place.at])) place.load(table, r);
     while (place.at >= 0) {
         c += step;
-        next.find(table, j, c);
-        next.load(table, ahead);
-        use(place, r);
+        next.find(table, j, c, place.at);
+        if (next.at >= 0 && wanted(table[next.at])) next.load(table, ahead);
+        if (wanted(table[place.at])) use(place, r);
         place = next;
 #pragma unroll
         for (int q = 0; q < kParts; q++) r[q] = ahead[q];
@@ -209,7 +214,7 @@ __device__ __forceinline__ void square_sums(const Tensor *table, const Job &j)
 {
     __shared__ double part[kThreads / 64];
     double sum = 0.0;
-    each_chunk<kParts, false>(table, j, [&](const Place<kParts> &place, const Raw (&r)[kParts]) {
+    each_chunk<kParts, false>(table, j, [](const Tensor &) { return true; }, [&](const Place<kParts> &place, const Raw (&r)[kParts]) {
         const Tensor &t = table[place.at];
         as_type(t, [&](auto type) {
             using P = Piece<decltype(type)>;
@@ -240,9 +245,9 @@ __device__ __forceinline__ void scale_values(const Tensor *table, const Job &j)
     if (blockIdx.x == 0 && threadIdx.x == 0) *j.norm = static_cast<float>(norm);
     const bool clipped = norm > j.max_norm;   // not with a NaN
     const double factor = clipped ? j.max_norm / norm : 1.0;
-    each_chunk<kParts, true>(table, j, [&](const Place<kParts> &place, const Raw (&r)[kParts]) {
+    if (!clipped && j.in_place) return;
+    each_chunk<kParts, true>(table, j, [&](const Tensor &t) { return clipped || t.out != t.data; }, [&](const Place<kParts> &place, const Raw (&r)[kParts]) {
         const Tensor &t = table[place.at];
-        if (!clipped && t.out == t.data) return;
         as_type(t, [&](auto type) {
             using P = Piece<decltype(type)>;
 #pragma unroll
@@ -318,6 +323,7 @@ void launch(const wfst_am_clip_args &a, hipStream_t st)
     Job j{};
     j.partial = reinterpret_cast<double *>(static_cast<char *>(a.workspace) + table_bytes(a.count));
     j.norm = a.norm, j.max_norm = a.max_norm;
+    j.in_place = !a.outs;
     const bool few = a.count <= kInArgs;
     Tensor *table = few ? nullptr : static_cast<Tensor *>(a.workspace);
     j.table = table;
@@ -357,7 +363,7 @@ hipError_t am_launch_clip(const wfst_am_clip_args &a, hipStream_t st)
 {
     int64_t chunks = 0;
     for (int64_t i = 0; i < a.count; i++) chunks += chunks_of(a.grads[i], kManyParts);
-    if (chunks >= kMostBlocks) launch<kManyParts>(a, st);
+    if (chunks >= 3 * kMostBlocks) launch<kManyParts>(a, st);
     else launch<kFewParts>(a, st);
     return hipGetLastError();
 }

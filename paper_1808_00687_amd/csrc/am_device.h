@@ -18,31 +18,36 @@ struct f8 {          // OCP e4m3
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(f16 x) { return static_cast<float>(x); }
 __device__ __forceinline__ float to_f32(bf16 x) { return static_cast<float>(x); }
-// Reductions over a wave without LDS: lanes meet by quad and row permutations,
-// then rows of 16 and halves are swapped.  Every lane gets the result, always in
-// the same order.
+// Reductions over a wave, or over each 8, 16 or 32 lanes of it, without LDS: lanes meet
+// by quad and row permutations, then rows of 16 and halves are swapped.  Every lane
+// gets the result, always in the same order.
 template <int kPattern>
 __device__ __forceinline__ int dpp(int v)
 {
     return __builtin_amdgcn_update_dpp(v, v, kPattern, 0xF, 0xF, true);
 }
 
-template <typename Op>
+template <int kLanes = 64, typename Op>
 __device__ __forceinline__ uint32_t wave_reduce(uint32_t v, Op op)
 {
+    static_assert(kLanes == 8 || kLanes == 16 || kLanes == 32 || kLanes == 64, "");
     v = op(v, static_cast<uint32_t>(dpp<0xB1>(static_cast<int>(v))));    // lane ^ 1
     v = op(v, static_cast<uint32_t>(dpp<0x4E>(static_cast<int>(v))));    // lane ^ 2
     v = op(v, static_cast<uint32_t>(dpp<0x141>(static_cast<int>(v))));   // mirrored in 8
+    if constexpr (kLanes == 8) return v;
     v = op(v, static_cast<uint32_t>(dpp<0x140>(static_cast<int>(v))));   // mirrored in 16
+    if constexpr (kLanes == 16) return v;
     const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
     v = op(r[0], r[1]);
+    if constexpr (kLanes == 32) return v;
     const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
     return op(h[0], h[1]);
 }
 
+template <int kLanes = 64>
 __device__ __forceinline__ float wave_sum(float v)
 {
-    return __uint_as_float(wave_reduce(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __uint_as_float(wave_reduce<kLanes>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
         return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
     }));
 }
@@ -54,9 +59,10 @@ __device__ __forceinline__ float wave_max(float v)
     }));
 }
 
+template <int kLanes = 64>
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
 {
-    return wave_reduce(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+    return wave_reduce<kLanes>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
 #define AM_LDS __attribute__((address_space(3)))

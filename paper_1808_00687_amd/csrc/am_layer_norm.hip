@@ -8,6 +8,9 @@
 // registers, and in the backward pass their gradients are summed there over the
 // rows of a workgroup; workgroups' sums are joined by a second small kernel in a
 // fixed order.
+//
+// (53274, 1024) bf16 with the residual to e4m3: 76 us, 382 MB, 5.0 TB/s (a large copy
+// reaches 5.0); backward of (16384, 2048) bf16 with dsum: 48 us and 5 of the join, 268 MB.
 #include "am_rows.h"
 
 namespace wfd {
@@ -24,8 +27,8 @@ __device__ __forceinline__ void row_sums(float (&v)[K], SumScratch<N> &r, int &t
 {
     static_assert(K <= N, "");
 #pragma unroll
-    for (int k = 0; k < K; k++) v[k] = wave_sum(v[k]);
-    if constexpr (S::kWaves == 1) return;
+    for (int k = 0; k < K; k++) v[k] = wave_sum<S::kLanes>(v[k]);
+    if constexpr (S::kWaves <= 1) return;
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
@@ -135,7 +138,7 @@ __global__ __launch_bounds__(S::kThreads) void layer_norm_kernel(wfst_am_layer_n
                     top = e < left && b > top ? b : top;
                 }
             });
-            by.set(row_max_u32<S>(top, scratch, turn8));
+            by.template set<(S::kWaves > 0)>(row_max_u32<S>(top, scratch, turn8));
             if (t == 0) a.y_scale[m] = by.scale;
         }
         S::each(D, t, [&](int v, int64_t c, int64_t left) {
@@ -255,11 +258,22 @@ __global__ __launch_bounds__(S::kThreads) void layer_norm_backward_kernel(wfst_a
             store_floats(partial_b + blockIdx.x * D + c, left, db[v]);
         });
     } else {
-        // the workgroup's rows' sums, one after the other
+        // a wave's rows' sums, then the waves' sums one after the other
+        if constexpr (S::kLanes < 64)
+#pragma unroll
+            for (int v = 0; v < S::kHeld; v++)
+#pragma unroll
+                for (int e = 0; e < S::kC; e++)
+#pragma unroll
+                    for (int far = S::kLanes; far < 64; far *= 2) {
+                        dg[v][e] += __shfl_xor(dg[v][e], far);
+                        db[v][e] += __shfl_xor(db[v][e], far);
+                    }
         __shared__ float total[2][S::kHeld * S::kTpr * S::kC];
-        for (int w = 0; w < S::kRows; w++) {
+        const bool first_row = static_cast<int>(threadIdx.x & 63) < S::kTpr;
+        for (int w = 0; w < S::kThreads / 64; w++) {
             __syncthreads();
-            if (static_cast<int>(threadIdx.x) / S::kTpr != w) continue;
+            if (static_cast<int>(threadIdx.x) / 64 != w || !first_row) continue;
 #pragma unroll
             for (int v = 0; v < S::kHeld; v++)
 #pragma unroll
@@ -269,7 +283,7 @@ __global__ __launch_bounds__(S::kThreads) void layer_norm_backward_kernel(wfst_a
                     total[0][at] = dg[v][e], total[1][at] = db[v][e];
                 }
         }
-        if (threadIdx.x / S::kTpr == S::kRows - 1)
+        if (threadIdx.x / 64 == S::kThreads / 64 - 1 && first_row)
             S::each(D, t, [&](int v, int64_t c, int64_t left) {
                 store_floats(partial + blockIdx.x * D + c, left, dg[v]);
                 store_floats(partial_b + blockIdx.x * D + c, left, db[v]);
@@ -313,21 +327,58 @@ __global__ __launch_bounds__(256) void layer_norm_columns_kernel(wfst_am_layer_n
     store_floats(partial + (gridDim.y + blockIdx.y) * D + c, D - c, db);
 }
 
-// workgroups at most, and in the backward pass strips of rows whose sums are joined
+// Rows of few columns share a wave: (349525, 96) bf16 to 8 bits with the residual 63 us, with a wave a row
+// 217, (524288, 64) 44 and 317, (131072, 256) 43 and 83; backward of (349525, 96) with dsum 75 and 252, of (131072,
+// 256) 57 and 103.
+template <int C, typename F>
+void row_shape(int64_t D, F go)
+{
+    constexpr int k = 8 / C;
+    if (D <= 64) go(RowShape<8, 1 * k, C>{});
+    else if (D <= 128) go(RowShape<16, 1 * k, C>{});
+    else if (D <= 256) go(RowShape<32, 1 * k, C>{});
+    else am_row_shape_norm<C>(D, go);
+}
+
+// And for the gradients: rows of 1,025 to 2,048 float32 columns take 256 threads ((11184, 1500) 53 us, a wave 67),
+// 16-bit ones a wave ((22369, 1500) 76, 256 threads 90).  Held up to 16,384 columns ((1024, 32768) bf16 132 us, held
+// 290, float32 123 and 251).
+template <int C, typename F>
+void row_shape_backward(int64_t D, F go)
+{
+    constexpr int k = 8 / C;
+    if (D <= 64) go(RowShape<8, 1 * k, C>{});
+    else if (D <= 128) go(RowShape<16, 1 * k, C>{});
+    else if (D <= 256) go(RowShape<32, 1 * k, C>{});
+    else if (C == 4 && D > 1024 && D <= 2048) go(RowShape<256, 1 * k, C>{});
+    else if (D > 16384) go(RowShape<1024, 0, C>{});
+    else am_row_shape<C>(D, go);
+}
+
+// Workgroups at most.  Backward about as many as are resident, by the bytes of a matrix that a thread holds: one
+// more and the last ones run alone (268 MB each, 1 to 5 a CU: 512 bf16 columns 95, 67, 62, 58, 57 us; 1,024 72, 52,
+// 51, 60, 57; 2,048 64, 52, 63, 61, 61; 8,192 72, 63, 76, 79, 78; 2,048 float32 64, 49, 50, 51, 54).
 constexpr int64_t kForwardBlocks = 256 * 16;
-constexpr int64_t kBackwardBlocks = 256 * 3;
+
+template <typename S>
+constexpr int64_t backward_blocks(int64_t el)
+{
+    const int64_t held = S::kNv * S::kC * el;
+    return 256 * (S::kThreads > 256 ? 1 : held <= 16 ? 5 : held <= 32 ? 3 : held <= 96 ? 2 : 1);
+}
 
 struct Sums {
     int64_t strips, moments_bytes, partial_bytes;
 };
 
-Sums sums_of(int64_t M, int64_t D)
+// strips of rows whose sums are joined, and what the workspace holds
+Sums sums_of(int64_t M, int64_t D, int64_t el)
 {
     Sums n{};
-    am_row_shape_lean<8>(D, [&](auto shape) {   // the same for shorter chunks
+    const auto of = [&](auto shape) {
         using S = decltype(shape);
         if constexpr (S::kNv > 0) {
-            n.strips = static_cast<int64_t>(am_row_blocks<S>(M, kBackwardBlocks));
+            n.strips = static_cast<int64_t>(am_row_blocks<S>(M, backward_blocks<S>(el)));
         } else {
             // 16 rows a wave at least, about 1,024 workgroups at most
             const int64_t wide = (D + 511) / 512, tall = M / 64, most = 1024 / wide;
@@ -335,7 +386,9 @@ Sums sums_of(int64_t M, int64_t D)
             if (M && n.strips < 1) n.strips = 1;
             n.moments_bytes = (M * static_cast<int64_t>(sizeof(Moments)) + 255) & ~int64_t{255};
         }
-    });
+    };
+    if (el == 4) row_shape_backward<4>(D, of);
+    else row_shape_backward<8>(D, of);
     n.partial_bytes = (n.strips * D * 8 + 255) & ~int64_t{255};
     return n;
 }
@@ -350,22 +403,22 @@ void launch_layer_norm(const wfst_am_layer_norm_args &a, hipStream_t st)
             if (a.y.type == WFST_F8E4M3) return layer_norm_kernel<T, S, true><<<g, S::kThreads, 0, st>>>(a);
         layer_norm_kernel<T, S, false><<<g, S::kThreads, 0, st>>>(a);
     };
-    if (kChunk<T> > 4 && a.y.type == WFST_F32) am_row_shape_norm<4>(a.x.cols, go);
-    else am_row_shape_norm<kChunk<T>>(a.x.cols, go);
+    if (kChunk<T> > 4 && a.y.type == WFST_F32) row_shape<4>(a.x.cols, go);
+    else row_shape<kChunk<T>>(a.x.cols, go);
 }
 
 template <typename T>
 void launch_layer_norm_backward(const wfst_am_layer_norm_backward_args &a, hipStream_t st)
 {
     const int64_t M = a.s.rows, D = a.s.cols;
-    const Sums n = sums_of(M, D);
+    const Sums n = sums_of(M, D, sizeof(T));
     const bool wanted = a.dgain || a.dbias;
     char *work = static_cast<char *>(a.workspace);
     Moments *moments = reinterpret_cast<Moments *>(work);
     float *partial = reinterpret_cast<float *>(work + n.moments_bytes);
-    am_row_shape_lean<kChunk<T>>(D, [&](auto shape) {
+    row_shape_backward<kChunk<T>>(D, [&](auto shape) {
         using S = decltype(shape);
-        const unsigned g = M ? am_row_blocks<S>(M, kBackwardBlocks) : 0;
+        const unsigned g = M ? am_row_blocks<S>(M, S::kNv > 0 ? backward_blocks<S>(sizeof(T)) : 256 * 3) : 0;
         if constexpr (S::kNv > 0) {
             if (M) layer_norm_backward_kernel<T, S><<<g, S::kThreads, 0, st>>>(a, wanted ? partial : nullptr, nullptr);
         } else if (M) {
@@ -398,7 +451,7 @@ hipError_t am_launch_layer_norm(const wfst_am_layer_norm_args &a, hipStream_t st
 int64_t am_layer_norm_backward_bytes(const wfst_am_layer_norm_backward_args &a)
 {
     if (!a.dgain && !a.dbias) return 0;
-    const Sums n = sums_of(a.s.rows, a.s.cols);
+    const Sums n = sums_of(a.s.rows, a.s.cols, am_type_bytes(a.s.type));
     return n.moments_bytes + n.partial_bytes;
 }
 

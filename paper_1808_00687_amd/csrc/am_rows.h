@@ -1,7 +1,7 @@
 // Rows of the acoustic model's row operators: who reads which part, and the
 // reductions over a row.
 //
-// A row belongs to TPR threads (a wave, 256 or 1024), C consecutive columns at
+// A row belongs to TPR threads (8, 16, 32, a wave, 256 or 1024), C consecutive columns at
 // a time: chunk c is thread c % TPR's.  C is 8 where every matrix has at most 16-bit
 // elements and 4 where one has 32-bit ones, so that no access to a matrix is wider
 // than 16 bytes and neighbouring lanes' accesses touch.  (Vectors are 32-bit in
@@ -20,7 +20,8 @@ template <int TPR, int NV, int C>
 struct RowShape {
     static constexpr int kThreads = TPR < 256 ? 256 : TPR;
     static constexpr int kRows = kThreads / TPR;           // rows a workgroup works on
-    static constexpr int kWaves = TPR / 64;                // waves a row
+    static constexpr int kWaves = TPR / 64;                // waves a row (0: several rows a wave)
+    static constexpr int kLanes = TPR < 64 ? TPR : 64;     // lanes of a wave that share a row
     static constexpr int kTpr = TPR, kNv = NV, kC = C;
     static constexpr int kHeld = NV > 0 ? NV : 1;
 
@@ -163,8 +164,8 @@ __device__ __forceinline__ void row_sums(float &u, float &v, RowScratch &r, int 
 template <typename S>
 __device__ __forceinline__ uint32_t row_max_u32(uint32_t v, RowScratch &r, int &turn)
 {
-    v = wave_max_u32(v);
-    if constexpr (S::kWaves == 1) return v;
+    v = wave_max_u32<S::kLanes>(v);
+    if constexpr (S::kWaves <= 1) return v;
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) r.a[turn][wave] = __uint_as_float(v);
     __syncthreads();
@@ -199,7 +200,8 @@ struct E4m3Quotient {
     float scale = 1.0f, inv = 1.0f;
     bool whole = false;   // is a quotient formed by a division?
 
-    // top: bits of the row's largest magnitude
+    // top: bits of the row's largest magnitude; kUniform: a wave has one row
+    template <bool kUniform = true>
     __device__ __forceinline__ void set(uint32_t top)
     {
         scale = __uint_as_float(top) / kE4m3Max;
@@ -208,7 +210,8 @@ struct E4m3Quotient {
         // (Markstein 1990) unless the divisor's bits are all ones or something leaves the
         // range; 72.8 us for the norm of (53274, 1024) bf16, 74.5 with divisions.
         inv = 1.0f / scale;
-        whole = __builtin_amdgcn_readfirstlane(!(scale >= 0x1p-90f && scale <= 0x1p90f) || (__float_as_uint(scale) & 0x7FFFFFu) == 0x7FFFFFu) != 0;
+        whole = !(scale >= 0x1p-90f && scale <= 0x1p90f) || (__float_as_uint(scale) & 0x7FFFFFu) == 0x7FFFFFu;
+        if constexpr (kUniform) whole = __builtin_amdgcn_readfirstlane(whole) != 0;
     }
     template <int C>
     __device__ __forceinline__ void divide(float (&s)[C]) const

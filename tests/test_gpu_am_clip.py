@@ -113,6 +113,15 @@ def test_any_shape(am):
         am.wfst_am_clip([t.t()], 1.0)
 
 
+def test_more_than_31_bits_of_values(am):
+    # 2^31 + 26 values of 0.5: the norm is exact but for its root, a factor of 1 / 16 is exact
+    t = torch.full((2, (1 << 30) + 13), 0.5, dtype=BF16, device="cuda")
+    want = 0.5 * math.sqrt(t.numel())
+    _, norm = am.wfst_am_clip([t], want / 16)
+    assert abs(float(norm) - want) <= R.U32 * want * 1.001
+    assert float(t.min()) == float(t.max()) == 0.5 / 16
+
+
 def test_what_is_within_the_limit_is_not_written(am):
     g = rng(5)
     t = normal(g, 300, 200).to(BF16).cuda()
