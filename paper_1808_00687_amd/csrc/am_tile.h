@@ -303,13 +303,16 @@ __device__ __forceinline__ void am_set(f32x4 &v, uint32_t bits)
     v[e] = __uint_as_float(bits);
 }
 
-// Tile (ti, tj) of workgroup `block` of `count`.  Workgroups go to the 8
-// chiplets in turn; each chiplet gets a run of consecutive tiles, and runs go
-// through blocks of 8 rows of tiles, so a chiplet's L2 sees few rows and columns.
-__device__ __forceinline__ void am_tile_of(uint32_t block, uint32_t rows, uint32_t cols, uint32_t &ti, uint32_t &tj)
+// Tile (ti, tj) and part of k of workgroup `block`, of parts * rows * cols in a row.
+// Workgroups go to the 8 chiplets in turn; each chiplet gets a run of consecutive
+// tiles of one part, and runs go through blocks of 8 rows of tiles, so a chiplet's L2
+// sees few rows and columns.
+__device__ __forceinline__ void am_tile_of(uint32_t block, uint32_t rows, uint32_t cols, uint32_t parts, uint32_t &ti, uint32_t &tj, uint32_t &part)
 {
-    const uint32_t count = rows * cols, each = count / 8, more = count % 8, xcd = block % 8;
-    const uint32_t t = xcd * each + (xcd < more ? xcd : more) + block / 8;
+    const uint32_t tiles = rows * cols, count = tiles * parts, each = count / 8, more = count % 8, xcd = block % 8;
+    uint32_t t = xcd * each + (xcd < more ? xcd : more) + block / 8;
+    part = 0;
+    if (parts > 1) part = t / tiles, t %= tiles;
     const uint32_t group = t / (8 * cols), at = t % (8 * cols);
     const uint32_t height = rows - group * 8 < 8 ? rows - group * 8 : 8;
     ti = group * 8 + at % height;
@@ -552,14 +555,20 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
     };
 
     const int lane_ = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    uint32_t ti, tj;
-    am_tile_of(p.first + blockIdx.x, (p.a.extent + BM - 1) / BM, (p.b.extent + kResults - 1) / kResults, ti, tj);
+    uint32_t ti, tj, k_part;
+    const uint32_t rows = (p.a.extent + BM - 1) / BM, cols = (p.b.extent + kResults - 1) / kResults;
+    if (gridDim.x == rows * cols) {   // all in one launch
+        am_tile_of(blockIdx.y * gridDim.x + blockIdx.x, rows, cols, p.splits, ti, tj, k_part);
+    } else {
+        am_tile_of(p.first + blockIdx.x, rows, cols, 1, ti, tj, k_part);
+        k_part = blockIdx.y;
+    }
     const int64_t i0 = static_cast<int64_t>(ti) * BM, j0 = static_cast<int64_t>(tj) * kResults;
     const int wi = wave / WN * (BM / S::WM), wj = wave % WN * (BN / WN);
 
     const int32_t stages = (p.inner + kK - 1) / kK;
-    const int32_t s_first = static_cast<int32_t>(static_cast<int64_t>(stages) * blockIdx.y / p.splits);
-    const int32_t s_last = static_cast<int32_t>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / p.splits);
+    const int32_t s_first = static_cast<int32_t>(static_cast<int64_t>(stages) * k_part / p.splits);
+    const int32_t s_last = static_cast<int32_t>(static_cast<int64_t>(stages) * (k_part + 1) / p.splits);
 
     SideA sa;
     SideB sb;
@@ -788,7 +797,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
     if (j >= p.b.extent) return;
     float b_scale[kRun], bias[kRun];
     if (p.splits == 1) am_columns(p, j, b_scale, bias);
-    const wfst_matrix partial{p.partial + static_cast<int64_t>(blockIdx.y) * p.a.extent * p.b.extent, p.a.extent, p.b.extent, p.b.extent, WFST_F32, 0};
+    const wfst_matrix partial{p.partial + static_cast<int64_t>(k_part) * p.a.extent * p.b.extent, p.a.extent, p.b.extent, p.b.extent, WFST_F32, 0};
     am_each<TI>([&](auto f) {
         const int64_t i = i0 + wi + f * 16 + (lane_ & 15);
         if (i >= p.a.extent) return;
