@@ -662,7 +662,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
         }(std::make_integer_sequence<int, kPeriod>{});
     };
 
-#pragma clang loop unroll(disable)
+    // Unrolled: as a loop the compiler kept two copies of some sums and had to fetch
+    // offsets from memory inside the products' loop, each time behind the stage on its way.
+#pragma clang loop unroll(full)
     for (int part = kTwice ? 0 : 1; part < 2; part++) {
     const AmOperand a{part ? p.a.data : p.a_low, p.a.ld, p.a.extent};
     s = s_first;
