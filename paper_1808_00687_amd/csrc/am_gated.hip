@@ -14,7 +14,7 @@ namespace {
 // dz = [dgate dvalue] in the operands' type, or in two values of it (dz_low is not
 // NULL), and sums of the unrounded dz over a strip of rows.  8 columns of either a
 // thread; `across` threads (a power of two) side by side, 256 / across rows at a
-// time.  sums: [strips][2 N].  Bound by memory.
+// time.  sums: [strips][2 N].  Bound by memory: (16384, 2048) bf16 to two values 86 us, 470 MB, 5.5 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void gated_slope_kernel(wfst_am_gated_backward_args a, T *dz, T *dz_low, float *sums, int across)
 {
@@ -68,7 +68,9 @@ wfst_am_linear_backward_args as_layer(const wfst_am_gated_backward_args &a)
     return b;
 }
 
-BackwardPlan plan_of(const wfst_am_gated_backward_args &a) { return am_backward_plan(as_layer(a), true, a.round_dz ? 1 : 2, a.dy.cols); }
+// A row a thread where there are few: its loads, activation and stores are a chain of about 2 us ((833, 1280) with dbias
+// and a small dx 26 us, with four 30; 50 rows of 512 18 and 23).
+BackwardPlan plan_of(const wfst_am_gated_backward_args &a) { return am_backward_plan(as_layer(a), true, a.round_dz ? 1 : 2, a.dy.cols, 1); }
 
 template <typename T>
 void launch_backward(const wfst_am_gated_backward_args &a, hipStream_t st)

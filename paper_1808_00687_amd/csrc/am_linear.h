@@ -39,14 +39,15 @@ struct BackwardPlan {
     int64_t strips;   // of rows, in that pass
 };
 
-// in_workspace: is dz written there (it is dy else)?  parts: of dz.  across_cols: columns that the pass over dy has side by side
-inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a, bool in_workspace, int32_t parts, int64_t across_cols)
+// in_workspace: is dz written there (it is dy else)?  parts: of dz.  across_cols: columns that the pass over dy has side by
+// side; rows: of a thread in that pass, at least
+inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a, bool in_workspace, int32_t parts, int64_t across_cols, int64_t rows)
 {
     const int64_t M = a.dy.rows, N = a.dy.cols;
     BackwardPlan p{0, parts, 0, {64, 1}, {64, 1}, 1, 1};
     while (p.across < 64 && p.across * 8 < across_cols) p.across *= 2;
-    // 4 rows a thread at least, about 1,024 workgroups at most
-    const int64_t wide = (across_cols + p.across * 8 - 1) / (p.across * 8), tall = M * p.across / 1024, most = 1024 / wide;
+    // about 1,024 workgroups at most
+    const int64_t wide = (across_cols + p.across * 8 - 1) / (p.across * 8), tall = M * p.across / (256 * rows), most = 1024 / wide;
     p.strips = tall < most ? tall : most;
     if (p.strips < 1) p.strips = 1;
     if (a.dbias && p.strips > 1) p.partial_bytes = (p.strips * N * 4 + 255) & ~int64_t{255};
@@ -73,7 +74,7 @@ inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a, bool
 
 inline BackwardPlan am_backward_plan(const wfst_am_linear_backward_args &a)
 {
-    return am_backward_plan(a, a.activation != WFST_ACT_NONE, am_dz_in_parts(a) ? 2 : 1, a.dy.cols);
+    return am_backward_plan(a, a.activation != WFST_ACT_NONE, am_dz_in_parts(a) ? 2 : 1, a.dy.cols, 4);
 }
 
 // act'(z), and act(z) where it is asked for
