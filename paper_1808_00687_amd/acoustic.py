@@ -24,7 +24,9 @@ no_grad and in inference mode they are not), and the gradients are the
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import struct
+from itertools import chain, repeat
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -499,68 +501,71 @@ def wfst_am_distill_backward(logits: torch.Tensor, top_index: torch.Tensor, top_
     return dlogits
 
 
+_numel, _dense, _place, _gpu = (torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.data_ptr,
+                                torch.Tensor.get_device)
+_dtype, _grad = operator.attrgetter("dtype"), operator.attrgetter("requires_grad")
+
+
 def _tensors(ts, name: str, device: int, keep: Optional[list] = None) -> list:
     """Tensors of any shape as wfst_matrix fields, one after the other.  A dense one is a single row (rows of its
     last dimension where one would be too long); one that is not has to be a matrix (or is copied, if ``keep`` is
     given)."""
+    codes = list(map(_TYPES.get, map(_dtype, ts)))   # (whole lists at a time: a model has hundreds)
+    if None in codes:
+        raise TypeError("%s: type %s is not taken" % (name, ts[codes.index(None)].dtype))
+    if torch.is_grad_enabled() and any(map(_grad, ts)):
+        raise ValueError(_NO_GRAPH % name)
+    if set(map(_gpu, ts)) != {device}:
+        raise ValueError("%s must be on one GPU" % name)
+    counts = list(map(_numel, ts))
+    if all(map(_dense, ts)) and min(counts) > 0 and max(counts) < 1 << 31:
+        return list(chain.from_iterable(zip(map(_place, ts), repeat(1), counts, counts, codes, repeat(0))))
     flat = []
-    add, types, recorded = flat.extend, _TYPES, torch.is_grad_enabled()
-    for t in ts:
-        code = types.get(t.dtype)
-        if code is None:
-            raise TypeError("%s: type %s is not taken" % (name, t.dtype))
-        if recorded and t.requires_grad:
-            raise ValueError(_NO_GRAPH % name)
-        if t.get_device() != device:
-            raise ValueError("%s must be on one GPU" % name)
-        n = t.numel()
+    for t, code, n in zip(ts, codes, counts):
         if n and not t.is_contiguous():
             if t.dim() == 2 or keep is None:
-                add(_matrix(t, name, device, keep))
+                flat.extend(_matrix(t, name, device, keep))
                 continue
             t = t.contiguous()
             keep.append(t)
-        if 0 < n < 1 << 31:
-            add((t.data_ptr(), 1, n, n, code, 0))
-        elif n:
-            cols = t.shape[-1]
-            add((t.data_ptr(), n // cols, cols, cols, code, 0))
-        else:
-            add((0, 0, 1, 1, code, 0))
+        cols = n if n < 1 << 31 else t.shape[-1]
+        flat.extend((t.data_ptr(), n // cols, cols, cols, code, 0) if n else (0, 0, 1, 1, code, 0))
     return flat
 
 
-def _same_shapes(a: list, b: list) -> None:
-    """Where one of a pair of _tensors is a matrix of several rows and the other a single row, that one too
-    becomes a matrix."""
+def _pair(a: list, b: list) -> None:
+    """The fields of pairs of tensors, where some differ in rows or columns: a single row beside a matrix of as many
+    values becomes one, too."""
     for i in range(1, len(a), 6):
         if a[i] != b[i]:
             few, many = (a, b) if a[i] == 1 else (b, a)
-            few[i], few[i + 1], few[i + 2] = many[i], many[i + 1], many[i + 1]
+            if few[i] == 1 and few[i + 1] == many[i] * many[i + 1]:
+                few[i], few[i + 1], few[i + 2] = many[i], many[i + 1], many[i + 1]
 
 
 @_here
 def wfst_am_clip(grads: Sequence[torch.Tensor], max_norm: float, *, out: Optional[Sequence[torch.Tensor]] = None
                  ) -> Tuple[Sequence[torch.Tensor], torch.Tensor]:
     """(out, norm): the tensors times what keeps the norm of all of them within
-    ``max_norm`` (infinity: as they are), in ``out`` (tensors of the same types
-    and shapes) or else in place; ``norm`` [1] is that before the clipping
-    (wfst_am_clip).  Tensors that are not dense have to be matrices; a
-    parameter's gradient may be of any shape."""
+    ``max_norm`` (infinity: as they are), in ``out`` (a tensor of the same type
+    and number of values for each, in the same order) or else in place; ``norm``
+    [1] is that before the clipping (wfst_am_clip).  Tensors that are not dense
+    have to be matrices; a parameter's gradient may be of any shape."""
     if not isinstance(grads, (list, tuple)) or not grads:
         raise TypeError("grads must be a list of one tensor or more")
     d, n, keep = _device(grads[0], "grads"), len(grads), []
-    if out is not None and (len(out) != n or any(o.shape != g.shape for o, g in zip(out, grads))):
-        raise ValueError("out must have the shapes of grads")
-    to = grads if out is None else out
-    fields = struct.Struct(_M * n)
-    places = _tensors(to, "grads" if out is None else "out", d)
+    layout = _M * n
     if out is None:
-        read = written = fields.pack(*places)
+        to = grads
+        read = written = struct.pack(layout, *_tensors(grads, "grads", d))
     else:
-        values = _tensors(grads, "grads", d, keep)
-        _same_shapes(values, places)
-        read, written = fields.pack(*values), fields.pack(*places)
+        to = out
+        if not isinstance(out, (list, tuple)) or len(out) != n:
+            raise ValueError("out must be a list of as many tensors as grads")
+        values, places = _tensors(grads, "grads", d, keep), _tensors(out, "out", d)
+        if values[1::6] != places[1::6] or values[2::6] != places[2::6]:
+            _pair(values, places)
+        read, written = struct.pack(layout, *values), struct.pack(layout, *places)
     first = grads[0]
     norm = first.new_empty(1, dtype=torch.float32)
     at = C.cast(C.c_char_p(read), C.c_void_p).value

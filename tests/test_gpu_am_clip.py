@@ -111,6 +111,34 @@ def test_any_shape(am):
     compare([out], norm, [t.t()], 1.0, "transposed")
     with pytest.raises(ValueError, match="adjacent"):
         am.wfst_am_clip([t.t()], 1.0)
+    # dense outputs of as many values, and matrices beside dense tensors
+    flat = torch.empty(1200).cuda()
+    _, norm = am.wfst_am_clip([t], 1.0, out=[flat])
+    compare([flat.view(40, 30)], norm, [t], 1.0, "flat")
+    wide = torch.empty(40, 35).cuda()
+    _, norm = am.wfst_am_clip([t], 1.0, out=[wide[:, :30]])
+    compare([wide[:, :30]], norm, [t], 1.0, "into columns")
+    wide[:, :30] = t
+    _, norm = am.wfst_am_clip([wide[:, :30], t], 1.0, out=[flat.view(40, 30), torch.empty_like(t)])
+    compare([flat.view(40, 30)], norm / math.sqrt(2), [t], 1.0 / math.sqrt(2), "from columns")
+    from paper_1808_00687_amd import wfstdec
+    column = torch.empty(1200, 2).cuda()[:, :1]
+    _, norm = am.wfst_am_clip([t], 1.0, out=[column])
+    compare([column.reshape(40, 30)], norm, [t], 1.0, "into one column")
+    for out in ([torch.empty(30, 39).cuda()], [flat[:1199]], [torch.empty(1201, 2).cuda()[:, :1]]):
+        with pytest.raises(wfstdec.WfstError, match="shape"):
+            am.wfst_am_clip([t], 1.0, out=out)
+    for out in ([flat, flat], flat, []):
+        with pytest.raises(ValueError, match="as many"):
+            am.wfst_am_clip([t], 1.0, out=out)
+    with pytest.raises(wfstdec.WfstError, match="type"):
+        am.wfst_am_clip([t], 1.0, out=[t.bfloat16()])
+    with pytest.raises(ValueError, match="requires a gradient"):
+        am.wfst_am_clip([t, torch.zeros(3, requires_grad=True, device="cuda")], 1.0)
+    with pytest.raises(ValueError, match="one GPU"):
+        am.wfst_am_clip([t, torch.zeros(3)], 1.0)
+    with pytest.raises(TypeError, match="int32"):
+        am.wfst_am_clip([t, torch.zeros(3, dtype=torch.int32).cuda()], 1.0)
 
 
 def test_more_than_31_bits_of_values(am):
