@@ -491,9 +491,10 @@ int wfst_set_debug_opts(const wfst_debug_opts *opts);
  * ---------------------------------------------------------------------------
  * Acoustic-model operators: what makes the log-likelihood rows that the
  * search reads.  The layers of a feed-forward acoustic model (matrix product
- * with bias, activation and residual; root-mean-square norm with the
- * residual's addition and an output in 8 bits), its training from a teacher's
- * top logits, and the conversion of its logits to rows for wfst_decode.
+ * with bias, activation and residual; gated layer; root-mean-square and layer
+ * norm with the residual's addition and an output in 8 bits), its training
+ * from a teacher's top logits with the clipping of its gradients, and the
+ * conversion of its logits to rows for wfst_decode.
  *
  * Unlike the decode calls these only enqueue: a call checks its arguments,
  * launches its kernels on hip_stream (of the current HIP device) and returns.
@@ -851,6 +852,7 @@ int wfst_am_distill_backward(const wfst_am_distill_args *args, void *hip_stream)
  * clipped a grad in place is not written.  With a NaN among the values the norm
  * is one and nothing is clipped; an infinity makes the norm infinite and, unless
  * max_norm is, the factor 0: infinities become NaN, the others 0.
+ * The check of the places takes host memory, about 100 bytes a tensor.
  * Errors: WFST_EINVAL (also a workspace that is too small), WFST_ENOMEM,
  * WFST_EDEVICE.
  */

@@ -1,6 +1,7 @@
 """Binding of the acoustic-model operators of libwfstdec.so (the wfst_am_*
 calls in include/wfstdec.h): the layers of a network that scores frames, its
-loss against a teacher's top logits, and its logits as rows for wfst_decode.
+loss against a teacher's top logits, the clipping of its gradients, and its
+logits as rows for wfst_decode.
 
 The functions keep the C names and only marshal arguments; every step runs in
 the library's HIP kernels.  Operands are torch tensors on one GPU.  A matrix

@@ -7,7 +7,7 @@ namespace wfd {
 template <>
 void am_product_gated<bf16>(const AmProduct &p, int32_t tile, hipStream_t st)
 {
-    if (tile == 0) am_gated_thin<bf16>(p, st);
+    if (tile == 0) am_thin<bf16, true>(p, st);
     else am_gated_product<bf16>(p, tile, st);
 }
 

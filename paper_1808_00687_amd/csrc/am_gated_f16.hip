@@ -7,7 +7,7 @@ namespace wfd {
 template <>
 void am_product_gated<f16>(const AmProduct &p, int32_t tile, hipStream_t st)
 {
-    if (tile == 0) am_gated_thin<f16>(p, st);
+    if (tile == 0) am_thin<f16, true>(p, st);
     else am_gated_product<f16>(p, tile, st);
 }
 

@@ -7,7 +7,7 @@ namespace wfd {
 template <>
 void am_product_gated<f8>(const AmProduct &p, int32_t tile, hipStream_t st)
 {
-    if (tile == 0) am_gated_thin<f8>(p, st);
+    if (tile == 0) am_thin<f8, true>(p, st);
     else am_gated_product<f8>(p, tile, st);
 }
 

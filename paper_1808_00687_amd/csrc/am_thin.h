@@ -36,8 +36,8 @@ __device__ __forceinline__ i32x4 am_thin_load(const AmOperand &o, int64_t row, i
     return i32x4{static_cast<int>(w[0]), static_cast<int>(w[1]), static_cast<int>(w[2]), static_cast<int>(w[3])};
 }
 
-// kGated: the first half of the TJ fragments are gates, the second half the same
-// results' values, p.b.extent rows behind them.
+// kGated: of a fragment's 16 rows of b the first 8 are gates, the others the same results'
+// values, p.b.extent rows behind them.
 template <typename E, int TI, int TJ, bool kGated>
 __global__ __launch_bounds__(kThinWaves * 64, 2) void am_thin_kernel(AmProduct p)
 {
@@ -54,9 +54,8 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void am_thin_kernel(AmProduct p
     int64_t row_a[TI], row_b[TJ];   // past the end: the last row again, whose results are not stored
     am_each<TI>([&](auto f) { row_a[f] = i0 + f * 16 + s < p.a.extent ? i0 + f * 16 + s : p.a.extent - 1; });
     am_each<TJ>([&](auto f) {
-        constexpr bool kValue = kGated && f >= TJ / 2;
-        const int64_t j = j0 + (kValue ? f - TJ / 2 : f) * 16 + s;
-        row_b[f] = (j < p.b.extent ? j : p.b.extent - 1) + (kValue ? p.b.extent : 0);
+        const int64_t j = kGated ? j0 + f * 8 + (s & 7) : j0 + f * 16 + s;
+        row_b[f] = (j < p.b.extent ? j : p.b.extent - 1) + (kGated && s >= 8 ? p.b.extent : 0);
     });
     const int32_t steps = (p.inner + kStep - 1) / kStep;
     const int32_t s_first = static_cast<int32_t>(static_cast<int64_t>(steps) * wave / kThinWaves);
@@ -111,7 +110,10 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void am_thin_kernel(AmProduct p
         float v[2 * kOwn], b_scale[2 * kOwn], bias[2 * kOwn];
         am_columns_gated(p, j, b_scale, bias);
 #pragma unroll
-        for (int e = 0; e < kOwn; e++) v[e] = sum(rj + e), v[kOwn + e] = sum(kResults + rj + e);
+        for (int e = 0; e < kOwn; e++) {
+            const int c = (rj + e) / 8 * 16 + (rj + e) % 8;   // the gate's column
+            v[e] = sum(c), v[kOwn + e] = sum(c + 8);
+        }
         am_finish_gated<kOwn>(p, i, j, v, b_scale, bias);
     } else {
         float v[kOwn], b_scale[kOwn], bias[kOwn];
@@ -137,30 +139,21 @@ void am_launch_thin(const AmProduct &p, hipStream_t st)
 // whatever the shape (measured), so the best shape is the one whose busiest CU has
 // the fewest rows of k to read.  (833, 2048, 80): 4 x 2 on 42 CUs 14.0 us, 2 x 1
 // on 135 8.1.
-template <typename E>
+template <typename E, bool kGated = false>
 void am_thin(const AmProduct &p, hipStream_t st)
 {
     const auto rows = [&](int ti, int tj) {
-        return (am_tiles(p.a.extent, p.b.extent, ti * 16, tj * 16) + kComputeUnits - 1) / kComputeUnits * (ti + tj);
+        return (am_tiles(p.a.extent, p.b.extent, ti * 16, kGated ? tj * 8 : tj * 16) + kComputeUnits - 1) / kComputeUnits * (ti + tj);
     };
     const int64_t r11 = rows(1, 1), r21 = rows(2, 1), r22 = rows(2, 2), r42 = rows(4, 2);
-    if (r42 <= r22 && r42 <= r21 && r42 <= r11) am_launch_thin<E, 4, 2>(p, st);
-    else if (r22 <= r21 && r22 <= r11) am_launch_thin<E, 2, 2>(p, st);
-    else if (r21 <= r11) am_launch_thin<E, 2, 1>(p, st);
-    else am_launch_thin<E, 1, 1>(p, st);
-}
-
-// The same for gated layers, with a fragment of gates and one of values a workgroup.
-template <typename E>
-void am_gated_thin(const AmProduct &p, hipStream_t st)
-{
-    const auto rows = [&](int ti) {
-        return (am_tiles(p.a.extent, p.b.extent, ti * 16, 16) + kComputeUnits - 1) / kComputeUnits * (ti + 2);
-    };
-    const int64_t r1 = rows(1), r2 = rows(2), r4 = rows(4);
-    if (r4 <= r2 && r4 <= r1) am_launch_thin<E, 4, 2, true>(p, st);
-    else if (r2 <= r1) am_launch_thin<E, 2, 2, true>(p, st);
-    else am_launch_thin<E, 1, 2, true>(p, st);
+    if constexpr (kGated) {   // 1 row of (1024, 4096) 4.8 us, 2 x 2 5.2
+        const int64_t r12 = rows(1, 2);
+        if (r12 < r42 && r12 < r22 && r12 < r21 && r12 < r11) return am_launch_thin<E, 1, 2, kGated>(p, st);
+    }
+    if (r42 <= r22 && r42 <= r21 && r42 <= r11) am_launch_thin<E, 4, 2, kGated>(p, st);
+    else if (r22 <= r21 && r22 <= r11) am_launch_thin<E, 2, 2, kGated>(p, st);
+    else if (r21 <= r11) am_launch_thin<E, 2, 1, kGated>(p, st);
+    else am_launch_thin<E, 1, 1, kGated>(p, st);
 }
 
 }  // namespace wfd
