@@ -113,7 +113,7 @@ hipError_t am_launch_gated(const wfst_am_gated_args &a, hipStream_t st)
     p.activation = a.activation;
     // as a layer's products (am_linear.hip), of 2 N outputs
     const bool thin = M <= 32 || am_tiles(M, 2 * N, 64, 64) <= kComputeUnits / 2;
-    const int32_t tile = thin ? 0 : am_plan(M, 2 * N, p.inner, false, am_gated_direct(p.a, p.b, p.inner, static_cast<int>(el))).tile;
+    const int32_t tile = thin ? 0 : am_plan(M, 2 * N, p.inner, false, am_gated_direct(p.a, p.b, p.inner, static_cast<int>(el)), true).tile;
     if (a.x.type == WFST_F16) am_product_gated<f16>(p, tile, st);
     else if (a.x.type == WFST_BF16) am_product_gated<bf16>(p, tile, st);
     else am_product_gated<f8>(p, tile, st);

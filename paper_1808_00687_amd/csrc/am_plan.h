@@ -46,9 +46,11 @@ void am_in_launches(int64_t blocks, F go)
         go(static_cast<uint32_t>(first), static_cast<uint32_t>(blocks - first < kMost ? blocks - first : kMost));
 }
 
+constexpr int32_t kAmWide = 192;
+
 // Which tiles, and into how many parts k is split.
 struct AmPlan {
-    int32_t tile;     // 256, 128 or 64
+    int32_t tile;     // 256, 128 or 64; kAmWide: 128 x 256
     int32_t splits;
 };
 
@@ -67,7 +69,11 @@ struct AmPlan {
 // tile is missed by more than 10% in (4096, 1024, 2048) e4m3, 27 us in 256, 23 in 128,
 // (3000, 1024, 2048), 25 and 22, and (53274, 512, 640), 56 and 46; of 14 in bf16 in two,
 // (3000, 1024, 2048), 28.5 and 23, and (4096, 1024, 2048), 29 and 25.
-inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split, bool whole)
+// Gated layers have tiles of 128 x 256 besides (`wide`), where they are at most one a CU:
+// (777, 1024, 4096) 28.9 us in 256 x 256, 19.7 so; (1500, 2048, 2048) 45.7 and 34.7; in more
+// rounds they gain nothing, (3000, 1024, 4096) 56.5 and 58.5, and tiles of 128 x 128 that are at
+// most one a CU are faster, (400, 1024, 4096) 14.7 and 18.1, (777, 2048, 2048) 25.9 and 31.7.
+inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split, bool whole, bool wide = false)
 {
     struct Kind {
         int32_t tile;
@@ -75,17 +81,17 @@ inline AmPlan am_plan(int64_t rows, int64_t cols, int64_t inner, bool may_split,
         double stage[4];
     };
     constexpr Kind direct[] = {{256, 1, INT64_MAX, {1.45}}, {128, 1, kComputeUnits, {0.95}}, {128, 3, INT64_MAX, {1.5, 1.9, 2.3}},
-                               {64, 2, INT64_MAX, {0.5, 0.55}}};
+                               {64, 2, INT64_MAX, {0.5, 0.55}}, {kAmWide, 1, kComputeUnits, {1.08}}};
     // forward, and with k-major operands (the gradients' products, those that may be split)
     constexpr Kind staged[2][2] = {{{128, 4, INT64_MAX, {1.2, 1.5, 2.2, 2.9}}, {64, 4, INT64_MAX, {0.58, 0.72, 1.2, 1.6}}},
                                    {{128, 4, INT64_MAX, {1.2, 1.4, 2.1, 2.85}}, {64, 4, INT64_MAX, {0.58, 0.7, 0.85, 1.15}}}};
     const int64_t stages = (inner + 63) / 64;
     AmPlan best{64, 1};
     double least = 1e30;
-    for (int i = 0; i < (whole ? 4 : 2); i++) {
+    for (int i = 0; i < (whole ? wide ? 5 : 4 : 2); i++) {
         const Kind &k = whole ? direct[i] : staged[may_split][i];
         for (int32_t s = 1; s <= (may_split ? 64 : 1) && (s == 1 || stages / s >= 4); s *= 2) {
-            const int64_t n = am_tiles(rows, cols, k.tile, k.tile) * s, at_once = kComputeUnits * k.fit, rest = n % at_once;
+            const int64_t n = am_tiles(rows, cols, k.tile == kAmWide ? 128 : k.tile, k.tile == kAmWide ? 256 : k.tile) * s, at_once = kComputeUnits * k.fit, rest = n % at_once;
             if (n > k.most) break;
             double t = static_cast<double>(n / at_once) * k.stage[k.fit - 1];
             if (rest) t += k.stage[(rest - 1) / kComputeUnits];

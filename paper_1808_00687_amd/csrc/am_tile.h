@@ -834,6 +834,7 @@ void am_launch_tiles(const AmProduct &p, hipStream_t st)
 
 using AmLarge = AmShape<256, 256, 2, 4, 128, 2>;
 using AmLarge8 = AmShape<256, 128, 2, 2, 64, 3>;   // two workgroups a CU
+using AmWide = AmShape<128, 256, 2, 4, 128, 2>;
 using AmMedium = AmShape<128, 128, 2, 2, 64, 3>;
 using AmMediumMajor = AmShape<128, 128, 2, 2, 64, 4>;
 using AmMediumDeep = AmShape<128, 128, 2, 2, 128, 4>;   // one workgroup a CU
@@ -869,6 +870,7 @@ void am_gated_product(const AmProduct &p, int32_t tile, hipStream_t st)
 {
     if (am_gated_direct(p.a, p.b, p.inner, sizeof(E))) {
         if (tile == 256) am_launch_tiles<E, false, false, true, std::conditional_t<sizeof(E) == 1, AmLarge8, AmLarge>, false, false, true>(p, st);
+        else if (tile == kAmWide) am_launch_tiles<E, false, false, true, AmWide, false, false, true>(p, st);
         else if (tile == 128 && am_tiles(p.a.extent, 2 * int64_t{p.b.extent}, 128, 128) <= kComputeUnits)
             am_launch_tiles<E, false, false, true, AmMediumDeep, false, false, true>(p, st);
         else if (tile == 128) am_launch_tiles<E, false, false, true, AmMedium, false, false, true>(p, st);

@@ -75,9 +75,9 @@ def test_strides_and_alignment(am, dt, pad, offset, out_pad):
         case(am, m, k, n, dt, "silu", out, 4, pre=True, pad=pad, offset=offset, out_pad=out_pad)
 
 
-# 256 x 128 results a workgroup, 128 x 64 in one round and in several, rows off 16 bytes
+# 256 x 128 results a workgroup, 128 x 64 in one round and in several, 128 x 128, rows off 16 bytes
 LARGE = [(1500, 1400, 100), (2904, 1024, 1500), (2040, 456, 980), (4096, 520, 512), (1501, 1403, 700), (3001, 200, 2005),
-         (8200, 136, 2050)]
+         (8200, 136, 2050), (1470, 328, 2040), (1921, 72, 1913)]
 
 
 @pytest.mark.parametrize("dt", [BF16, F16, F8])
