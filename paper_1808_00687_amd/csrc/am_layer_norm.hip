@@ -11,6 +11,8 @@
 //
 // (53274, 1024) bf16 with the residual to e4m3: 76 us, 382 MB, 5.0 TB/s (a large copy
 // reaches 5.0); backward of (16384, 2048) bf16 with dsum: 48 us and 5 of the join, 268 MB.
+#include <type_traits>
+
 #include "am_rows.h"
 
 namespace wfd {
@@ -43,6 +45,54 @@ __device__ __forceinline__ void row_sums(float (&v)[K], SumScratch<N> &r, int &t
     turn ^= 1;
 }
 
+// A thread's chunks of one row of a matrix, as RowPart's, but threads past the row's end go
+// through nothing ((52429, 1280) bf16 gradients with dsum 119 us, 172 otherwise; (104858, 640)
+// 131 and 170), and a chunk of 8 over it is the row's last 8 values, moved to their places: one
+// load in place of seven ((23141, 2900) 168 and 227).
+template <typename S, typename T>
+struct Part {
+    using V = Chunk<T, S::kC>;
+    using Bits = std::conditional_t<sizeof(T) * S::kC == 16, unsigned __int128, uint64_t>;
+    static_assert(sizeof(V) == sizeof(Bits), "");
+    static constexpr bool kMoved = S::kC == 8;
+    const T *p;
+    V held[S::kHeld];
+
+    __device__ __forceinline__ void hold(const T *row, int64_t cols, int t)
+    {
+        p = row;
+        if constexpr (S::kNv > 0)
+#pragma unroll
+            for (int v = 0; v < S::kNv; v++) {
+                const int64_t c = (static_cast<int64_t>(v) * S::kTpr + t) * S::kC, left = cols - c;
+                held[v] = V{};
+                if (left >= S::kC) {
+                    held[v] = *(const AM_GLOBAL V *)(row + c);
+                } else if (left > 0) {
+                    if (kMoved && c > 0) {
+                        // A vector register, although a wave's threads may share the address: a scalar load
+                        // of one that is not on 4 bytes takes the 4 bytes that it lies in.
+                        int64_t last = cols - S::kC;
+                        __asm__("" : "+v"(last));
+                        const V u = *(const AM_GLOBAL V *)(row + last);
+                        held[v] = __builtin_bit_cast(V, __builtin_bit_cast(Bits, u) >> static_cast<int>((S::kC - left) * static_cast<int64_t>(sizeof(T)) * 8));
+                    } else {
+                        held[v] = load_chunk<T, S::kC>(row + c, left, static_cast<T>(0.0f));
+                    }
+                }
+            }
+    }
+    __device__ __forceinline__ void get(int v, int64_t c, int64_t left, float (&x)[S::kC]) const
+    {
+        if constexpr (S::kNv > 0) {
+#pragma unroll
+            for (int e = 0; e < S::kC; e++) x[e] = static_cast<float>(held[v][e]);
+        } else {
+            load_floats<T, S::kC>(p + c, left, x);
+        }
+    }
+};
+
 // A row's mean is m0 + c; rho is the reciprocal of its standard deviation.
 struct Moments {
     float m0, c, rho;
@@ -68,7 +118,7 @@ __global__ __launch_bounds__(S::kThreads) void layer_norm_kernel(wfst_am_layer_n
     RowPart<S, float> gain, bias;
     if (a.gain) gain.hold(a.gain, D, t);
     if (a.bias) bias.hold(a.bias, D, t);
-    RowPart<S, T> x, r, x_next, r_next;
+    Part<S, T> x, r, x_next, r_next;
     const auto hold = [&](int64_t m) {
         if (m >= M) return;
         x_next.hold(row<T>(a.x, m), D, t);
@@ -173,7 +223,7 @@ __global__ __launch_bounds__(S::kThreads) void layer_norm_backward_kernel(wfst_a
     RowPart<S, float> gain;
     if (a.gain) gain.hold(a.gain, D, t);
     float dg[S::kHeld][S::kC] = {}, db[S::kHeld][S::kC] = {};
-    RowPart<S, T> s, dy, ds, s_next, dy_next;
+    Part<S, T> s, dy, ds, s_next, dy_next;
     const auto hold = [&](int64_t m) {
         if (m >= M) return;
         s_next.hold(row<T>(a.s, m), D, t);
@@ -329,7 +379,8 @@ __global__ __launch_bounds__(256) void layer_norm_columns_kernel(wfst_am_layer_n
 
 // Rows of few columns share a wave: (349525, 96) bf16 to 8 bits with the residual 63 us, with a wave a row
 // 217, (524288, 64) 44 and 317, (131072, 256) 43 and 83; backward of (349525, 96) with dsum 75 and 252, of (131072,
-// 256) 57 and 103.
+// 256) 57 and 103.  Rows of 1,025 to 1,536 16-bit columns take three chunks a lane ((52429, 1280) to 8 bits with the
+// residual 101 us, in four 129).
 template <int C, typename F>
 void row_shape(int64_t D, F go)
 {
@@ -337,6 +388,7 @@ void row_shape(int64_t D, F go)
     if (D <= 64) go(RowShape<8, 1 * k, C>{});
     else if (D <= 128) go(RowShape<16, 1 * k, C>{});
     else if (D <= 256) go(RowShape<32, 1 * k, C>{});
+    else if (C == 8 && D > 1024 && D <= 1536) go(RowShape<64, 3, C>{});
     else am_row_shape_norm<C>(D, go);
 }
 
@@ -350,6 +402,7 @@ void row_shape_backward(int64_t D, F go)
     if (D <= 64) go(RowShape<8, 1 * k, C>{});
     else if (D <= 128) go(RowShape<16, 1 * k, C>{});
     else if (D <= 256) go(RowShape<32, 1 * k, C>{});
+    else if (C == 8 && D > 1024 && D <= 1536) go(RowShape<64, 3, C>{});
     else if (C == 4 && D > 1024 && D <= 2048) go(RowShape<256, 1 * k, C>{});
     else if (D > 16384) go(RowShape<1024, 0, C>{});
     else am_row_shape<C>(D, go);

@@ -20,7 +20,7 @@ def am():
     return acoustic
 
 
-WIDTHS = [1, 2, 7, 8, 9, 64, 65, 440, 511, 513, 1000, 1024, 1025, 1300, 2048, 2500, 4097, 5000, 6145, 8192, 9001, 16384, 20000]
+WIDTHS = [1, 2, 7, 8, 9, 15, 63, 64, 65, 129, 255, 257, 440, 511, 513, 1000, 1024, 1025, 1300, 1536, 1537, 2048, 2500, 4097, 5000, 6145, 8192, 9001, 16384, 20000]
 
 
 def check(am, x, r, gain, bias, out, tag, pad=0, offset=0, eps=1e-5, in_place=False):
