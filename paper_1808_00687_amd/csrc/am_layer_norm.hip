@@ -411,7 +411,7 @@ void row_shape_backward(int64_t D, F go)
 // Workgroups at most.  Backward about as many as are resident, by the bytes of a matrix that a thread holds: one
 // more and the last ones run alone (268 MB each, 1 to 5 a CU: 512 bf16 columns 95, 67, 62, 58, 57 us; 1,024 72, 52,
 // 51, 60, 57; 2,048 64, 52, 63, 61, 61; 8,192 72, 63, 76, 79, 78; 2,048 float32 64, 49, 50, 51, 54).
-constexpr int64_t kForwardBlocks = 256 * 16;
+constexpr int64_t kForwardBlocks = 256 * 32;   // (53274, 1024) to 8 bits: 8, 16, 24, 32, 64 a CU take 93, 97, 91, 90, 97
 
 template <typename S>
 constexpr int64_t backward_blocks(int64_t el)

@@ -39,9 +39,12 @@
 // Measured, bf16: (16384, 4096, 1024) k-contiguous 107 us, 1,280 TFLOP/s (the
 // library's product 94 us); (16384, 4096, 1024) with b k-major 120; k = 16384
 // into 4096 x 1024, both k-major, 139 and 17 for joining 4 parts; with a in two parts
-// 240 and 318.  The matrix cores are busy 53% of the time (k-contiguous a) and 37% (both
-// k-major, 1.3 GB of reads behind the L2s for two parts).  No LDS bank conflicts but in
-// k-contiguous stages of 64 bytes, where they take 6 to 11% of a CU's cycles (7 in 8
+// 255 and 288.  The matrix cores are busy 53% of the time (403 MB of reads behind the L2s
+// for two parts of both k-major; 1.3 GB when a part's tiles were dealt to all chiplets).
+// Gated, (16384, 1024, 4096): 244 us, 1,127 TFLOP/s (the library's plain product of twice the
+// outputs 246), with pre 310 (matrix cores busy 37%: 403 MB are stored while no products are
+// formed).  No LDS bank conflicts but in
+// k-contiguous stages of 64 bytes, where they take 6 to 11% of a CU's cycles (7 to 9 in 8
 // bits, 11 in unaligned rows).  The rest is the waves' meeting once a stage and, for a
 // short k, the start and the epilogue of a tile ((16384, 1024, 4096): 142 to 159 us).
 // 256 x 256 tiles with 4 waves of twice the registers made the compiler move sums about;
@@ -557,7 +560,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesASimd) void am_tile_kernel(Am
     const int lane_ = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t ti, tj, k_part;
     const uint32_t rows = (p.a.extent + BM - 1) / BM, cols = (p.b.extent + kResults - 1) / kResults;
-    if (gridDim.x == rows * cols) {   // all in one launch
+    bool one_launch = false;   // are several parts' tiles all in it?
+    if constexpr (kMajorB) one_launch = gridDim.x == rows * cols;
+    if (one_launch) {
         am_tile_of(blockIdx.y * gridDim.x + blockIdx.x, rows, cols, p.splits, ti, tj, k_part);
     } else {
         am_tile_of(p.first + blockIdx.x, rows, cols, 1, ti, tj, k_part);
