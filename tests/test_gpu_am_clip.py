@@ -14,8 +14,6 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-CHUNK = 16384   # bytes of a workgroup's turn
-
 
 @pytest.fixture(scope="module")
 def am():
