@@ -35,7 +35,9 @@ __global__ __launch_bounds__(256) void gated_slope_kernel(wfst_am_gated_backward
             for (int e = 0; e < 8; e++) {
                 float act;
                 const float slope = am_slope(z[e], a.activation, &act);
-                u[e] = g[e] * u[e] * slope;
+                // the slope (at most 1.13) takes bf16's larger factor: dy * value may be no float32 where dz is one
+                const bool by_value = __is_same(T, bf16) && fabsf(u[e]) > fabsf(g[e]);
+                u[e] = (by_value ? u[e] : g[e]) * slope * (by_value ? g[e] : u[e]);
                 z[e] = g[e] * act;
                 sum[e] += u[e];
                 sum[8 + e] += z[e];

@@ -1,0 +1,38 @@
+"""The gated layer, the layer norm and the clipping at the ends of the types' ranges and of the sizes that they take."""
+import pytest
+
+import am_reference as R
+import am_reference_more as Q
+from test_gpu_am_operators import BF16, F32
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def am():
+    assert torch.cuda.is_available(), "no GPU"
+    from paper_1808_00687_amd import acoustic
+    return acoustic
+
+
+@pytest.mark.parametrize("kind", ["none", "relu", "silu", "gelu"])
+@pytest.mark.parametrize("large", [(1e20, 1e20), (3e30, 1e12), (1e12, 3e30), (1e30, 1e-25), (1e-25, 1e30)])
+def test_gradients_of_gates_whose_factors_are_far_from_one(am, kind, large):
+    # dy value is no float32 where the slope makes dy value slope one, or 0.  A row a gate, so nothing is summed: dbias of a
+    # row is its float32 dz, dw of x = 1 the dz as two bfloat16 values hold it
+    size_dy, size_value = large
+    for gate in (-100.0, -60.0, -20.0, -3.0, 0.0, 1.0):
+        dy = torch.full((1, 1), size_dy).to(BF16)
+        pre = torch.tensor([[gate, size_value]]).to(BF16)
+        dz, slack = Q.gated_dz(dy, pre, kind)
+        if not (dz.abs() < 3e38).all():
+            continue
+        one = torch.ones(1, 1, dtype=BF16).cuda()
+        _, dw, db = am.wfst_am_gated_backward(dy.cuda(), pre.cuda(), one, torch.ones(2, 1, dtype=BF16).cuda(), activation=kind,
+                                               weight_dtype=F32)
+        err = slack + 2 * R.U32 * dz.abs()   # and the products' own roundings
+        tag = "%s %s %g" % (kind, large, gate)
+        R.close(db[None], dz, err, tag + " dbias")
+        R.close(dw.t(), dz, err + 2.0 ** -16 * dz.abs() + R.TINY[BF16], tag + " dw")
