@@ -10,6 +10,7 @@
 // (53274, 1024) bf16 with the residual to e4m3: 72 us, 382 MB, 5.3 TB/s (a large
 // copy reaches 5.1); backward of (16384, 2048) bf16 with dsum: 57 us, 268 MB,
 // 4.7 TB/s, 5 of it the join.
+#include "am_plan.h"
 #include "am_rows.h"
 
 namespace wfd {
@@ -203,12 +204,13 @@ __global__ __launch_bounds__(256) void norm_dgain_kernel(wfst_am_norm_backward_a
 }
 
 // 32 columns a workgroup, 32 threads a column, 4 strips of a thread on their way at a
-// time; blockIdx.y: which of two sums (the second one's strips behind the first one's)
-__global__ __launch_bounds__(1024) void column_join_kernel(const float *partial, int64_t strips, int64_t n, float *out, float *out2)
+// time; blockIdx.y: which of two sums (the second one's strips behind the first one's);
+// `block`: of the launch's first workgroup
+__global__ __launch_bounds__(1024) void column_join_kernel(const float *partial, int64_t strips, int64_t n, uint32_t block, float *out, float *out2)
 {
     __shared__ float part[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + x;
+    const int64_t c = static_cast<int64_t>(block + blockIdx.x) * 32 + x;
     if (blockIdx.y) partial += strips * n, out = out2;
     float t = 0.0f;
     if (c < n) {
@@ -294,7 +296,9 @@ void launch_norm_backward(const wfst_am_norm_backward_args &a, hipStream_t st)
 
 void am_launch_column_join(const float *partial, int64_t strips, int64_t n, float *out, float *out2, hipStream_t st)
 {
-    column_join_kernel<<<dim3(static_cast<unsigned>((n + 31) / 32), out2 ? 2 : 1), 1024, 0, st>>>(partial, strips, n, out, out2);
+    am_in_launches((n + 31) / 32, [&](uint32_t first, uint32_t blocks) {
+        column_join_kernel<<<dim3(blocks, out2 ? 2 : 1), 1024, 0, st>>>(partial, strips, n, first, out, out2);
+    }, 1024);
 }
 
 hipError_t am_launch_norm(const wfst_am_norm_args &a, hipStream_t st)

@@ -35,15 +35,15 @@ inline bool am_gated_direct(const AmOperand &a, const AmOperand &b, int32_t inne
 
 inline int64_t am_tiles(int64_t rows, int64_t cols, int64_t m, int64_t n) { return ((rows + m - 1) / m) * ((cols + n - 1) / n); }
 
-// go(first, count) for consecutive runs of `blocks` workgroups, each run a launch: one
-// takes fewer than 2^32 threads in a dimension (a workgroup has at most 512), and
-// runs start at multiples of 8, so a block's chiplet is its index modulo 8.
+// go(first, count) for consecutive runs of `blocks` workgroups of at most `threads` threads,
+// each run a launch: one takes fewer than 2^32 threads in a dimension, and runs start at
+// multiples of 8, so a block's chiplet is its index modulo 8.
 template <typename F>
-void am_in_launches(int64_t blocks, F go)
+void am_in_launches(int64_t blocks, F go, int64_t threads = 512)
 {
-    constexpr int64_t kMost = int64_t{1} << 22;
-    for (int64_t first = 0; first < blocks; first += kMost)
-        go(static_cast<uint32_t>(first), static_cast<uint32_t>(blocks - first < kMost ? blocks - first : kMost));
+    const int64_t most = (int64_t{1} << 31) / threads;
+    for (int64_t first = 0; first < blocks; first += most)
+        go(static_cast<uint32_t>(first), static_cast<uint32_t>(blocks - first < most ? blocks - first : most));
 }
 
 constexpr int32_t kAmWide = 192;

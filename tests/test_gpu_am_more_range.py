@@ -36,3 +36,24 @@ def test_gradients_of_gates_whose_factors_are_far_from_one(am, kind, large):
         tag = "%s %s %g" % (kind, large, gate)
         R.close(db[None], dz, err, tag + " dbias")
         R.close(dw.t(), dz, err + 2.0 ** -16 * dz.abs() + R.TINY[BF16], tag + " dw")
+
+
+def test_gradients_of_rows_of_2_to_the_27_columns(am):
+    # their sums are joined by more workgroups than one launch takes
+    width = (1 << 27) + 33
+    g = torch.Generator("cuda").manual_seed(3)
+    s, dy = (torch.randn(1, width, generator=g, device="cuda", dtype=BF16) for _ in range(2))
+    dx, dg, db = am.wfst_am_layer_norm_backward(dy, s)
+    assert torch.equal(db, dy[0].float())   # of one row
+    del dx
+    v = s[0].double()
+    mean = v.mean()
+    v -= mean
+    r = float(1 / torch.sqrt((v * v).mean() + 1e-5))
+    size = float(v.abs().mean())
+    # am_reference_more.py's Moments: the mean, a difference, the reciprocal deviation
+    e_mean = R.sum_bound(width, size * width) / width
+    rel = (R.LAMBDA * width ** 0.5 + 8) * R.U32 / 2 + 6 * R.U32
+    off = (dg.double() - v * r * dy[0].double()).abs_()
+    bound = (v.abs_().mul_(r * (3 * R.U32 + rel + R.U32)).add_(r * e_mean)).mul_(dy[0].double().abs())
+    assert bool((off <= bound).all()), float((off - bound).max())
