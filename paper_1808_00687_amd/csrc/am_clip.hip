@@ -125,7 +125,7 @@ struct Piece {
     }
 };
 
-using Raw = uint32_t __attribute__((ext_vector_type(4), aligned(1)));   // 16 bytes at any address
+using Raw = Chunk<uint32_t, 4, 1>;   // 16 bytes at any address
 
 // A chunk of a tensor, 16 bytes a thread and part.
 template <int kParts>

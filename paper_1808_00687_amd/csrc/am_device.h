@@ -69,9 +69,17 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
 #define AM_GLOBAL __attribute__((address_space(1)))
 
 // C consecutive elements of a row, at any address (wide accesses need no
-// alignment on this hardware); n of them exist, the others read as `fill`.
-template <typename T, int C>
-using Chunk = T __attribute__((ext_vector_type(C), aligned(sizeof(T))));
+// alignment on this hardware); n of them exist, the others read as `fill`.  The type
+// says so by a typedef: in a `using` the compiler drops `aligned` without a word and
+// takes the vector's own, and from that it may make a scalar load of an address that
+// a wave's threads share, which drops the address's low bits.
+template <typename T, int C, int kAlign>
+struct ChunkOf {
+    typedef T Type __attribute__((ext_vector_type(C), aligned(kAlign)));
+    static_assert(alignof(Type) == kAlign, "");
+};
+template <typename T, int C, int kAlign = sizeof(T)>
+using Chunk = typename ChunkOf<T, C, kAlign>::Type;
 
 template <typename T, int C>
 __device__ __forceinline__ Chunk<T, C> load_chunk(const T *p, int64_t n, T fill)
@@ -111,7 +119,7 @@ __device__ __forceinline__ void store_floats(T *p, int64_t n, const float (&x)[C
 template <int C>
 __device__ __forceinline__ void store_floats(f8 *p, int64_t n, const float (&x)[C])
 {
-    using V = uint32_t __attribute__((ext_vector_type(C / 4), aligned(1)));
+    using V = Chunk<uint32_t, C / 4, 1>;
     V v;
 #pragma unroll
     for (int h = 0; h < C / 4; h++) {

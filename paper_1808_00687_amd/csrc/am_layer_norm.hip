@@ -70,11 +70,7 @@ struct Part {
                     held[v] = *(const AM_GLOBAL V *)(row + c);
                 } else if (left > 0) {
                     if (kMoved && c > 0) {
-                        // A vector register, although a wave's threads may share the address: a scalar load
-                        // of one that is not on 4 bytes takes the 4 bytes that it lies in.
-                        int64_t last = cols - S::kC;
-                        __asm__("" : "+v"(last));
-                        const V u = *(const AM_GLOBAL V *)(row + last);
+                        const V u = *(const AM_GLOBAL V *)(row + (cols - S::kC));
                         held[v] = __builtin_bit_cast(V, __builtin_bit_cast(Bits, u) >> static_cast<int>((S::kC - left) * static_cast<int64_t>(sizeof(T)) * 8));
                     } else {
                         held[v] = load_chunk<T, S::kC>(row + c, left, static_cast<T>(0.0f));

@@ -64,7 +64,7 @@ namespace wfd {
 
 using i16x4 = short __attribute__((ext_vector_type(4)));
 using i32x4 = int __attribute__((ext_vector_type(4)));
-using i32x4_any = int __attribute__((ext_vector_type(4), aligned(1)));   // at any address
+using i32x4_any = Chunk<int, 4, 1>;   // at any address
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using f16x8 = f16 __attribute__((ext_vector_type(8)));
 using bf16x8 = bf16 __attribute__((ext_vector_type(8)));
@@ -152,7 +152,7 @@ __device__ __forceinline__ void am_store_row(const wfst_matrix &m, int64_t i, in
 {
     T *p = static_cast<T *>(m.data) + i * m.row_stride + j;
     constexpr int kStep = N * sizeof(T) >= 16 ? 16 / sizeof(T) : N;
-    using V = T __attribute__((ext_vector_type(kStep), aligned(sizeof(T))));
+    using V = Chunk<T, kStep>;
     if (full) {
 #pragma unroll
         for (int s = 0; s < N; s += kStep) {
@@ -181,7 +181,7 @@ __device__ __forceinline__ void am_add_row(const wfst_matrix &m, int64_t i, int6
 {
     const T *p = static_cast<const T *>(m.data) + i * m.row_stride + j;
     constexpr int kStep = N * sizeof(T) >= 16 ? 16 / sizeof(T) : N;
-    using V = T __attribute__((ext_vector_type(kStep), aligned(sizeof(T))));
+    using V = Chunk<T, kStep>;
     if (full) {
 #pragma unroll
         for (int s = 0; s < N; s += kStep) {
