@@ -1,5 +1,11 @@
 """The layer norm, the gated layer and the clipping at the limits of what they take: host code, compiled alone (no GPU
 needed)."""
+import os
+import subprocess
+
+import pytest
+
+from paper_1808_00687_amd.csrc import build
 from test_am_plan import run
 
 
@@ -16,3 +22,21 @@ def test_columns_of_a_join_fit_their_launches(tmp_path):
             at += count
         assert at == -(-n // 32)
         assert n > 1 << 26 or len(runs) == 2
+
+
+def test_the_gradients_products_do_not_ask_for_their_grid(tmp_path):
+    # it lies behind the arguments in memory: one more read, 0.4 us, before a workgroup knows its tile
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("no hipcc")
+    src = tmp_path / "tile.hip"
+    src.write_text("""#include "am_tile.h"
+namespace wfd {
+template __global__ void am_tile_kernel<bf16, true, true, false, AmSmallMajorStaged, false, false, false>(AmProduct);
+template __global__ void am_tile_kernel<bf16, false, true, true, AmSmallMajor, false, true, false>(AmProduct);
+}
+""")
+    flags = [f for f in build.FLAGS if f != "-fPIC"]
+    text = subprocess.check_output([build.HIPCC, "-x", "hip", *flags, "--cuda-device-only", "-S", "-emit-llvm", str(src), "-o", "-"],
+                                   text=True, stderr=subprocess.DEVNULL)
+    assert text.count("define protected amdgpu_kernel void @") == 2
+    assert "llvm.amdgcn.implicitarg.ptr" not in text
