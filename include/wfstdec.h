@@ -852,7 +852,9 @@ int wfst_am_distill_backward(const wfst_am_distill_args *args, void *hip_stream)
  * clipped a grad in place is not written.  With a NaN among the values the norm
  * is one and nothing is clipped; an infinity makes the norm infinite and, unless
  * max_norm is, the factor 0: infinities become NaN, the others 0.
- * The check of the places takes host memory, about 100 bytes a tensor.
+ * The check of the places takes host memory, about 100 bytes a tensor and at most
+ * about 400, and the time of a sort (more only for grads that overlap other grads in
+ * part).
  * Errors: WFST_EINVAL (also a workspace that is too small), WFST_ENOMEM,
  * WFST_EDEVICE.
  */

@@ -1,6 +1,5 @@
 // Entry points of the acoustic-model operators: the argument checks (before
 // any device call), then one launcher each.
-#include <algorithm>
 #include <cmath>
 #include <cstddef>
 #include <cstdint>
@@ -8,27 +7,12 @@
 #include <vector>
 
 #include "am.h"
+#include "am_places.h"
 #include "internal.h"
 
 using namespace wfd;
 
 namespace {
-
-struct Range {
-    uintptr_t lo, hi;        // bytes [lo, hi); empty where there is nothing
-    uintptr_t stride = 0;    // of a matrix of several rows: bytes [lo + i stride, lo + i stride + width) of them
-    uintptr_t width = 0;
-};
-
-// No byte of one is a byte of the other.  Matrices with the same stride are compared by
-// their columns (slices of one buffer), others by their whole spans.
-bool disjoint(const Range &a, const Range &b)
-{
-    if (!(a.lo < b.hi && b.lo < a.hi)) return true;
-    if (!a.stride || a.stride != b.stride) return false;
-    const uintptr_t off = b.lo >= a.lo ? (b.lo - a.lo) % a.stride : (a.stride - (a.lo - b.lo) % a.stride) % a.stride;
-    return off >= a.width && off + b.width <= a.stride;
-}
 
 // A call's checks: the first one that fails sets the message.
 struct Checks {
@@ -373,36 +357,18 @@ bool check_sizes(Checks &c, const wfst_am_clip_args &a)
     return c.need(a.count >= 0 && a.count <= WFST_AM_MAX_TENSORS, "the tensors must be 0 to 65536");
 }
 
-// Outputs lie apart from one another and from all other grads.  Spans are gone
-// through in the order of their first bytes; those that the present one may overlap
-// are kept, so tensors with places of their own cost a sort.
+// Outputs lie apart from one another and from all other grads.
 bool check_places(Checks &c, const wfst_am_clip_args &a, Range norm, Range workspace)
 {
-    struct Span {
-        Range r;
-        int64_t i;     // tensor; -1: the norm or the workspace
-        bool written;
-    };
-    std::vector<Span> spans, outs, ins;   // all; those written and those read that reach as far as the present one
+    std::vector<Span> spans;
     spans.reserve(static_cast<size_t>(a.count) * 2 + 2);
     for (int64_t i = 0; i < a.count; i++) {
-        spans.push_back({range_of(a.outs ? a.outs[i] : a.grads[i]), i, true});
-        if (a.outs && !same_place(a.outs[i], a.grads[i])) spans.push_back({range_of(a.grads[i]), i, false});
+        spans.push_back({range_of(a.outs ? a.outs[i] : a.grads[i]), true});
+        if (a.outs && !same_place(a.outs[i], a.grads[i])) spans.push_back({range_of(a.grads[i]), false});
     }
-    spans.push_back({norm, -1, true});
-    spans.push_back({workspace, -1, true});
-    std::sort(spans.begin(), spans.end(), [](const Span &x, const Span &y) { return x.r.lo < y.r.lo; });
-    for (const Span &s : spans) {
-        if (s.r.lo == s.r.hi) continue;
-        for (std::vector<Span> *v : {&outs, &ins}) std::erase_if(*v, [&](const Span &o) { return o.r.hi <= s.r.lo; });
-        for (const Span &o : outs)
-            if (!c.apart(s.r, o.r, kOverlap)) return false;
-        if (s.written)
-            for (const Span &o : ins)
-                if (!c.apart(s.r, o.r, kOverlap)) return false;
-        (s.written ? outs : ins).push_back(s);
-    }
-    return true;
+    spans.push_back({norm, true});
+    spans.push_back({workspace, true});
+    return c.need(spans_apart(spans), kOverlap);
 }
 
 bool check(Checks &c, const wfst_am_clip_args &a)

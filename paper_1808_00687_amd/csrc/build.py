@@ -23,7 +23,7 @@ SOURCES = ["graph.cpp", "decode.cpp", "search_kernel.hip", "search_record_kernel
            "final_kernels.hip", "word_kernel.hip", "am.cpp", "am_norm.hip", "am_layer_norm.hip", "am_distill.hip", "am_clip.hip", "am_loglikes.hip", "am_linear.hip",
            "am_linear_bf16.hip", "am_linear_f16.hip", "am_linear_f8.hip", "am_gated.hip", "am_gated_bf16.hip",
            "am_gated_f16.hip", "am_gated_f8.hip"]
-HEADERS = ["internal.h", "device_util.h", "record_set.h", "search_body.h", "am.h", "am_device.h", "am_linear.h", "am_plan.h", "am_rows.h", "am_softmax.h", "am_thin.h", "am_tile.h"]
+HEADERS = ["internal.h", "device_util.h", "record_set.h", "search_body.h", "am.h", "am_device.h", "am_linear.h", "am_places.h", "am_plan.h", "am_rows.h", "am_softmax.h", "am_thin.h", "am_tile.h"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
