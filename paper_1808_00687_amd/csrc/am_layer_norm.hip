@@ -381,11 +381,10 @@ template <int C, typename F>
 void row_shape(int64_t D, F go)
 {
     constexpr int k = 8 / C;
-    if (D <= 64) go(RowShape<8, 1 * k, C>{});
-    else if (D <= 128) go(RowShape<16, 1 * k, C>{});
-    else if (D <= 256) go(RowShape<32, 1 * k, C>{});
-    else if (C == 8 && D > 1024 && D <= 1536) go(RowShape<64, 3, C>{});
-    else am_row_shape_norm<C>(D, go);
+    am_shape_of<UpTo<64, RowShape<8, 1 * k, C>>, UpTo<128, RowShape<16, 1 * k, C>>, UpTo<256, RowShape<32, 1 * k, C>>,
+                UpTo<512, RowShape<64, 1 * k, C>>, UpTo<1024, RowShape<64, 2 * k, C>>, UpTo<C == 8 ? 1536 : 0, RowShape<64, 3, C>>,
+                UpTo<2048, RowShape<64, 4 * k, C>>, UpTo<4096, RowShape<256, 2 * k, C>>, UpTo<6144, RowShape<256, 3 * k, C>>,
+                UpTo<8192, RowShape<256, 4 * k, C>>, UpTo<16384, RowShape<1024, 2 * k, C>>, UpTo<INT64_MAX, RowShape<1024, 0, C>>>(D, go);
 }
 
 // And for the gradients: rows of 1,025 to 2,048 float32 columns take 256 threads ((11184, 1500) 53 us, a wave 67),
@@ -395,13 +394,11 @@ template <int C, typename F>
 void row_shape_backward(int64_t D, F go)
 {
     constexpr int k = 8 / C;
-    if (D <= 64) go(RowShape<8, 1 * k, C>{});
-    else if (D <= 128) go(RowShape<16, 1 * k, C>{});
-    else if (D <= 256) go(RowShape<32, 1 * k, C>{});
-    else if (C == 8 && D > 1024 && D <= 1536) go(RowShape<64, 3, C>{});
-    else if (C == 4 && D > 1024 && D <= 2048) go(RowShape<256, 1 * k, C>{});
-    else if (D > 16384) go(RowShape<1024, 0, C>{});
-    else am_row_shape<C>(D, go);
+    am_shape_of<UpTo<64, RowShape<8, 1 * k, C>>, UpTo<128, RowShape<16, 1 * k, C>>, UpTo<256, RowShape<32, 1 * k, C>>,
+                UpTo<512, RowShape<64, 1 * k, C>>, UpTo<1024, RowShape<64, 2 * k, C>>, UpTo<C == 8 ? 1536 : 0, RowShape<64, 3, C>>,
+                UpTo<2048, std::conditional_t<C == 8, RowShape<64, 4, C>, RowShape<256, 1 * k, C>>>, UpTo<4096, RowShape<256, 2 * k, C>>,
+                UpTo<6144, RowShape<256, 3 * k, C>>, UpTo<8192, RowShape<256, 4 * k, C>>, UpTo<16384, RowShape<1024, 2 * k, C>>,
+                UpTo<INT64_MAX, RowShape<1024, 0, C>>>(D, go);
 }
 
 // Workgroups at most.  Backward about as many as are resident, by the bytes of a matrix that a thread holds: one

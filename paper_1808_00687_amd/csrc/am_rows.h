@@ -41,7 +41,28 @@ struct RowShape {
     }
 };
 
-// Calls go(shape) with the shape for rows of D columns.  Its bounds, in us for 8e7
+// A table of shapes: rows of up to kMost columns take S (0: it is not in the table).
+template <int64_t kMost, typename S>
+struct UpTo {
+    static constexpr int64_t kColumns = kMost;
+    using Shape = S;
+};
+
+// Calls go(shape) with a table's first shape that takes rows of D columns.  Bounds ascend, so
+// every shape has its rows: those that none would take are not compiled.
+template <typename First, typename... Rest, typename F>
+void am_shape_of(int64_t D, F go)
+{
+    if constexpr (First::kColumns == 0) {
+        am_shape_of<Rest...>(D, go);
+    } else {
+        static_assert(sizeof...(Rest) > 0 || First::kColumns == INT64_MAX, "");
+        if (D <= First::kColumns) return go(typename First::Shape{});
+        if constexpr (sizeof...(Rest) > 0) am_shape_of<Rest...>(D, go);
+    }
+}
+
+// The shape for rows of D columns.  Its bounds, in us for 8e7
 // bf16 values (norm to 8 bits with a residual / loss with gradient / log-likelihoods):
 //   1,024 columns: a wave 73 / 85 / 60, 256 threads 87 / 180 / 110
 //   2,048: a wave 106 / 109 / 94, 256 threads 112 / 147 / 92
@@ -54,15 +75,9 @@ template <int C, typename F>
 void am_row_shape(int64_t D, F go)
 {
     constexpr int k = 8 / C;
-    if (D <= 512) go(RowShape<64, 1 * k, C>{});
-    else if (D <= 1024) go(RowShape<64, 2 * k, C>{});
-    else if (D <= 2048) go(RowShape<64, 4 * k, C>{});
-    else if (D <= 4096) go(RowShape<256, 2 * k, C>{});
-    else if (D <= 6144) go(RowShape<256, 3 * k, C>{});
-    else if (D <= 8192) go(RowShape<256, 4 * k, C>{});
-    else if (D <= 16384) go(RowShape<1024, 2 * k, C>{});
-    else if (D <= kRowHeld) go(RowShape<1024, 4 * k, C>{});
-    else go(RowShape<1024, 0, C>{});
+    am_shape_of<UpTo<512, RowShape<64, 1 * k, C>>, UpTo<1024, RowShape<64, 2 * k, C>>, UpTo<2048, RowShape<64, 4 * k, C>>,
+                UpTo<4096, RowShape<256, 2 * k, C>>, UpTo<6144, RowShape<256, 3 * k, C>>, UpTo<8192, RowShape<256, 4 * k, C>>,
+                UpTo<16384, RowShape<1024, 2 * k, C>>, UpTo<kRowHeld, RowShape<1024, 4 * k, C>>, UpTo<INT64_MAX, RowShape<1024, 0, C>>>(D, go);
 }
 
 // The same for the norm's gradients, which hold three matrices and sums besides: a
@@ -73,9 +88,9 @@ template <int C, typename F>
 void am_row_shape_lean(int64_t D, F go)
 {
     constexpr int k = 8 / C;
-    if (D > 1024 && D <= 2048) go(RowShape<256, 1 * k, C>{});
-    else if (D > 6144 && D <= 8192) go(RowShape<1024, 1 * k, C>{});
-    else am_row_shape<C>(D, go);
+    am_shape_of<UpTo<512, RowShape<64, 1 * k, C>>, UpTo<1024, RowShape<64, 2 * k, C>>, UpTo<2048, RowShape<256, 1 * k, C>>,
+                UpTo<4096, RowShape<256, 2 * k, C>>, UpTo<6144, RowShape<256, 3 * k, C>>, UpTo<8192, RowShape<1024, 1 * k, C>>,
+                UpTo<16384, RowShape<1024, 2 * k, C>>, UpTo<kRowHeld, RowShape<1024, 4 * k, C>>, UpTo<INT64_MAX, RowShape<1024, 0, C>>>(D, go);
 }
 
 // And for the norm forward, whose rows with their residuals' take twice the registers:
@@ -84,8 +99,10 @@ void am_row_shape_lean(int64_t D, F go)
 template <int C, typename F>
 void am_row_shape_norm(int64_t D, F go)
 {
-    if (D > 16384) go(RowShape<1024, 0, C>{});
-    else am_row_shape<C>(D, go);
+    constexpr int k = 8 / C;
+    am_shape_of<UpTo<512, RowShape<64, 1 * k, C>>, UpTo<1024, RowShape<64, 2 * k, C>>, UpTo<2048, RowShape<64, 4 * k, C>>,
+                UpTo<4096, RowShape<256, 2 * k, C>>, UpTo<6144, RowShape<256, 3 * k, C>>, UpTo<8192, RowShape<256, 4 * k, C>>,
+                UpTo<16384, RowShape<1024, 2 * k, C>>, UpTo<INT64_MAX, RowShape<1024, 0, C>>>(D, go);
 }
 
 // Workgroups for M rows: at most `most`, about as many as the chip holds at
