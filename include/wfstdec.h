@@ -770,6 +770,8 @@ int wfst_am_layer_norm(const wfst_am_layer_norm_args *args, void *hip_stream);
  *   workspace  at least wfst_am_layer_norm_backward_workspace bytes, 256-byte
  *            aligned
  *
+ * A row's sums are float32, of s, the squares of its differences, u and u times the
+ * differences: none may pass 3e38.
  * Errors: WFST_EINVAL, WFST_EDEVICE.
  */
 typedef struct wfst_am_layer_norm_backward_args {

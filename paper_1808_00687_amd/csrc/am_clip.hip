@@ -8,6 +8,10 @@
 // stores are not kept there.  125 tensors of 1.6 GB: 920 us, 4.9 GB in all, 5.3 TB/s (10
 // more forwards, 40 more with stores that are kept); the norm alone of 1 GB: 187 us, 5.7 TB/s.
 //
+// Tensors whose rows have gaps are slower: each 16 bytes' row and column are a division,
+// and nothing is on its way ahead.  1 GB of bf16 in rows of 8,192, 8 more apart: the
+// norm 340 us, without gaps 196, with outputs 780 and 585; f32 313, 198, 719 and 580.
+//
 // The sum is held in 64 bits (a square of a float32 may be no float32, and a
 // billion of them would lose bits): a workgroup's goes to the workspace, and every
 // workgroup of the second pass adds all of them up in the same order, so there is

@@ -373,10 +373,10 @@ __global__ __launch_bounds__(256) void layer_norm_columns_kernel(wfst_am_layer_n
     store_floats(partial + (gridDim.y + blockIdx.y) * D + c, D - c, db);
 }
 
-// Rows of few columns share a wave: (349525, 96) bf16 to 8 bits with the residual 63 us, with a wave a row
-// 217, (524288, 64) 44 and 317, (131072, 256) 43 and 83; backward of (349525, 96) with dsum 75 and 252, of (131072,
-// 256) 57 and 103.  Rows of 1,025 to 1,536 16-bit columns take three chunks a lane ((52429, 1280) to 8 bits with the
-// residual 101 us, in four 129).
+// Rows of few columns share a wave: (349525, 96) bf16 to 8 bits with the residual 50 us, with a wave a row 192,
+// (524288, 64) 42 and 280, (131072, 256) 42 and 73; backward of (349525, 96) with dsum 67 and 233, of (131072, 256) 55 and
+// 97.  Rows of 1,025 to 1,536 16-bit columns take three chunks a lane ((52429, 1280) to 8 bits with the residual 93 us, in
+// four 120; backward with dsum 112 and 118).
 template <int C, typename F>
 void row_shape(int64_t D, F go)
 {
@@ -387,9 +387,9 @@ void row_shape(int64_t D, F go)
                 UpTo<8192, RowShape<256, 4 * k, C>>, UpTo<16384, RowShape<1024, 2 * k, C>>, UpTo<INT64_MAX, RowShape<1024, 0, C>>>(D, go);
 }
 
-// And for the gradients: rows of 1,025 to 2,048 float32 columns take 256 threads ((11184, 1500) 53 us, a wave 67),
-// 16-bit ones a wave ((22369, 1500) 76, 256 threads 90).  Held up to 16,384 columns ((1024, 32768) bf16 132 us, held
-// 290, float32 123 and 251).
+// And for the gradients: rows of 1,025 to 2,048 float32 columns take 256 threads ((11184, 1500) 53 us, a wave 59),
+// 16-bit ones a wave ((22369, 1500) 68, 256 threads 130; (16384, 2048) 52 and 75).  Held up to 16,384 columns ((1024,
+// 32768) bf16 132 us, held 249, float32 247 and 473).
 template <int C, typename F>
 void row_shape_backward(int64_t D, F go)
 {
@@ -404,7 +404,10 @@ void row_shape_backward(int64_t D, F go)
 // Workgroups at most.  Backward about as many as are resident, by the bytes of a matrix that a thread holds: one
 // more and the last ones run alone (268 MB each, 1 to 5 a CU: 512 bf16 columns 95, 67, 62, 58, 57 us; 1,024 72, 52,
 // 51, 60, 57; 2,048 64, 52, 63, 61, 61; 8,192 72, 63, 76, 79, 78; 2,048 float32 64, 49, 50, 51, 54).
-constexpr int64_t kForwardBlocks = 256 * 32;   // (53274, 1024) to 8 bits: 8, 16, 24, 32, 64 a CU take 93, 97, 91, 90, 97
+//   Forward, 4, 8, 16, 24, 32 and 64 a CU: (53274, 1024) bf16 to 8 bits with the residual 80.5, 79.6, 76.7, 75.7, 74.2
+// and 71.6 us, without 49.3, 46.9, 44.6, 44.2, 43.1 and 45.5; (349525, 96) 58.7, 54.1, 51.6, 49.0, 48.6 and 47.6 with it;
+// (16384, 4096) 54.6 with 32 and 58.3 with 64 without.
+constexpr int64_t kForwardBlocks = 256 * 32;
 
 template <typename S>
 constexpr int64_t backward_blocks(int64_t el)
@@ -469,7 +472,8 @@ void launch_layer_norm_backward(const wfst_am_layer_norm_backward_args &a, hipSt
             if (M) layer_norm_backward_kernel<T, S><<<g, S::kThreads, 0, st>>>(a, wanted ? partial : nullptr, nullptr);
         } else if (M) {
             if (wanted) {
-                // the gradients of gain and bias before dx may overwrite dy
+                // The gradients of gain and bias before dx may overwrite dy.  In all s is gone through six times
+                // and dy four: (1024, 32768) bf16 with dsum 132 us, dx alone 71.
                 wfst_am_layer_norm_backward_args b = a;
                 b.dx.data = nullptr;
                 layer_norm_backward_kernel<T, S><<<g, S::kThreads, 0, st>>>(b, nullptr, moments);
