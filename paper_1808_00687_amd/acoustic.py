@@ -551,7 +551,8 @@ def wfst_am_clip(grads: Sequence[torch.Tensor], max_norm: float, *, out: Optiona
     ``max_norm`` (infinity: as they are), in ``out`` (a tensor of the same type
     and number of values for each, in the same order) or else in place; ``norm``
     [1] is that before the clipping (wfst_am_clip).  Tensors that are not dense
-    have to be matrices; a parameter's gradient may be of any shape."""
+    have to be matrices; a parameter's gradient may be of any shape, its last
+    dimension below 2^31."""
     if not isinstance(grads, (list, tuple)) or not grads:
         raise TypeError("grads must be a list of one tensor or more")
     d, n, keep = _device(grads[0], "grads"), len(grads), []

@@ -57,3 +57,33 @@ def test_gradients_of_rows_of_2_to_the_27_columns(am):
     off = (dg.double() - v * r * dy[0].double()).abs_()
     bound = (v.abs_().mul_(r * (3 * R.U32 + rel + R.U32)).add_(r * e_mean)).mul_(dy[0].double().abs())
     assert bool((off <= bound).all()), float((off - bound).max())
+
+
+def test_as_many_tensors_as_are_taken(am):
+    # descriptions in 924 launches; sizes from 1 to 37 values, all of them 1 / 64, so sums and the factor are exact
+    sizes = [1 + i * 7 % 37 for i in range(65536)]
+    flat = torch.full((sum(sizes),), 1 / 64, device="cuda")
+    out = torch.zeros_like(flat)
+    want = (sum(sizes) / 4096) ** 0.5
+    _, norm = am.wfst_am_clip(list(flat.split(sizes)), want / 8, out=list(out.split(sizes)))
+    assert abs(float(norm) - want) <= R.U32 * want * 1.001
+    assert float(out.min()) == float(out.max()) == 1 / 512
+    with pytest.raises(Exception, match="65536"):
+        am.wfst_am_clip([flat] + list(flat.split(sizes)), 1.0)
+
+
+def test_norms_of_more_than_32_bits_of_values(am):
+    # rows do not depend on one another; gradients of gain and bias are sums that float32 holds exactly
+    m, width = (1 << 22) + 5, 1032
+    x = torch.randn(m, width, device="cuda", dtype=BF16)
+    assert x.numel() > 1 << 32
+    tail = x[-9:].clone()
+    y, scale, _ = am.wfst_am_layer_norm(x, out_dtype=torch.float8_e4m3fn)
+    want, want_scale, _ = am.wfst_am_layer_norm(tail, out_dtype=torch.float8_e4m3fn)
+    assert torch.equal(y[-9:].view(torch.uint8), want.view(torch.uint8)) and torch.equal(scale[-9:], want_scale)
+    del y, scale
+    dy = torch.ones_like(x)
+    dx, _, db = am.wfst_am_layer_norm_backward(dy, x)
+    assert torch.equal(db, torch.full_like(db, m))
+    want, _, _ = am.wfst_am_layer_norm_backward(dy[-9:].clone(), tail)
+    assert torch.equal(dx[-9:], want)
