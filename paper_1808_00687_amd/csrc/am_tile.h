@@ -42,7 +42,7 @@
 // 255 and 288.  The matrix cores are busy 53% of the time (403 MB of reads behind the L2s
 // for two parts of both k-major; 1.3 GB when a part's tiles were dealt to all chiplets).
 // Gated, (16384, 1024, 4096): 244 us, 1,127 TFLOP/s (the library's plain product of twice the
-// outputs 246), with pre 310 (matrix cores busy 37%: 403 MB are stored while no products are
+// outputs 246), with pre 310 (matrix cores busy 37 to 39%: 403 MB are stored while no products are
 // formed).  No LDS bank conflicts but in
 // k-contiguous stages of 64 bytes, where they take 6 to 11% of a CU's cycles (7 to 9 in 8
 // bits, 11 in unaligned rows).  The rest is the waves' meeting once a stage and, for a
